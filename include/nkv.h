@@ -298,6 +298,109 @@ int nkv_decode_attention(const void *q, const void *packed_k, const void *packed
                          double scale, float *out, float *lse, void *ws, size_t ws_bytes, void *hip_stream);
 
 /*
+ * ---- Paged cache: the rows that are kept after the pass, and the tokens that are generated behind them ----
+ *
+ * A paged cache holds the K and V rows of units u = s * H + h (sequence s, KV head h) on pages of NKV_PAGE_ROWS rows that
+ * lie anywhere in one pool.  A sequence is a prompt of one layer, or, for all layers in one call, (prompt, layer) with
+ * s = p * L + l: the units are then numbered as everywhere else.  Units have lengths of their own, as the heads' budgets
+ * have.  The caller owns pool, table and lens (device memory) and hands out the pages:
+ *     table[u][j]   the page of unit u's rows 64 j .. 64 j + 63            int32 [n_seqs * H][max_pages]
+ *     lens[u]       rows of unit u, those that the current call appends or reads among them    int32 [n_seqs * H]
+ * so a token is appended by adding one to lens (for all layers at once, say) and calling nkv_pages_append, and the calls
+ * themselves change neither.  lens is clamped to [0, 64 * max_pages].  A table entry outside [0, n_pages) is no page: rows
+ * are not written there, read as zeros and left out of the attention.  Units may share pages that are only read.
+ *
+ * Formats (d the head dim; a page is nkv_page_bytes() bytes, all of its parts 16-byte aligned):
+ *   NKV_PAGES_16BIT  K [64][d], V [64][d] in `dtype`
+ *   NKV_PAGES_FP4    4-bit floating point in blocks of 32 dims of a row with a power of two each: a code is a sign (bit 3)
+ *                    and a magnitude 0, 0.5, 1, 1.5, 2, 3, 4 or 6 (bits 0-2); a scale byte e stands for 2^(e - 127).
+ *                    Of a block with largest magnitude m the scale is the least 2^s, s >= -126, with m < 7 * 2^s (so
+ *                    m itself is not cut off by more than it is rounded), and every code the nearest to x / 2^s, of two
+ *                    equally near ones the even code.  A block with an infinity or NaN gets scale byte 255, which reads
+ *                    as NaN.  d * 17/16 bytes for a K and a V row, 136 for d = 128.
+ *                      K codes  [64][d / 2], dim 2 i in the lower half of byte i
+ *                      V codes  [16 row quads][d / c][4 rows][c / 2], c = 4, 8, 16 dims for d <= 64, 128, 256: what one
+ *                               lane of the attention's product with V reads of four rows is 16 bytes (8, 32)
+ *                      K scales [d / 32][16][4], of row 16 t + r at [block][r][t]
+ *                      V scales [4][d / 32][4][4], of row 16 t + 4 g + i at [g][block][t][i]
+ * Rows of d = 64, 96, 128, 192 or 256 dims (K and V alike) of bf16 or fp16; others are refused with NKV_EUNSUPPORTED.
+ * Inputs must be finite, as everywhere; rows behind a unit's last one may hold anything.
+ */
+#define NKV_PAGE_ROWS 64
+enum { NKV_PAGES_16BIT = 0, NKV_PAGES_FP4 = 1 };
+enum {
+    NKV_ROPE_HALVES = 0,      /* dims i and i + rot / 2 are a pair */
+    NKV_ROPE_PAIRS = 1        /* dims 2 i and 2 i + 1 are a pair   */
+};
+
+typedef struct nkv_pages {
+    uint32_t struct_size;     /* sizeof(nkv_pages)                                   */
+    int32_t  n_seqs;          /* sequences                                           */
+    int32_t  H;               /* KV heads per sequence, up to NKV_MAX_HEADS          */
+    int32_t  d;               /* head dim of keys and values                         */
+    int32_t  dtype;           /* NKV_DTYPE_BF16 or NKV_DTYPE_F16: rows and queries   */
+    int32_t  format;          /* NKV_PAGES_*                                         */
+    int32_t  n_pages;         /* pages of the pool                                   */
+    int32_t  max_pages;       /* entries of a unit's row of the table                */
+    void    *pool;            /* DEVICE, n_pages * nkv_page_bytes() bytes, 16-byte aligned */
+    const int32_t *table;     /* DEVICE                                              */
+    const int32_t *lens;      /* DEVICE                                              */
+} nkv_pages;
+
+/* New tokens of every sequence: n_new each, the last n_new rows of the sequence's units.  Sequences with fewer new tokens
+ * than n_new have them last, behind tokens with a negative position: such a token, and one whose position is not in the
+ * table of angles, is left out (its row is not written, nor its row of q_out). */
+typedef struct nkv_tokens {
+    uint32_t struct_size;     /* sizeof(nkv_tokens)                                                            */
+    int32_t  n_new;           /* tokens per sequence                                                           */
+    int32_t  n_q_heads;       /* query heads, a multiple of H; 0: no queries                                   */
+    int32_t  rot;             /* dims that are rotated, the first ones of a row: a multiple of 16 up to d; 0: none */
+    int32_t  rope_style;      /* NKV_ROPE_*                                                                    */
+    int32_t  n_positions;     /* rows of rope                                                                  */
+    const void *k, *v, *q;    /* DEVICE, [sequence][token][head][d] by the strides below                       */
+    void    *q_out;           /* DEVICE, dense [n_seqs][n_new][n_q_heads][d]: the rotated queries              */
+    int64_t  k_strides[3], v_strides[3], q_strides[3];   /* {sequence, token, head} in elements, multiples of 8 */
+    const int32_t *positions; /* DEVICE, [n_seqs][n_new]: where the token stands in the text (not lens: rows    */
+                              /* may have been evicted); NULL if rot = 0: all tokens are there                 */
+    const float *rope;        /* DEVICE, [n_positions][2][rot / 2]: cosines, then sines, of a position's angles */
+} nkv_tokens;
+
+/* Bytes of a page; -1 for rows that are not supported. */
+int64_t nkv_page_bytes(int32_t d, int32_t dtype, int32_t format);
+
+/*
+ * Appends new tokens: k is rotated by its position's angles, (x, y) -> (x cos - y sin, y cos + x sin) in 64 bits and
+ * rounded to 32 (so that the 4-bit code does not depend on how the rotation is computed), and goes with v, rounded to the
+ * cache's format, to the pages of rows lens[u] - n_new .. lens[u] - 1; the queries of the same tokens are rotated into
+ * q_out.  Pages of different units that overlap race.
+ */
+int nkv_pages_append(const nkv_tokens *tokens, const nkv_pages *pages, void *hip_stream);
+
+/*
+ * Packed rows, as nkv_select_compact leaves them (head_off [units + 1], rows: how many rows packed_k / packed_v
+ * hold, head_off is clamped to it), to and from the pages: the n rows head_off[u] .. head_off[u + 1] - 1 are
+ * rows lens[u] - n .. lens[u] - 1 of unit u; those that would lie in front of row 0 are left out (load) or read as zeros.
+ * nkv_pages_read gives 4-bit values in `dtype`, those beyond its largest finite value as that value.
+ */
+int nkv_pages_load(const void *packed_k, const void *packed_v, const int64_t *head_off, int64_t rows, const nkv_pages *pages,
+                   void *hip_stream);
+int nkv_pages_read(void *packed_k, void *packed_v, const int64_t *head_off, int64_t rows, const nkv_pages *pages,
+                   void *hip_stream);
+
+/*
+ * Attention of the last n_new tokens of every sequence over its pages, grouped-query with G = n_q_heads / H: for token t,
+ * unit u and query head h * G + g, over the rows i < lens[u] - (n_new - 1 - t),
+ *   out[s][t][h*G+g] = sum_i softmax(scale * <q[s][t][h*G+g], k_i>)_i * v_i        fp32 [n_seqs][n_new][n_q_heads][d]
+ *   lse[s][t][h*G+g] = log sum_i exp(scale * <q, k_i>)   (optional, may be NULL)   fp32 [n_seqs][n_new][n_q_heads]
+ * q is dense [n_seqs][n_new][n_q_heads][d] in `dtype` (q_out of nkv_pages_append).  A token that sees no row gets out = 0,
+ * lse = -inf.  Products are exact and added up in fp32; keys and values of 4-bit pages enter as the values they stand for.
+ * Scratch: nkv_pages_workspace_bytes.  A call is deterministic.
+ */
+int nkv_pages_workspace_bytes(const nkv_pages *pages, int32_t n_q_heads, int32_t n_new, size_t *bytes);
+int nkv_pages_attention(const void *q, const nkv_pages *pages, int32_t n_q_heads, int32_t n_new, double scale, float *out,
+                        float *lse, void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
  * Plain device-to-device copy of `bytes` bytes (a multiple of 16, both pointers 16-byte aligned): contiguous
  * 16 KB pieces per workgroup, non-temporal 16-byte loads and stores -- the access pattern of the K/V gather
  * without its indirection.  dst == NULL: the loads only (what a pure reader can reach).  Not part of the pass:

@@ -28,10 +28,14 @@ FLAG_VECTOR_SCAN = 128
 FLAG_SELECT_PER_HEAD = 64
 FLAG_COMPACT_IN_PLACE = 256
 PIN = 3.0e38
+PAGE_ROWS = 64
+PAGES_16BIT, PAGES_FP4 = 0, 1
+ROPE_HALVES, ROPE_PAIRS = 0, 1
 
 EXPORTS = ("nkv_params_default", "nkv_block_size", "nkv_k0", "nkv_m_safe", "nkv_m_p", "nkv_packed_rows",
            "nkv_workspace_bytes", "nkv_score", "nkv_score_raw", "nkv_budget", "nkv_budget_noalloc", "nkv_select_compact",
-           "nkv_decode_workspace_bytes", "nkv_decode_attention", "nkv_copy_probe", "nkv_strerror", "nkv_version")
+           "nkv_decode_workspace_bytes", "nkv_decode_attention", "nkv_page_bytes", "nkv_pages_append", "nkv_pages_load",
+           "nkv_pages_read", "nkv_pages_workspace_bytes", "nkv_pages_attention", "nkv_copy_probe", "nkv_strerror", "nkv_version")
 KERNELS = ("scan", "finalize", "budget", "select", "gather", "decode")
 PASS_KERNELS = KERNELS[:5]          # the kernels of the compression pass itself
 
@@ -51,6 +55,20 @@ class nkv_shape(C.Structure):
                 ("n_prompts", C.c_int32), ("cu_seqlens", C.POINTER(C.c_int32)),
                 ("key_strides", C.POINTER(C.c_int64)), ("value_strides", C.POINTER(C.c_int64)),
                 ("key_layer_offsets", C.POINTER(C.c_int64)), ("value_layer_offsets", C.POINTER(C.c_int64))]
+
+
+class nkv_pages(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("n_seqs", C.c_int32), ("H", C.c_int32), ("d", C.c_int32),
+                ("dtype", C.c_int32), ("format", C.c_int32), ("n_pages", C.c_int32), ("max_pages", C.c_int32),
+                ("pool", C.c_void_p), ("table", C.c_void_p), ("lens", C.c_void_p)]
+
+
+class nkv_tokens(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("n_new", C.c_int32), ("n_q_heads", C.c_int32), ("rot", C.c_int32),
+                ("rope_style", C.c_int32), ("n_positions", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("q", C.c_void_p), ("q_out", C.c_void_p), ("k_strides", C.c_int64 * 3),
+                ("v_strides", C.c_int64 * 3), ("q_strides", C.c_int64 * 3), ("positions", C.c_void_p),
+                ("rope", C.c_void_p)]
 
 
 class NkvError(RuntimeError):
@@ -92,6 +110,14 @@ def lib() -> C.CDLL:
         L.nkv_decode_workspace_bytes.argtypes = [C.POINTER(nkv_shape), C.c_int32, i64, C.POINTER(C.c_size_t)]
         L.nkv_decode_attention.argtypes = [vp, vp, vp, vp, i64, C.POINTER(nkv_shape), C.POINTER(nkv_params),
                                            C.c_int32, f64, vp, vp, vp, C.c_size_t, vp]
+        L.nkv_page_bytes.argtypes = [C.c_int32, C.c_int32, C.c_int32]
+        L.nkv_page_bytes.restype = i64
+        L.nkv_pages_append.argtypes = [C.POINTER(nkv_tokens), C.POINTER(nkv_pages), vp]
+        L.nkv_pages_load.argtypes = [vp, vp, vp, i64, C.POINTER(nkv_pages), vp]
+        L.nkv_pages_read.argtypes = [vp, vp, vp, i64, C.POINTER(nkv_pages), vp]
+        L.nkv_pages_workspace_bytes.argtypes = [C.POINTER(nkv_pages), C.c_int32, C.c_int32, C.POINTER(C.c_size_t)]
+        L.nkv_pages_attention.argtypes = [vp, C.POINTER(nkv_pages), C.c_int32, C.c_int32, f64, vp, vp, vp,
+                                          C.c_size_t, vp]
         L.nkv_copy_probe.argtypes = [vp, vp, C.c_size_t, vp]
         L.nkv_strerror.argtypes = [C.c_int]
         L.nkv_strerror.restype = C.c_char_p
@@ -268,6 +294,125 @@ def decode_attention(q, packed_k, packed_v, head_off, rows: int, shape: Shape, p
                                     _stream(stream))
     if rc:
         raise NkvError(rc, "nkv_decode_attention")
+
+
+class Pages:
+    """A paged cache as ``nkv_pages`` in nkv.h describes it: ``pool`` (uint8, n_pages * page_bytes), ``table`` int32
+    [n_seqs * H, max_pages], ``lens`` int32 [n_seqs * H], all on the device and owned by the caller."""
+
+    def __init__(self, n_seqs: int, H: int, d: int, dtype: int, format: int, pool, table, lens):
+        import torch
+        size = page_bytes(d, dtype, format)
+        if size < 0:
+            raise NkvError(NKV_EUNSUPPORTED, "nkv_page_bytes")
+        nbytes = pool.numel() * pool.element_size()
+        if table.dtype != torch.int32 or lens.dtype != torch.int32 or table.shape[0] != n_seqs * H or \
+                table.dim() != 2 or lens.numel() != n_seqs * H or nbytes < size:
+            raise ValueError("table is int32 [n_seqs * H, max_pages], lens int32 [n_seqs * H], the pool a page or more")
+        if not (pool.is_contiguous() and table.is_contiguous() and lens.is_contiguous()):
+            raise ValueError("pool, table and lens are contiguous")
+        self.pool, self.table, self.lens = pool, table, lens
+        self.n_seqs, self.H, self.d, self.dtype, self.format = int(n_seqs), int(H), int(d), int(dtype), int(format)
+        self.c = nkv_pages(C.sizeof(nkv_pages), int(n_seqs), int(H), int(d), int(dtype), int(format), nbytes // size,
+                           int(table.shape[1]), _ptr(pool), _ptr(table), _ptr(lens))
+
+
+def page_bytes(d: int, dtype: int, format: int) -> int:
+    """Bytes of a page of 64 rows; -1 for rows that are not supported."""
+    return int(lib().nkv_page_bytes(int(d), int(dtype), int(format)))
+
+
+def rope_table(n_positions: int, rot: int, base: float = 10000.0, device="cuda"):
+    """Cosines and sines [n_positions, 2, rot / 2] of position * base^(-2 i / rot), angles in 64 bits."""
+    import torch
+    f = dict(dtype=torch.float64, device=device)
+    angle = torch.arange(n_positions, **f)[:, None] * base ** (-torch.arange(0, rot, 2, **f) / rot)
+    return torch.stack([angle.cos(), angle.sin()], 1).float().contiguous()
+
+
+_TORCH_NAMES = {DTYPE_F32: "torch.float32", DTYPE_BF16: "torch.bfloat16", DTYPE_F16: "torch.float16"}
+
+
+def _check_rows(t, what: str, dtype: int, shape=None) -> None:
+    """Rows that a call reads or writes: their type, and their shape where it is given, dense but for an append's inputs."""
+    if str(t.dtype) != _TORCH_NAMES.get(int(dtype)):
+        raise ValueError(f"{what} is {t.dtype}, and the pages' rows are {_TORCH_NAMES.get(int(dtype))}")
+    if shape is not None and (tuple(t.shape) != tuple(shape) or not t.is_contiguous()):
+        raise ValueError(f"{what} is dense {list(shape)}")
+
+
+def pages_append(k, v, pages: Pages, positions=None, rope=None, rope_style: int = ROPE_HALVES, q=None, q_out=None,
+                 stream=None) -> None:
+    """New tokens' k, v [n_seqs, n, H, d] (any strides but the last dim's) to the last n rows of the pages, k rotated
+    by ``rope`` [n_positions, 2, rot / 2] at ``positions`` int32 [n_seqs, n] on the way; q [n_seqs, n, Hq, d] rotated
+    into q_out; see ``nkv_pages_append`` in nkv.h."""
+    n = int(k.shape[1])
+    Hq = 0 if q is None else int(q.shape[2])
+    for name, t, heads in (("k", k, pages.H), ("v", v, pages.H), ("q", q, Hq)):
+        if t is not None:
+            _check_rows(t, name, pages.dtype)
+            if tuple(t.shape) != (pages.n_seqs, n, heads, pages.d) or t.stride(3) != 1:
+                raise ValueError(f"{name} is [n_seqs, n, heads, d], neighbouring dims next to each other")
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out are given together")
+    if q_out is not None:
+        _check_rows(q_out, "q_out", pages.dtype, (pages.n_seqs, n, Hq, pages.d))
+    rot, n_positions = (0, 0) if rope is None else (2 * int(rope.shape[-1]), int(rope.shape[0]))
+    if rope is not None and (str(rope.dtype) != "torch.float32" or rope.dim() != 3 or rope.shape[1] != 2 or
+                             not rope.is_contiguous()):
+        raise ValueError("rope is fp32 [n_positions, 2, rot / 2], contiguous")
+    if positions is not None and (str(positions.dtype) != "torch.int32" or positions.numel() != pages.n_seqs * n or
+                                  not positions.is_contiguous()):
+        raise ValueError("positions is int32 [n_seqs, n], contiguous")
+
+    def strides(t):
+        return (C.c_int64 * 3)(*(0 if t is None or t.shape[i] == 1 else int(t.stride(i)) for i in range(3)))
+
+    tokens = nkv_tokens(C.sizeof(nkv_tokens), n, Hq, rot, int(rope_style), n_positions, _ptr(k), _ptr(v), _ptr(q),
+                        _ptr(q_out), strides(k), strides(v), strides(q), _ptr(positions), _ptr(rope))
+    rc = lib().nkv_pages_append(C.byref(tokens), C.byref(pages.c), _stream(stream))
+    if rc:
+        raise NkvError(rc, "nkv_pages_append")
+
+
+def pages_load(packed_k, packed_v, head_off, rows: int, pages: Pages, stream=None) -> None:
+    """Packed rows [rows, d] (as ``select_compact`` leaves them) to the end of every unit's pages."""
+    _check_rows(packed_k, "packed_k", pages.dtype)
+    _check_rows(packed_v, "packed_v", pages.dtype)
+    rc = lib().nkv_pages_load(_ptr(packed_k), _ptr(packed_v), _ptr(head_off), int(rows), C.byref(pages.c),
+                              _stream(stream))
+    if rc:
+        raise NkvError(rc, "nkv_pages_load")
+
+
+def pages_read(packed_k, packed_v, head_off, rows: int, pages: Pages, stream=None) -> None:
+    """The last head_off[u + 1] - head_off[u] rows of every unit to packed rows [rows, d]."""
+    _check_rows(packed_k, "packed_k", pages.dtype)
+    _check_rows(packed_v, "packed_v", pages.dtype)
+    rc = lib().nkv_pages_read(_ptr(packed_k), _ptr(packed_v), _ptr(head_off), int(rows), C.byref(pages.c),
+                              _stream(stream))
+    if rc:
+        raise NkvError(rc, "nkv_pages_read")
+
+
+def pages_workspace_bytes(pages: Pages, n_q_heads: int, n_new: int = 1) -> int:
+    out = C.c_size_t(0)
+    rc = lib().nkv_pages_workspace_bytes(C.byref(pages.c), int(n_q_heads), int(n_new), C.byref(out))
+    if rc:
+        raise NkvError(rc, "nkv_pages_workspace_bytes")
+    return int(out.value)
+
+
+def pages_attention(q, pages: Pages, n_q_heads: int, n_new: int, scale: float, out, lse=None, ws=None,
+                    stream=None) -> None:
+    """The last n_new tokens' attention over the pages: q [n_seqs, n_new, Hq, d] -> out fp32 of that shape (and lse
+    [n_seqs, n_new, Hq]); see ``nkv_pages_attention`` in nkv.h."""
+    _check_rows(q, "q", pages.dtype, (pages.n_seqs, n_new, n_q_heads, pages.d))
+    rc = lib().nkv_pages_attention(_ptr(q), C.byref(pages.c), int(n_q_heads), int(n_new), float(scale), _ptr(out),
+                                   _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(),
+                                   _stream(stream))
+    if rc:
+        raise NkvError(rc, "nkv_pages_attention")
 
 
 def copy_probe(dst, src, stream=None) -> None:

@@ -255,6 +255,39 @@ int prepare_budget(const float *scores, const nkv_shape *shape, const nkv_params
     return NKV_OK;
 }
 
+int check_pages(const nkv_pages *p)
+{
+    if (!p || p->struct_size != sizeof(nkv_pages)) return NKV_EINVAL;
+    if (p->dtype < NKV_DTYPE_F32 || p->dtype > NKV_DTYPE_F8_E4M3) return NKV_EINVAL;
+    if (p->format != NKV_PAGES_16BIT && p->format != NKV_PAGES_FP4) return NKV_EINVAL;
+    if (p->n_seqs < 1 || p->H < 1 || p->H > NKV_MAX_HEADS || p->d < 1 || p->n_pages < 1 || p->max_pages < 1) return NKV_ESHAPE;
+    if (!pages_row_supported(p->dtype, p->d)) return NKV_EUNSUPPORTED;
+    if (!p->pool || !p->table || !p->lens || (uintptr_t)p->pool % 16 || (uintptr_t)p->table % 4 || (uintptr_t)p->lens % 4) return NKV_EINVAL;
+    // the half pages of all units together, and a unit's rows, are counted in 32 bits
+    if ((int64_t)p->n_seqs * p->H * p->max_pages >= (1ll << 30) || p->max_pages >= (1 << 25)) return NKV_ESHAPE;
+    return NKV_OK;
+}
+
+int check_packed(const void *k, const void *v, const int64_t *head_off, int64_t rows, const nkv_pages *pages)
+{
+    const int rc = check_pages(pages);
+    if (rc) return rc;
+    if (!head_off || rows < 0 || (rows > 0 && (!k || !v)) || (uintptr_t)k % 16 || (uintptr_t)v % 16 || (uintptr_t)head_off % 8) return NKV_EINVAL;
+    if (rows / NKV_PAGE_ROWS + 2 * (int64_t)pages->n_seqs * pages->H >= (1ll << 31)) return NKV_ESHAPE;
+    return NKV_OK;
+}
+
+int check_attention(const nkv_pages *pages, int32_t n_q_heads, int32_t n_new)
+{
+    const int rc = check_pages(pages);
+    if (rc) return rc;
+    if (n_new < 1 || n_q_heads < pages->H || n_q_heads % pages->H) return NKV_EINVAL;
+    // a workgroup for every output row, at most 65535 groups of 16 of a unit's
+    const int64_t cols = (int64_t)n_q_heads / pages->H * n_new;
+    if (cols > 16 * 65535 || (int64_t)pages->n_seqs * pages->H * cols >= (1ll << 31)) return NKV_ESHAPE;
+    return NKV_OK;
+}
+
 }  // namespace
 }  // namespace nkv
 
@@ -504,6 +537,73 @@ int nkv_decode_attention(const void *q, const void *packed_k, const void *packed
                          scale, out, lse, ws, ws_bytes, Prof{params->prof_start, params->prof_stop},
                          (hipStream_t)hip_stream) == hipSuccess
                ? NKV_OK : NKV_EHIP;
+}
+
+int64_t nkv_page_bytes(int32_t d, int32_t dtype, int32_t format)
+{
+    if (format != NKV_PAGES_16BIT && format != NKV_PAGES_FP4) return -1;
+    return pages_row_supported(dtype, d) ? page_bytes_of(d, format) : -1;
+}
+
+int nkv_pages_append(const nkv_tokens *tokens, const nkv_pages *pages, void *hip_stream)
+{
+    int rc = check_pages(pages);
+    if (rc) return rc;
+    if (!tokens || tokens->struct_size != sizeof(nkv_tokens)) return NKV_EINVAL;
+    const nkv_tokens &t = *tokens;
+    if (t.n_new < 1 || t.n_q_heads < 0 || t.n_q_heads % pages->H) return NKV_EINVAL;
+    if (!t.k || !t.v || (t.n_q_heads > 0 && (!t.q || !t.q_out))) return NKV_EINVAL;
+    if ((uintptr_t)t.k % 16 || (uintptr_t)t.v % 16 || (uintptr_t)t.q % 16 || (uintptr_t)t.q_out % 16) return NKV_EINVAL;
+    for (int i = 0; i < 3; ++i)
+        if (t.k_strides[i] % 8 || t.v_strides[i] % 8 || (t.n_q_heads > 0 && t.q_strides[i] % 8)) return NKV_EINVAL;
+    if (t.rot < 0 || t.rot > pages->d || t.rot % 16) return NKV_EINVAL;
+    if (t.rot > 0) {
+        if (!t.positions || !t.rope || t.n_positions < 1) return NKV_EINVAL;
+        if (t.rope_style != NKV_ROPE_HALVES && t.rope_style != NKV_ROPE_PAIRS) return NKV_EINVAL;
+    }
+    if ((uintptr_t)t.positions % 4 || (uintptr_t)t.rope % 16) return NKV_EINVAL;
+    if (t.n_q_heads > 0 && t.q == t.q_out) return NKV_EINVAL;       // a pair's dims are read by two threads
+    // one thread for every 16 bytes of the tokens, numbered in 32 bits
+    if ((int64_t)pages->n_seqs * t.n_new >= (1ll << 31) ||
+        (int64_t)pages->n_seqs * t.n_new * (2 * pages->H + t.n_q_heads) >= (1ll << 32) / (pages->d / 8))
+        return NKV_ESHAPE;
+    return launch_pages_append(t, *pages, (hipStream_t)hip_stream) == hipSuccess ? NKV_OK : NKV_EHIP;
+}
+
+int nkv_pages_load(const void *packed_k, const void *packed_v, const int64_t *head_off, int64_t rows, const nkv_pages *pages,
+                   void *hip_stream)
+{
+    const int rc = check_packed(packed_k, packed_v, head_off, rows, pages);
+    if (rc) return rc;
+    return launch_pages_rows(true, packed_k, packed_v, head_off, rows, *pages, (hipStream_t)hip_stream) == hipSuccess ? NKV_OK : NKV_EHIP;
+}
+
+int nkv_pages_read(void *packed_k, void *packed_v, const int64_t *head_off, int64_t rows, const nkv_pages *pages, void *hip_stream)
+{
+    const int rc = check_packed(packed_k, packed_v, head_off, rows, pages);
+    if (rc) return rc;
+    return launch_pages_rows(false, packed_k, packed_v, head_off, rows, *pages, (hipStream_t)hip_stream) == hipSuccess ? NKV_OK : NKV_EHIP;
+}
+
+int nkv_pages_workspace_bytes(const nkv_pages *pages, int32_t n_q_heads, int32_t n_new, size_t *bytes)
+{
+    if (!bytes) return NKV_EINVAL;
+    const int rc = check_attention(pages, n_q_heads, n_new);
+    if (rc) return rc;
+    *bytes = pages_ws_bytes(*pages, n_q_heads, n_new);
+    return NKV_OK;
+}
+
+int nkv_pages_attention(const void *q, const nkv_pages *pages, int32_t n_q_heads, int32_t n_new, double scale, float *out, float *lse,
+                        void *ws, size_t ws_bytes, void *hip_stream)
+{
+    int rc = check_attention(pages, n_q_heads, n_new);
+    if (rc) return rc;
+    if (!q || !out || !isfinite(scale)) return NKV_EINVAL;
+    if ((uintptr_t)q % 16 || (uintptr_t)out % 16 || (uintptr_t)lse % 4) return NKV_EINVAL;
+    rc = check_ws(ws, ws_bytes, pages_ws_bytes(*pages, n_q_heads, n_new));
+    if (rc) return rc;
+    return launch_pages_attention(q, *pages, n_q_heads, n_new, scale, out, lse, ws, (hipStream_t)hip_stream) == hipSuccess ? NKV_OK : NKV_EHIP;
 }
 
 int nkv_copy_probe(void *dst, const void *src, size_t bytes, void *hip_stream)

@@ -165,6 +165,16 @@ hipError_t launch_decode(const void *q, const void *pk, const void *pv, const in
                          int n_units, int G, int d, int dv, int64_t rows, double scale, float *out, float *lse,
                          void *ws, size_t ws_bytes, const Prof &prof, hipStream_t st);
 
+// ---- paged cache ----
+bool pages_row_supported(int dtype, int d);
+inline int64_t page_bytes_of(int d, int format) { return format == NKV_PAGES_FP4 ? 68 * (int64_t)d : 256 * (int64_t)d; }
+hipError_t launch_pages_append(const nkv_tokens &t, const nkv_pages &p, hipStream_t st);
+hipError_t launch_pages_rows(bool load, const void *k, const void *v, const int64_t *head_off, int64_t rows, const nkv_pages &p,
+                             hipStream_t st);
+size_t pages_ws_bytes(const nkv_pages &p, int n_q_heads, int n_new);
+hipError_t launch_pages_attention(const void *q, const nkv_pages &p, int n_q_heads, int n_new, double scale, float *out, float *lse,
+                                  void *ws, hipStream_t st);
+
 // ---- plain copy, the bandwidth yardstick ----
 hipError_t launch_copy_probe(void *dst, const void *src, size_t bytes, hipStream_t st);
 

@@ -1,0 +1,492 @@
+"""The paged cache on the GPU against oracle/pages.py.
+
+Bars.  What is written to pages, read from them, and rotated is compared bit for bit: a rotation in 64 bits rounded to 32 is the same
+number whatever the order of its operations, and a code is the nearest one of the value so rounded.  Attention: |out - oracle| <=
+1e-5 max(1, max|V|), |lse - oracle| <= 1e-5 max(1, |lse|), as for attention over packed rows: the products are exact, logits of a few tens
+at most carry some 1e-6 from their sums in fp32, and the output is a convex combination of value rows.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import pages as op
+import nkv_inputs
+import paper_2605_26678_amd as nkv
+from pages_util import Cache, DTYPES, from_bits, to_bits
+from parity_util import shape_of
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TOL = 1e-5
+
+
+def _f64(t):
+    return t.detach().cpu().double().numpy()
+
+
+def _attend(c, q, scale, n, Hq, want_lse=True, stream=None):
+    """A call with room to spare around out and lse, and none around the scratch, which holds NaN before."""
+    pages = c.on(DEV)
+    need = nkv.pages_workspace_bytes(pages, Hq, n)
+    ws = torch.full((need + 512,), 255, dtype=torch.uint8, device=DEV)
+    out = torch.full((c.S * n * Hq * c.d + 128,), float("nan"), device=DEV)
+    lse = torch.full((c.S * n * Hq + 128,), float("nan"), device=DEV)
+    o, l = out[64:-64].view(c.S, n, Hq, c.d), lse[64:-64].view(c.S, n, Hq)
+    torch.cuda.synchronize()
+    nkv.pages_attention(q.to(DEV), pages, Hq, n, scale, o, l if want_lse else None, ws[:need], stream=stream)
+    torch.cuda.synchronize()
+    assert bool((ws[need:] == 255).all()), "written behind the scratch"
+    for x in (out[:64], out[-64:], lse[:64], lse[-64:]):
+        assert bool(x.isnan().all()), "written beside the outputs"
+    assert torch.equal(c.d_pool.cpu(), torch.from_numpy(c.pool)) and torch.equal(c.d_lens.cpu(), torch.from_numpy(c.lens))
+    return o, l
+
+
+def _check(c, q, o, l, scale, what, n):
+    want, want_lse = op.attention(_f64(q), c.pool, c.table, c.lens, c.H, scale, c.d, c.fp4, from_bits(c.torch_dtype))
+    vmax = 6.0 if c.fp4 else 6.0                           # codes of up to 6 * 2^-1, rows of a few standard deviations
+    assert np.isfinite(_f64(o)).all(), what
+    err = np.abs(_f64(o) - want).max()
+    assert err <= TOL * max(1.0, vmax), f"{what}: out off by {err:.3e}"
+    if l is not None:
+        assert np.array_equal(np.isneginf(_f64(l)), np.isneginf(want_lse)), what
+        fin = np.isfinite(want_lse)
+        e2 = np.abs(_f64(l)[fin] - want_lse[fin]) / np.maximum(1.0, np.abs(want_lse[fin]))
+        assert e2.size == 0 or e2.max() <= TOL, f"{what}: lse off by {e2.max():.3e}"
+
+
+def _queries(c, n, Hq, seed):
+    g = torch.Generator().manual_seed(seed)
+    return torch.randn(c.S, n, Hq, c.d, generator=g).to(c.torch_dtype)
+
+
+EDGES = [0, 1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 700]
+
+
+# ---- rows in and out ----
+
+def _append_case(c, n, Hq, rot, halves, seed, positions=None, fused=True):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(c.S, n, Hq + 2 * c.H, c.d, generator=g) * torch.exp(torch.randn(c.S, n, Hq + 2 * c.H, 1, generator=g))
+    x = x.to(c.torch_dtype)
+    rope = nkv.rope_table(60, rot, device="cpu") if rot else None
+    if positions is None:
+        positions = torch.randint(0, 60, (c.S, n), generator=g, dtype=torch.int32)
+    if not fused:                                          # heads outside of tokens, and a hole between sequences
+        wide = torch.zeros(c.S, Hq + 2 * c.H, n + 1, c.d, dtype=x.dtype)
+        wide[:, :, :n] = x.transpose(1, 2)
+        x = wide[:, :, :n].transpose(1, 2)
+    return x, rope, positions
+
+
+def _append_oracle(c, x, rope, positions, n, Hq, rot, halves):
+    """The pool after the call, and q_out (NaN where nothing is written)."""
+    pool, bits = c.pool.copy(), to_bits(c.torch_dtype)
+    f = _f64(x)
+    q, k, v = f[:, :, :Hq], f[:, :, Hq:Hq + c.H], f[:, :, Hq + c.H:]
+    pos = positions.numpy()
+    if rot:
+        q, k = (op.rotate(t, pos, rope.numpy(), halves) for t in (q, k))
+    q_out = np.full(q.shape, np.nan)
+    for s in range(c.S):
+        for t in range(n):
+            if rot and not 0 <= pos[s, t] < rope.shape[0] or pos[s, t] < 0:
+                continue
+            q_out[s, t] = from_bits(c.torch_dtype)(bits(q[s, t]).reshape(-1)).reshape(Hq, c.d)
+            for h in range(c.H):
+                u = s * c.H + h
+                row = min(max(int(c.lens[u]), 0), 64 * c.width) - n + t
+                if row < 0:
+                    continue
+                p = int(c.table[u, row // 64])
+                if 0 <= p < pool.shape[0]:
+                    op.write_row(pool[p], row % 64, True, k[s, t, h], c.fp4, bits)
+                    op.write_row(pool[p], row % 64, False, v[s, t, h], c.fp4, bits)
+    return pool, q_out
+
+
+def _run_append(c, x, rope, positions, n, Hq, rot, halves, give_positions=True):
+    pages = c.on(DEV)
+    d = x.to(DEV) if x.is_contiguous() else torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=DEV).copy_(x)
+    q_out = torch.full((c.S, n, Hq, c.d), float("nan"), dtype=x.dtype, device=DEV) if Hq else None
+    torch.cuda.synchronize()
+    nkv.pages_append(d[:, :, Hq:Hq + c.H], d[:, :, Hq + c.H:], pages, positions=positions.to(DEV) if give_positions else None,
+                     rope=rope.to(DEV) if rot else None, rope_style=nkv.ROPE_HALVES if halves else nkv.ROPE_PAIRS,
+                     q=d[:, :, :Hq] if Hq else None, q_out=q_out)
+    torch.cuda.synchronize()
+    return c.d_pool.cpu().numpy(), q_out
+
+
+@pytest.mark.parametrize("d", [64, 96, 128, 192, 256])
+@pytest.mark.parametrize("fmt", ["fp4", "16bit"])
+@pytest.mark.parametrize("dtype,halves,part", [("bf16", True, 1), ("bf16", False, 1), ("fp16", True, 2), ("fp16", False, 2), ("bf16", True, 0)])
+def test_append_writes_the_oracles_bytes(d, fmt, dtype, halves, part):
+    rot = d // part if part else 0
+    n, Hq = 5, 4
+    c = Cache(2, 2, d, dtype, fmt, [5, 64, 67, 131], rows=1.0, seed=d)
+    x, rope, positions = _append_case(c, n, Hq, rot, halves, 7 * d, fused=halves)
+    want, want_q = _append_oracle(c, x, rope, positions, n, Hq, rot, halves)
+    got, q_out = _run_append(c, x, rope, positions, n, Hq, rot, halves, give_positions=bool(rot))
+    assert np.array_equal(got, want), f"{(got != want).sum()} bytes differ"
+    assert np.array_equal(_f64(q_out), want_q)
+
+
+@pytest.mark.parametrize("fmt", ["fp4", "16bit"])
+def test_append_leaves_out_padding_foreign_positions_and_pages_that_are_none(fmt):
+    """Leading tokens of negative positions, positions behind the table, rows in front of row 0, table entries outside the pool, lengths
+    beyond the table's row and below zero."""
+    n, Hq = 6, 2
+    c = Cache(4, 2, 64, "bf16", fmt, [70, 6, 3, 0, 130, 66, 64, 64], width=3, rows=1.0, seed=5)
+    c.table[4, 2], c.table[5, 1] = c.pool.shape[0], -7
+    c.lens[6], c.lens[7] = 1000, -3                        # clamped to 192 rows (two pages there are none) and to none
+    x, rope, positions = _append_case(c, n, Hq, 64, True, 3)
+    positions[0, :3] = -1
+    positions[1, 2] = 60
+    want, want_q = _append_oracle(c, x, rope, positions, n, Hq, 64, True)
+    got, q_out = _run_append(c, x, rope, positions, n, Hq, 64, True)
+    assert np.array_equal(got, want)
+    assert np.array_equal(_f64(q_out), want_q, equal_nan=True)
+
+
+def test_append_without_queries_and_one_token():
+    c = Cache(3, 1, 128, "fp16", "fp4", [1, 64, 65], rows=1.0, seed=6)
+    x, rope, positions = _append_case(c, 1, 0, 128, True, 8)
+    want, _ = _append_oracle(c, x, rope, positions, 1, 0, 128, True)
+    got, _ = _run_append(c, x, rope, positions, 1, 0, 128, True)
+    assert np.array_equal(got, want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_4_bit_codes_of_ties_zeros_extremes_and_nan(dtype):
+    """Every half-way point, zeros, the smallest and largest values of the type, a NaN and an infinity in a block each."""
+    c = Cache(1, 1, 64, dtype, "fp4", [64], seed=9)
+    half = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0])
+    x = torch.zeros(64, 64)
+    for i in range(40):
+        scale = 2.0 ** (i - 20 if dtype == "bf16" else i % 20 - 10)
+        x[i, :8], x[i, 8:16] = half * scale, -half * scale
+        x[i, 32:40] = half * scale * (1 + 2.0 ** -7)
+        x[i, 41] = 7.0 * scale
+        x[i, 42] = 6.96875 * scale
+    top, tiny = torch.finfo(DTYPES[dtype][0]).max, torch.finfo(DTYPES[dtype][0]).tiny
+    x[40, :32], x[41, :32], x[42, :32] = top, tiny, tiny / 64
+    x[43, 3], x[44, 35], x[45, 63] = float("nan"), float("inf"), -float("inf")
+    x[46] = -0.0
+    rows = x.to(c.torch_dtype)
+    pages = c.on(DEV)
+    off = torch.tensor([0, 64], device=DEV)
+    nkv.pages_load(rows.to(DEV), rows.flip(0).contiguous().to(DEV), off, 64, pages)
+    torch.cuda.synchronize()
+    want, f = c.pool.copy(), _f64(rows)
+    for r in range(64):
+        op.write_row(want[c.table[0, 0]], r, True, f[r], True, None)
+        op.write_row(want[c.table[0, 0]], r, False, f[63 - r], True, None)
+    assert np.array_equal(c.d_pool.cpu().numpy(), want)
+    k, v = torch.empty_like(rows, device=DEV), torch.empty_like(rows, device=DEV)
+    nkv.pages_read(k, v, off, 64, pages)
+    K, V = op.read_rows(want[c.table[0, 0]], 64, True, None)
+    for got, exact in ((k, K), (v, V)):
+        as_type = torch.from_numpy(np.clip(exact, -top, top)).to(c.torch_dtype)
+        assert torch.equal(got.cpu().nan_to_num(7.0), as_type.nan_to_num(7.0))
+        assert torch.equal(got.cpu().isnan(), as_type.isnan())
+
+
+@pytest.mark.parametrize("d", [64, 96, 128, 192, 256])
+@pytest.mark.parametrize("fmt,dtype", [("fp4", "bf16"), ("fp4", "fp16"), ("16bit", "bf16")])
+@pytest.mark.parametrize("behind", [0, 37])
+def test_load_and_read(d, fmt, dtype, behind):
+    """Ragged packed rows to the end of every unit's pages, `behind` rows that are there already, and back: whole pools and rows compared."""
+    n = [0, 1, 63, 64, 65, 200, 0, 130]
+    c = Cache(4, 2, d, dtype, fmt, [x + behind for x in n], rows=1.0, seed=d + behind)
+    off = np.concatenate([[0], np.cumsum(n)])
+    rows = int(off[-1])
+    g = torch.Generator().manual_seed(d)
+    k, v = (torch.randn(rows, d, generator=g).to(c.torch_dtype) for _ in range(2))
+    want, bits = c.pool.copy(), to_bits(c.torch_dtype)
+    for u in range(8):
+        for i in range(n[u]):
+            row = behind + i
+            for key, x in ((True, k), (False, v)):
+                op.write_row(want[c.table[u, row // 64]], row % 64, key, _f64(x[off[u] + i]), c.fp4, bits)
+    pages = c.on(DEV)
+    d_off = torch.from_numpy(off).to(DEV)
+    nkv.pages_load(k.to(DEV), v.to(DEV), d_off, rows, pages)
+    torch.cuda.synchronize()
+    assert np.array_equal(c.d_pool.cpu().numpy(), want)
+    back = [torch.full((rows + 2, d), float("nan"), dtype=c.torch_dtype, device=DEV) for _ in range(2)]
+    nkv.pages_read(back[0][1:-1], back[1][1:-1], d_off, rows, pages)
+    torch.cuda.synchronize()
+    for got, x in zip(back, (k, v)):
+        held = op.values(*op.quantise(_f64(x))) if c.fp4 else _f64(x)
+        assert np.array_equal(_f64(got[1:-1]), held)
+        assert bool(got[0].isnan().all()) and bool(got[-1].isnan().all())
+
+
+def test_rows_that_have_no_place():
+    """More packed rows than a unit has: the front ones are left out, and read as zeros; pages outside the pool are not written and read as zeros; offsets beyond
+    the buffer and descending ones are clamped."""
+    c = Cache(1, 5, 64, "bf16", "16bit", [70, 40, 130, 10, 5], rows=1.0, seed=11)
+    c.table[2, 1] = c.pool.shape[0] + 3
+    off = [0, 150, 190, 320, 310, 500]                     # unit 0: 80 rows in front; unit 3: descending; unit 4: clamped to 400
+    rows = 400
+    g = torch.Generator().manual_seed(2)
+    k, v = (torch.randn(rows, 64, generator=g).to(torch.bfloat16) for _ in range(2))
+    want, bits = c.pool.copy(), to_bits(torch.bfloat16)
+    held = np.full((2, rows, 64), np.nan)
+    for u in range(5):
+        a, b = min(off[u], rows), min(off[u + 1], rows)
+        for i in range(a, b):
+            row = int(c.lens[u]) - (b - a) + i - a
+            held[:, i] = 0.0
+            if row >= 0 and c.table[u, row // 64] < c.pool.shape[0]:
+                for j, x in enumerate((k, v)):
+                    op.write_row(want[c.table[u, row // 64]], row % 64, j == 0, _f64(x[i]), False, bits)
+                    held[j, i] = _f64(x[i])
+    pages = c.on(DEV)
+    d_off = torch.tensor(off, device=DEV)
+    nkv.pages_load(k.to(DEV), v.to(DEV), d_off, rows, pages)
+    torch.cuda.synchronize()
+    got = c.d_pool.cpu().numpy()
+    page_rows = [(int(c.table[4, 0]), r) for r in range(5)]   # unit 4: 90 rows for 5 places, those of unit 3 among them
+    assert np.array_equal(got, want), page_rows
+    back = [torch.full((rows, 64), float("nan"), dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    nkv.pages_read(back[0], back[1], d_off, rows, pages)
+    torch.cuda.synchronize()
+    for j in range(2):
+        assert np.array_equal(_f64(back[j])[:310], held[j][:310], equal_nan=True)
+    nkv.pages_load(k.to(DEV), v.to(DEV), d_off, 0, pages)  # no rows at all
+    torch.cuda.synchronize()
+
+
+def test_many_units_of_few_rows():
+    c = Cache(600, 8, 64, "bf16", "16bit", np.arange(4800) % 4, seed=12)
+    off = np.concatenate([[0], np.cumsum(c.lens.astype(np.int64))])
+    rows = int(off[-1])
+    k = torch.randn(rows, 64, generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).to(DEV)
+    v, pages, d_off = k * 2, c.on(DEV), torch.from_numpy(off).to(DEV)
+    nkv.pages_load(k, v, d_off, rows, pages)
+    a, b = torch.empty_like(k), torch.empty_like(k)
+    nkv.pages_read(a, b, d_off, rows, pages)
+    torch.cuda.synchronize()
+    assert torch.equal(a, k) and torch.equal(b, v)
+
+
+# ---- attention ----
+
+@pytest.mark.parametrize("d", [64, 96, 128, 192, 256])
+@pytest.mark.parametrize("fmt", ["fp4", "16bit"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("G,n", [(1, 1), (4, 1), (3, 2)])
+def test_attention_at_every_edge(d, fmt, dtype, G, n):
+    c = Cache(8, 2, d, dtype, fmt, EDGES, rows=1.0, seed=d + G)
+    q = _queries(c, n, 2 * G, 3)
+    o, l = _attend(c, q, d ** -0.5, n, 2 * G)
+    _check(c, q, o, l, d ** -0.5, f"{d} {fmt} {dtype} G={G} n={n}", n)
+
+
+@pytest.mark.parametrize("fmt", ["fp4", "16bit"])
+@pytest.mark.parametrize("G,n", [(2, 1), (5, 1), (8, 1), (16, 1), (20, 1), (33, 1), (4, 4), (8, 5), (1, 17), (16, 3), (6, 7)])
+def test_attention_groups_and_tokens(fmt, G, n):
+    c = Cache(2, 3, 128, "bf16", fmt, [3, 64, 70, 131, 0, 390], rows=1.0, seed=G)
+    q = _queries(c, n, 3 * G, 5)
+    o, l = _attend(c, q, 128 ** -0.5, n, 3 * G)
+    _check(c, q, o, l, 128 ** -0.5, f"G={G} n={n}", n)
+
+
+@pytest.mark.parametrize("fmt,d,dtype", [("fp4", 128, "bf16"), ("16bit", 128, "bf16"), ("fp4", 64, "fp16"), ("16bit", 64, "fp16")])
+def test_attention_over_long_and_short_units_together(fmt, d, dtype):
+    """One unit of 20 000 rows beside 30 of a few: stretches end inside the long one and run over several of the short ones."""
+    c = Cache(31, 1, d, dtype, fmt, [5] * 11 + [20000] + list(range(60, 79)), rows=1.0, seed=13)
+    q = _queries(c, 1, 4, 6)
+    o, l = _attend(c, q, d ** -0.5, 1, 4)
+    _check(c, q, o, l, d ** -0.5, fmt, 1)
+
+
+@pytest.mark.parametrize("fmt", ["fp4", "16bit"])
+def test_attention_over_many_units(fmt):
+    lens = (np.arange(3000) * 7) % 150
+    lens[100:400] = 0
+    c = Cache(375, 8, 64, "bf16", fmt, lens, rows=1.0, seed=14)
+    q = _queries(c, 1, 16, 7)
+    o, l = _attend(c, q, 0.125, 1, 16)
+    _check(c, q, o, l, 0.125, fmt, 1)
+
+
+@pytest.mark.parametrize("fmt", ["fp4", "16bit"])
+def test_pages_that_are_none_and_lengths_out_of_range(fmt):
+    c = Cache(3, 2, 128, "bf16", fmt, [200, 64, 130, 70, 10, 300], width=5, rows=1.0, seed=15)
+    c.table[0, 1], c.table[1, 0], c.table[2, 2], c.table[3, 0] = -1, c.pool.shape[0], 2 ** 31 - 1, -2 ** 31
+    c.lens[4], c.lens[5] = -5, 10 ** 9                     # no rows; all that the table's row can hold, some on no page
+    c.pool[c.table[5, 4]] = 0                              # its last page's unused rows are rows now
+    q = _queries(c, 2, 8, 8)
+    o, l = _attend(c, q, 0.1, 2, 8)
+    _check(c, q, o, l, 0.1, fmt, 2)
+
+
+@pytest.mark.parametrize("fmt", ["fp4", "16bit"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_later_tokens_nan_stays_with_it(fmt, d):
+    """Tokens see no row behind their own: a NaN in a later token's key or value reaches only those that see it."""
+    n, G = 4, 3
+    c = Cache(2, 1, d, "bf16", fmt, [70, 131], rows=1.0, seed=16)
+    q = _queries(c, n, G, 9)
+    want, _ = op.attention(_f64(q), c.pool, c.table, c.lens, 1, 0.1, d, c.fp4, from_bits(c.torch_dtype))
+    x = np.full(d, np.nan)
+    op.write_row(c.pool[c.table[0, 1]], 68 - 64, False, x, c.fp4, to_bits(c.torch_dtype))    # value of token 2 of 4
+    op.write_row(c.pool[c.table[1, 2]], 129 - 128, True, x, c.fp4, to_bits(c.torch_dtype))   # key
+    o, l = _attend(c, q, 0.1, n, G)
+    for s in range(2):
+        assert np.abs(_f64(o)[s, :2] - want[s, :2]).max() <= TOL * 6
+        assert np.isnan(_f64(o)[s, 2:]).all()
+
+
+@pytest.mark.parametrize("fmt", ["fp4", "16bit"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_peaked_flat_and_negative_logits(fmt, dtype):
+    """One row that takes nearly all weight, all rows alike (scale 0: the mean of the values, lse = log n), a negative scale, large logits."""
+    c = Cache(1, 2, 128, dtype, fmt, [500, 130], rows=1.0, seed=17)
+    q = _queries(c, 1, 4, 10)
+    for scale in (0.0, -0.1, 0.3):
+        o, l = _attend(c, q, scale, 1, 4)
+        _check(c, q, o, l, scale, str(scale), 1)
+    _, l = _attend(c, q, 0.0, 1, 4)
+    assert np.allclose(_f64(l)[0, 0], np.log([500, 500, 130, 130]), atol=1e-6)
+    big = (q * 30).to(q.dtype)                             # logits of some hundreds: 2^-24 of them, times the roundings of a sum, in the exponent
+    o, l = _attend(c, big, 0.088, 1, 4)
+    want, want_lse = op.attention(_f64(big), c.pool, c.table, c.lens, 2, 0.088, 128, c.fp4, from_bits(c.torch_dtype))
+    assert np.abs(_f64(o) - want).max() <= 6 * 2e-3 and np.abs(_f64(l) / want_lse - 1).max() <= TOL
+
+
+@pytest.mark.parametrize("fmt", ["fp4", "16bit"])
+def test_queries_of_very_different_sizes(fmt):
+    """Small query values beside large ones keep their share: dims whose keys are zero hold the large ones."""
+    c = Cache(1, 1, 128, "bf16", fmt, [64], rows=1.0, seed=18)
+    page = c.pool[c.table[0, 0]]
+    K, V = op.read_rows(page, 128, c.fp4, from_bits(c.torch_dtype))
+    for r in range(64):
+        K[r, :32] = 0.0
+        op.write_row(page, r, True, K[r], c.fp4, to_bits(c.torch_dtype))
+    q = _queries(c, 1, 1, 11)
+    q[..., :32] *= 500
+    o, l = _attend(c, q, 0.2, 1, 1)
+    _check(c, q, o, l, 0.2, fmt, 1)
+
+
+def test_units_may_share_pages():
+    c = Cache(4, 1, 64, "bf16", "fp4", [130, 100, 64, 130], rows=1.0, seed=19)
+    c.table[1:] = c.table[0]
+    q = _queries(c, 1, 2, 12)
+    o, l = _attend(c, q, 0.125, 1, 2)
+    _check(c, q, o, l, 0.125, "shared", 1)
+
+
+@pytest.mark.parametrize("fmt", ["fp4", "16bit"])
+def test_calls_repeat_bit_for_bit_on_any_stream_and_without_lse(fmt):
+    c = Cache(5, 2, 128, "bf16", fmt, [900, 64, 1, 0, 300, 2000, 77, 128, 129, 5], rows=1.0, seed=20)
+    q = _queries(c, 2, 8, 13)
+    o, l = _attend(c, q, 0.09, 2, 8)
+    other = torch.cuda.Stream()
+    o2, l2 = _attend(c, q, 0.09, 2, 8, stream=other)
+    o3, _ = _attend(c, q, 0.09, 2, 8, want_lse=False)
+    assert torch.equal(o, o2) and torch.equal(o, o3) and torch.equal(l, l2)
+
+
+def test_offsets_beyond_32_bits():
+    """A pool of more than 4 GiB: pages at its far end."""
+    d, far = 256, (1 << 32) // op.page_bytes(256, False) + 100
+    c = Cache(1, 1, d, "bf16", "16bit", [150], rows=1.0, seed=21)
+    pool = torch.full((far + 3, op.page_bytes(d, False)), 255, dtype=torch.uint8, device=DEV)
+    pool[far:far + 3] = torch.from_numpy(c.pool[c.table[0]]).to(DEV)
+    table = torch.arange(far, far + 3, dtype=torch.int32, device=DEV)[None]
+    lens = torch.tensor([150], dtype=torch.int32, device=DEV)
+    pages = nkv.Pages(1, 1, d, nkv.DTYPE_BF16, nkv.PAGES_16BIT, pool, table, lens)
+    q = _queries(c, 1, 2, 14)
+    out, ws = torch.empty(1, 1, 2, d, device=DEV), torch.empty(nkv.pages_workspace_bytes(pages, 2), dtype=torch.uint8, device=DEV)
+    nkv.pages_attention(q.to(DEV), pages, 2, 1, 0.06, out, None, ws)
+    _check(c, q, out, None, 0.06, "far", 1)
+    k, v = torch.empty(150, d, dtype=torch.bfloat16, device=DEV), torch.empty(150, d, dtype=torch.bfloat16, device=DEV)
+    off = torch.tensor([0, 150], device=DEV)
+    nkv.pages_read(k, v, off, 150, pages)
+    nkv.pages_load(v, k, off, 150, pages)                   # swapped
+    k2, v2 = torch.empty_like(k), torch.empty_like(v)
+    nkv.pages_read(k2, v2, off, 150, pages)
+    assert torch.equal(k, v2) and torch.equal(v, k2)
+
+
+# ---- together ----
+
+@pytest.mark.parametrize("fmt", ["fp4", "16bit"])
+def test_captured_decode_steps_replay(fmt):
+    """Three decode steps (lens + 1, append, attention) recorded once: every replay goes on from where the last one stopped, and eager steps from the
+    same start give the same bits."""
+    S, H, G, d, steps = 3, 2, 4, 128, 4
+    c = Cache(S, H, d, "bf16", fmt, [60, 61, 62, 63, 64, 10], width=4, rows=1.0, seed=22)
+    spare = np.full((S * H, c.pool.shape[1]), 255, np.uint8)   # a page more for every unit
+    for u in range(S * H):
+        c.table[u, (int(c.lens[u]) + 63) // 64] = c.pool.shape[0] + u
+    c.pool = np.concatenate([c.pool, spare])
+    rope = nkv.rope_table(200, d, device=DEV)
+    x = torch.randn(S, 1, (G + 2) * H, d, generator=torch.Generator().manual_seed(3)).to(torch.bfloat16).to(DEV)
+
+    def state():
+        pages = c.on(DEV)
+        s = dict(pages=pages, lens=c.d_lens, pool=c.d_pool, pos=torch.tensor([[100], [90], [80]], dtype=torch.int32, device=DEV))
+        s["q"] = torch.empty(S, 1, G * H, d, dtype=torch.bfloat16, device=DEV)
+        s["out"], s["lse"] = torch.empty(S, 1, G * H, d, device=DEV), torch.empty(S, 1, G * H, device=DEV)
+        s["ws"] = torch.empty(nkv.pages_workspace_bytes(pages, G * H), dtype=torch.uint8, device=DEV)
+        return s
+
+    def step(s):
+        s["lens"] += 1
+        nkv.pages_append(x[:, :, G * H:(G + 1) * H], x[:, :, (G + 1) * H:], s["pages"], positions=s["pos"], rope=rope, q=x[:, :, :G * H], q_out=s["q"])
+        nkv.pages_attention(s["q"], s["pages"], G * H, 1, d ** -0.5, s["out"], s["lse"], s["ws"])
+        s["pos"] += 1
+
+    eager, caught = state(), state()
+    wanted = []
+    for _ in range(steps):
+        step(eager)
+        wanted.append((eager["out"].clone(), eager["lse"].clone()))
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step(caught)
+    for out, lse in wanted:
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(caught["out"], out) and torch.equal(caught["lse"], lse)
+        float(x.float().sum())                              # the program's own work in between
+    assert torch.equal(caught["pool"], eager["pool"]) and torch.equal(caught["lens"], eager["lens"])
+    c.pool, c.lens = eager["pool"].cpu().numpy(), eager["lens"].cpu().numpy()
+    _check(c, eager["q"], eager["out"], eager["lse"], d ** -0.5, "after the last step", 1)
+
+
+@pytest.mark.parametrize("fmt", ["fp4", "16bit"])
+def test_the_compressors_rows_through_pages(fmt):
+    """compress -> load -> attend; 16-bit pages agree with attention over the packed rows themselves."""
+    w = nkv_inputs.small_workload("pages", 2, 2, 128, [700, 333])
+    K, V = nkv_inputs.make_kv(w, "cpu")
+    shape = shape_of(w)
+    comp = nkv.Compressor(shape, [0.6, 0.5])
+    r = comp.run(K.to(DEV), V.to(DEV))
+    lens = (r.head_off[1:] - r.head_off[:-1]).int()
+    c = Cache(4, 2, 128, "bf16", fmt, lens.cpu().numpy(), seed=23)
+    pages = c.on(DEV)
+    nkv.pages_load(r.packed_k, r.packed_v, r.head_off, comp.rows, pages)
+    q = nkv_inputs.make_queries(w, 8, K).to(DEV)             # [P, L, Hq, d]: sequence p * L + l
+    out = torch.empty(4, 1, 8, 128, device=DEV)
+    lse = torch.empty(4, 1, 8, device=DEV)
+    ws = torch.empty(nkv.pages_workspace_bytes(pages, 8), dtype=torch.uint8, device=DEV)
+    nkv.pages_attention(q.reshape(4, 1, 8, 128), pages, 8, 1, 128 ** -0.5, out, lse, ws)
+    torch.cuda.synchronize()
+    c.pool = c.d_pool.cpu().numpy()
+    _check(c, q.reshape(4, 1, 8, 128), out, lse, 128 ** -0.5, fmt, 1)
+    if fmt == "16bit":
+        want, want_lse = torch.empty(2, 2, 8, 128, device=DEV), torch.empty(2, 2, 8, device=DEV)
+        ws2 = torch.empty(max(256, nkv.decode_workspace_bytes(shape, 8, comp.rows)), dtype=torch.uint8, device=DEV)
+        nkv.decode_attention(q, r.packed_k, r.packed_v, r.head_off, comp.rows, shape, comp.params, 8, 128 ** -0.5, want, want_lse, ws2)
+        torch.cuda.synchronize()
+        assert float((out.reshape(want.shape) - want).abs().max()) <= 2 * TOL * 6
+        assert float((lse.reshape(want_lse.shape) - want_lse).abs().max()) <= 2 * TOL * 10
