@@ -23,30 +23,37 @@ using f32x4 = float __attribute__((ext_vector_type(4)));
 using bf16x8 = __bf16 __attribute__((ext_vector_type(8)));
 using f16x8 = _Float16 __attribute__((ext_vector_type(8)));
 
-constexpr int kThreads = 256, kWaves = kThreads / 64, kCols = 16;
-constexpr int kMostGroups = 512;         // workgroups: two for every compute unit
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kMostGroups = 768;         // workgroups: three for every compute unit
 constexpr float kNone = -1.0e30f;        // running maximum before any row was seen
 constexpr float kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ int clamp_len(int len, int max_pages) { return max(0, min(len, max_pages * kRows)); }
+
+struct Parts;
 
 struct AttendArgs {
     const uint16_t *q;
     const uint8_t *pool;
     const int32_t *table, *lens;
     int32_t n_units, H, G, n_new, n_pages, max_pages;
-    float scale_log2;
-    int2 *plan;                          // per unit: its first part and the one behind its last
+    float scale_log2;                    // positive
+    uint32_t flip;                       // sign bits of the query that change
+    Parts *plan;                         // per unit
     float *part;                         // [part][column][D + 4]: weighted values, maximum, sum
 };
 
-template <int D, bool F16, bool FP4> struct Geo {
+// FEW: up to five columns, whose weights' pieces lie side by side in the 16 columns of a product.
+template <int D, bool F16, bool FP4, bool FEW = false> struct Geo {
+    static constexpr int kCols = FEW ? 5 : 16;
     static constexpr int NB = D / kBlock, C = chunk_of(D), VL = D / C;        // VL lanes of 16 hold dims of V
-    static constexpr int kTiles = FP4 ? 4 : 2, kStep = 16 * kTiles;           // rows of a step
+    static constexpr int kTiles = 2, kStep = 16 * kTiles;           // rows of a step
     static constexpr int J = D / 32;                                          // products over the dims of a row
     // 4 bits: lane g holds dims D / 4 * g on, J words of a row; one scale byte or two if that is no more than a block or two
     static constexpr int kScales = D == 64 || D == 128 ? 1 : D == 256 ? 2 : J;
     static constexpr int kVWords = FP4 ? C / 2 : 2 * C;
+    // two halves' rows at once, where the registers are there for it
+    static constexpr bool kAhead = FP4 || D == 64;
     // fp16 weights are of up to 2^14, so that their second piece does not run out of exponents
     static constexpr bool kHalfP = F16 && !FP4;
     static constexpr float kShift = kHalfP ? 14.f : 0.f;
@@ -59,7 +66,7 @@ template <int D, bool F16, bool FP4> struct Rows {
     uint32_t k[Q::kTiles][FP4 ? Q::J : 4 * Q::J];   // row n of a tile; 4 bits: dims D / 4 * g + 8 j .., 16 bits: 32 j + 8 g ..
     uint32_t ks[Q::kScales];             // 4 bits: scale bytes of rows n, 16 + n, 32 + n, 48 + n of the lane's blocks
     uint32_t v[Q::kTiles][Q::kVWords];   // rows 4 g .. 4 g + 3 of a tile, dims C n .. C n + C - 1
-    u32x4 vs;                            // 4 bits: scale bytes of those rows, a word a tile
+    uint32_t vs[Q::kTiles];              // 4 bits: scale bytes of those rows, a word a tile
 };
 
 // N words from an address that is a multiple of the largest load that divides them.
@@ -93,13 +100,17 @@ __device__ __forceinline__ void load_rows(Rows<D, F16, FP4> &f, const uint8_t *_
     if constexpr (FP4) {
         using P = Fp4Page<D>;
 #pragma unroll
-        for (int t = 0; t < 4; ++t) load_words<Q::J>(f.k[t], page + P::k_code(16 * t + n, D / 4 * g));
+        for (int t = 0; t < Q::kTiles; ++t) load_words<Q::J>(f.k[t], page + P::k_code(half * Q::kStep + 16 * t + n, D / 4 * g));
 #pragma unroll
         for (int i = 0; i < Q::kScales; ++i)
             f.ks[i] = *reinterpret_cast<const uint32_t *>(page + P::k_scale(n, (D / 4 * g + (Q::kScales == Q::J ? 8 : 32) * i) / kBlock));
 #pragma unroll
-        for (int t = 0; t < 4; ++t) load_words<Q::kVWords>(f.v[t], page + P::v_code(16 * t + 4 * g, Q::C * vn));
-        f.vs = *reinterpret_cast<const u32x4 *>(page + P::v_scale(4 * g, Q::C * vn / kBlock));
+        for (int t = 0; t < Q::kTiles; ++t) load_words<Q::kVWords>(f.v[t], page + P::v_code(half * Q::kStep + 16 * t + 4 * g, Q::C * vn));
+        load_words<Q::kTiles>(f.vs, page + P::v_scale(half * Q::kStep + 4 * g, Q::C * vn / kBlock));
+        if (half) {
+#pragma unroll
+            for (int i = 0; i < Q::kScales; ++i) f.ks[i] >>= 16;
+        }
     } else {
         using P = WidePage<D>;
 #pragma unroll
@@ -113,19 +124,22 @@ __device__ __forceinline__ void load_rows(Rows<D, F16, FP4> &f, const uint8_t *_
     }
 }
 
-// A column's query as the products take it: word j of a lane holds the dims that k's does.
+// A column's query as the products take it: word j of a lane holds the dims that k's does.  A negative scale's sign goes to the query (flip:
+// 0x80008000), so that the largest logit is that of the largest product.
 template <int D, bool F16, bool FP4> struct Query {
     u32x4 w[F16 && FP4 ? 2 : 1][D / 32];
 };
 
 template <int D, bool F16, bool FP4>
-__device__ __forceinline__ void load_query(Query<D, F16, FP4> &f, const uint16_t *__restrict__ row, bool there, int g)
+__device__ __forceinline__ void load_query(Query<D, F16, FP4> &f, const uint16_t *__restrict__ row, bool there, uint32_t flip, int g)
 {
     using Q = Geo<D, F16, FP4>;
 #pragma unroll
     for (int j = 0; j < Q::J; ++j) {
         const int dim = FP4 ? D / 4 * g + 8 * j : 32 * j + 8 * g;
-        const u32x4 x = there ? *reinterpret_cast<const u32x4 *>(row + dim) : u32x4{0u, 0u, 0u, 0u};
+        u32x4 x = there ? *reinterpret_cast<const u32x4 *>(row + dim) : u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] ^= flip;
         if constexpr (F16 && FP4) {                                       // 11 bits: eight, and the three that are left
             float v[8], rest[8];
             unpack8<true>(x, v);
@@ -190,8 +204,8 @@ __device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return
 
 // Running state of 16 columns: lane (n, g) holds column n's maximum, its own rows' share of the sum, and the weighted values of dims
 // (4 g + i) C + t in o[t][i].
-template <int D, bool F16, bool FP4> struct State {
-    using Q = Geo<D, F16, FP4>;
+template <int D, bool F16, bool FP4, bool FEW> struct State {
+    using Q = Geo<D, F16, FP4, FEW>;
     float m, l;
     f32x4 o[Q::C];
     __device__ __forceinline__ void clear()
@@ -202,27 +216,57 @@ template <int D, bool F16, bool FP4> struct State {
     }
 };
 
-// A step's rows into the state.  MASKED: only the rows before `lim` of columns that take part (`on`); the others' state stays as it is, also
-// where a row that they do not see holds NaN.
-template <int D, bool F16, bool FP4, bool MASKED>
-__device__ __forceinline__ void accumulate(State<D, F16, FP4> &st, const Rows<D, F16, FP4> &f, const f32x4 (&products)[Geo<D, F16, FP4>::kTiles],
-                                           float scale_log2, int g, int lim, bool on)
+// The end of a unit's rows.  rel: rows from the half's first one on, lim: those that the lane's column sees, least: those that all columns see.
+// Rows that a column does not see get the product -inf, so weight 0; V of rows that are not there becomes 0 or 1, since 0 times NaN is NaN.  So it does
+// where a row that only later tokens see holds a NaN or infinity, whose columns get a NaN for a product instead.
+template <int D, bool F16, bool FP4>
+__device__ __forceinline__ void mask_rows(Rows<D, F16, FP4> &f, f32x4 (&s)[Geo<D, F16, FP4>::kTiles], int g, int rel, int lim, int least)
 {
     using Q = Geo<D, F16, FP4>;
-    float p[4 * Q::kTiles], top = kNone;
 #pragma unroll
     for (int t = 0; t < Q::kTiles; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            float x = products[t][i] * scale_log2;
-            if (MASKED) x = on && 16 * t + 4 * g + i < lim ? x : -INFINITY;
-            p[4 * t + i] = x;
-            top = fmaxf(top, x);
+            const int row = 16 * t + 4 * g + i;
+            bool clear = row >= rel, poison = false;
+            if (least < rel) {                                             // several tokens
+                bool odd = false;
+                if constexpr (FP4) odd = (f.vs[t] >> (8 * i) & 255u) == 255u;
+                else
+#pragma unroll
+                    for (int k = 0; k < Q::C / 2; ++k) {
+                        const uint32_t x = f.v[t][i * (Q::C / 2) + k], e = F16 ? 0x7c00u : 0x7f80u;
+                        odd |= (x & e) == e || (x >> 16 & e) == e;
+                    }
+                const unsigned long long lanes = __ballot(odd);            // all dims of the row: the 16 lanes of this g
+                poison = (lanes >> (16 * g) & 0xffffull) != 0ull && row >= least && row < rel;
+                clear |= poison;
+            }
+            if constexpr (FP4) f.vs[t] = clear ? (f.vs[t] & ~(255u << (8 * i))) | 127u << (8 * i) : f.vs[t];
+            else
+#pragma unroll
+                for (int k = 0; k < Q::C / 2; ++k) f.v[t][i * (Q::C / 2) + k] = clear ? 0u : f.v[t][i * (Q::C / 2) + k];
+            s[t][i] = row >= lim ? -INFINITY : poison ? __uint_as_float(0x7fc00000u) : s[t][i];
         }
-    auto larger = [](float a, float b) { return fmaxf(a, b); };
-    top = swap_reduce<16>(top, larger);
-    top = swap_reduce<32>(top, larger);
+}
+
+template <int D, bool F16, bool FP4, bool FEW>
+__device__ __forceinline__ void accumulate(State<D, F16, FP4, FEW> &st, const Rows<D, F16, FP4> &f, const f32x4 (&products)[Geo<D, F16, FP4>::kTiles],
+                                           float scale_log2, int piece)
+{
+    using Q = Geo<D, F16, FP4, FEW>;
+    constexpr int kSets = FEW ? 1 : Q::kPieces;                            // products with V a pair of dims
+    const uint32_t cut1 = piece >= 1 ? 0xffff0000u : 0u, cut2 = piece >= 2 ? 0xffff0000u : 0u;
+    float p[4 * Q::kTiles], top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 4 * Q::kTiles; ++i) {
+        p[i] = products[i / 4][i % 4];
+        top = fmaxf(top, p[i]);
+    }
+    top *= scale_log2;                                                     // (positive, see load_query)
     if (__any(top > st.m)) {                                               // seldom after a unit's first steps
+        auto larger = [](float a, float b) { return fmaxf(a, b); };
+        top = swap_reduce<32>(swap_reduce<16>(top, larger), larger);
         const float m = fmaxf(top, st.m), f0 = __builtin_amdgcn_exp2f(st.m - m);
         st.m = m;
         st.l *= f0;
@@ -235,21 +279,28 @@ __device__ __forceinline__ void accumulate(State<D, F16, FP4> &st, const Rows<D,
     float l = 0.f;
 #pragma unroll
     for (int i = 0; i < 4 * Q::kTiles; ++i) {
-        p[i] = __builtin_amdgcn_exp2f(p[i] + base);
+        p[i] = __builtin_amdgcn_exp2f(fmaf(p[i], scale_log2, base));
         l += p[i];
     }
     st.l += l;
 #pragma unroll
     for (int h = 0; h < Q::kTiles / 2; ++h) {
         // the 32 rows of tiles 2 h and 2 h + 1: words of two rows' weights, a piece at a time
-        u32x4 w[Q::kPieces];
+        u32x4 w[kSets];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             float a = p[8 * h + 2 * j], b = p[8 * h + 2 * j + 1];
             if constexpr (Q::kHalfP) {
                 const f16x2 hi = {(_Float16)a, (_Float16)b};
-                w[0][j] = __builtin_bit_cast(uint32_t, hi);
-                w[1][j] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)(a - (float)hi.x), (_Float16)(b - (float)hi.y)});
+                const f16x2 lo = {(_Float16)(a - (float)hi.x), (_Float16)(b - (float)hi.y)};
+                if constexpr (FEW) w[0][j] = __builtin_bit_cast(uint32_t, piece == 0 ? hi : lo);
+                else w[0][j] = __builtin_bit_cast(uint32_t, hi), w[1][j] = __builtin_bit_cast(uint32_t, lo);
+            } else if constexpr (FEW) {                                    // a lane's own piece
+                a -= __uint_as_float(__float_as_uint(a) & cut1);
+                b -= __uint_as_float(__float_as_uint(b) & cut1);
+                a -= __uint_as_float(__float_as_uint(a) & cut2);
+                b -= __uint_as_float(__float_as_uint(b) & cut2);
+                w[0][j] = high_halves(__float_as_uint(a), __float_as_uint(b));
             } else {
 #pragma unroll
                 for (int k = 0; k < 3; ++k) {                              // cut off, not rounded: three times eight bits are all 24
@@ -264,7 +315,6 @@ __device__ __forceinline__ void accumulate(State<D, F16, FP4> &st, const Rows<D,
 #pragma unroll
             for (int r = 0; r < 8; ++r) {
                 scale[r] = scale_value(f.vs[2 * h + r / 4] >> (8 * (r % 4)) & 255u);
-                if (MASKED) scale[r] = 32 * h + 16 * (r / 4) + 4 * g + r % 4 < lim ? scale[r] : 1.f;
             }
         }
 #pragma unroll
@@ -278,23 +328,15 @@ __device__ __forceinline__ void accumulate(State<D, F16, FP4> &st, const Rows<D,
                     x[r] = two_codes(f.v[t][at / 4], scale[r], at % 4);
                 } else {
                     x[r] = f.v[t][i * (Q::C / 2) + k];
-                    if (MASKED) x[r] = 16 * t + 4 * g + i < lim ? x[r] : 0u;
                 }
             }
             const u32x4 lo = {low_halves(x[0], x[1]), low_halves(x[2], x[3]), low_halves(x[4], x[5]), low_halves(x[6], x[7])};
             const u32x4 hi = {high_halves(x[0], x[1]), high_halves(x[2], x[3]), high_halves(x[4], x[5]), high_halves(x[6], x[7])};
             f32x4 a = st.o[2 * k], b = st.o[2 * k + 1];
 #pragma unroll
-            for (int c = Q::kPieces - 1; c >= 0; --c) {
+            for (int c = kSets - 1; c >= 0; --c) {
                 a = product<Q::kHalfP>(lo, w[c], a);
                 b = product<Q::kHalfP>(hi, w[c], b);
-            }
-            if (MASKED) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    a[i] = on ? a[i] : st.o[2 * k][i];
-                    b[i] = on ? b[i] : st.o[2 * k + 1][i];
-                }
             }
             st.o[2 * k] = a;
             st.o[2 * k + 1] = b;
@@ -302,166 +344,302 @@ __device__ __forceinline__ void accumulate(State<D, F16, FP4> &st, const Rows<D,
     }
 }
 
-// grid: (stretches / kWaves, groups of 16 columns)
-template <int D, bool F16, bool FP4> __global__ __launch_bounds__(kThreads, 2) void pages_attend_kernel(const AttendArgs a)
+// Which parts the workspace holds of a unit: one for every stretch x .. y - 1 that it lies in, but one (numbered as its first) for every
+// workgroup's kWaves stretches from group a to b - 1, which lie in the unit altogether.
+struct Parts {
+    int x, y, a, b;
+    __device__ int count() const { return a < b ? (kWaves * a - x) + (b - a) + (y - kWaves * b > 0 ? y - kWaves * b : 0) : y - x; }
+    __device__ int number(int i) const                                    // the stretch of the i-th part
+    {
+        if (a >= b) return x + i;
+        const int front = kWaves * a - x;
+        return i < front ? x + i : i < front + (b - a) ? kWaves * (a + i - front) : kWaves * b + (i - front - (b - a));
+    }
+};
+// of a unit whose c > 0 steps are the at-th on; total: of all units
+__device__ __forceinline__ Parts parts_of(uint32_t at, uint32_t c, uint32_t run, uint32_t total)
 {
-    using Q = Geo<D, F16, FP4>;
-    constexpr int kBytes = FP4 ? Fp4Page<D>::kBytes : WidePage<D>::kBytes;
-    __shared__ uint32_t wsum[kWaves];
-    __shared__ int start_unit[kWaves];
-    __shared__ uint32_t start_at[kWaves];
-    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
-    auto steps_of = [&](int u) { return (uint32_t)(clamp_len(a.lens[u], a.max_pages) + Q::kStep - 1) / Q::kStep; };
-    // ---- where this wavefront's stretch begins ----
-    const int per = (a.n_units + kThreads - 1) / kThreads, u0 = min(tid * per, a.n_units), u1 = min(u0 + per, a.n_units);
+    Parts p;
+    p.x = (int)(at / run);
+    p.y = (int)((at + c - 1) / run) + 1;
+    p.a = (int)((at + kWaves * run - 1) / (kWaves * run));
+    p.b = at + c == total ? (p.y + kWaves - 1) / kWaves : (int)((at + c) / (run * kWaves));
+    return p;
+}
+
+// Where a wavefront's stretch begins.  Stretches are of `run` pages; the pages of all units are counted in their order.
+struct Place {
+    uint32_t total, run;
+    int unit, unit0;                     // the unit that holds the stretch's first page, and that of the workgroup's first stretch
+    uint32_t first;                      // the first page of `unit`
+    bool joined;                         // all of the workgroup's pages lie in unit0: its wavefronts' parts become one
+};
+constexpr int kUnitsLane = 8;
+
+__device__ __forceinline__ uint32_t pages_of(const AttendArgs &a, int u) { return (uint32_t)(clamp_len(a.lens[u], a.max_pages) + kRows - 1) / kRows; }
+__device__ __forceinline__ bool plans() { return blockIdx.x == 0 && blockIdx.y == 0; }
+
+// Up to 512 units: every wavefront counts them by itself, all lengths asked for at once and no barrier.
+__device__ __forceinline__ Place placed_by_wave(const AttendArgs &a, int w)
+{
+    const int lane = threadIdx.x & (kWave - 1);
+    uint32_t c[kUnitsLane], at[kUnitsLane];
+#pragma unroll
+    for (int k = 0; k < kUnitsLane; ++k) c[k] = k * kWave + lane < a.n_units ? pages_of(a, k * kWave + lane) : 0u;
+    Place p;
+    p.total = 0u;
+#pragma unroll
+    for (int k = 0; k < kUnitsLane; ++k) {
+        if (k * kWave >= a.n_units) break;
+        const uint32_t incl = wave_prefix_sum(c[k]);
+        at[k] = p.total + incl - c[k];
+        p.total += (uint32_t)__builtin_amdgcn_readlane((int)incl, kWave - 1);
+    }
+    const uint32_t stretches = gridDim.x * kWaves;
+    p.run = max(1u, (p.total + stretches - 1) / stretches);
+    const uint32_t lo0 = blockIdx.x * kWaves * p.run, lo = lo0 + w * p.run, hi = min(lo0 + kWaves * p.run, p.total);
+    p.unit = p.unit0 = 0, p.first = 0u, p.joined = false;
+#pragma unroll
+    for (int k = 0; k < kUnitsLane; ++k) {
+        if (k * kWave >= a.n_units) break;
+        const unsigned long long mine = __ballot(at[k] <= lo && lo < at[k] + c[k]), groups = __ballot(at[k] <= lo0 && lo0 < at[k] + c[k]);
+        if (mine) {
+            const int l = __builtin_ctzll(mine);
+            p.unit = k * kWave + l;
+            p.first = (uint32_t)__builtin_amdgcn_readlane((int)at[k], l);
+        }
+        if (groups) {
+            const int l = __builtin_ctzll(groups);
+            p.unit0 = k * kWave + l;
+            p.joined = (uint32_t)__builtin_amdgcn_readlane((int)(at[k] + c[k]), l) >= hi;
+        }
+        if (plans() && w == 0 && k * kWave + lane < a.n_units) a.plan[k * kWave + lane] = c[k] ? parts_of(at[k], c[k], p.run, p.total) : Parts{0, 0, 0, 0};
+    }
+    return p;
+}
+
+// More units: the workgroup's threads count a share of them each.
+__device__ __forceinline__ Place placed_by_workgroup(const AttendArgs &a, int w)
+{
+    __shared__ uint32_t wsum[kWaves], first[kWaves];
+    __shared__ int unit[kWaves], joined;
+    const int tid = threadIdx.x, per = (a.n_units + kThreads - 1) / kThreads, u0 = min(tid * per, a.n_units), u1 = min(u0 + per, a.n_units);
     uint32_t mine = 0u;
-    for (int u = u0; u < u1; ++u) mine += steps_of(u);
-    uint32_t before = wave_prefix_sum(mine) - mine;
-    if (lane == 63) wsum[w] = before + mine;
+    for (int u = u0; u < u1; ++u) mine += pages_of(a, u);
+    uint32_t at = wave_prefix_sum(mine) - mine;
+    if ((tid & (kWave - 1)) == kWave - 1) wsum[w] = at + mine;
+    if (tid < kWaves) unit[tid] = 0, first[tid] = 0u;
     __syncthreads();
-    uint32_t total = 0u;
+    Place p;
+    p.total = 0u;
 #pragma unroll
     for (int i = 0; i < kWaves; ++i) {
-        before += i < w ? wsum[i] : 0u;
-        total += wsum[i];
+        at += i < w ? wsum[i] : 0u;
+        p.total += wsum[i];
     }
-    const uint32_t stretches = gridDim.x * kWaves, run = max(1u, (total + stretches - 1) / stretches);
-    const bool plans = blockIdx.x == 0 && blockIdx.y == 0;
-    if (plans || (before < (blockIdx.x + 1) * kWaves * run && before + mine > blockIdx.x * kWaves * run)) {
-        uint32_t at = before;
+    const uint32_t stretches = gridDim.x * kWaves;
+    p.run = max(1u, (p.total + stretches - 1) / stretches);
+    const uint32_t lo0 = blockIdx.x * kWaves * p.run, hi = min(lo0 + kWaves * p.run, p.total);
+    if (plans() || (at < hi && at + mine > lo0)) {
         for (int u = u0; u < u1; ++u) {
-            const uint32_t c = steps_of(u);
-            if (plans) a.plan[u] = c ? make_int2((int)(at / run) + u, (int)((at + c - 1) / run) + u + 1) : make_int2(0, 0);
+            const uint32_t c = pages_of(a, u);
+            if (plans()) a.plan[u] = c ? parts_of(at, c, p.run, p.total) : Parts{0, 0, 0, 0};
 #pragma unroll
-            for (int i = 0; i < kWaves; ++i) {
-                const uint32_t lo = (blockIdx.x * kWaves + i) * run;
-                if (at <= lo && lo < at + c) {
-                    start_unit[i] = u;
-                    start_at[i] = at;
+            for (int i = 0; i < kWaves; ++i)
+                if (at <= lo0 + i * p.run && lo0 + i * p.run < at + c) {
+                    unit[i] = u;
+                    first[i] = at;
+                    if (i == 0) joined = at + c >= hi;
                 }
-            }
             at += c;
         }
     }
     __syncthreads();
-    const uint32_t stretch = blockIdx.x * kWaves + w, lo = stretch * run, hi = min(lo + run, total);
-    if (lo >= hi) return;
-    int u = __builtin_amdgcn_readfirstlane(start_unit[w]);
-    uint32_t step = lo - __builtin_amdgcn_readfirstlane(start_at[w]);     // of the unit
-    // ---- columns ----
-    const int cols = a.n_new * a.G, col0 = blockIdx.y * kCols, col = col0 + n;
-    const bool there = col < cols;
-    const int token = (there ? col : cols - 1) / a.G, head = (there ? col : cols - 1) - token * a.G;
-    const int token0 = col0 / a.G, token1 = min(col0 + kCols, cols) - 1 >= 0 ? (min(col0 + kCols, cols) - 1) / a.G : 0;
-
-    Query<D, F16, FP4> q;
-    State<D, F16, FP4> st;
-    auto begin = [&]() {
-        const int s = u / a.H, h = u - s * a.H;
-        load_query<D, F16, FP4>(q, a.q + (((int64_t)s * a.n_new + token) * a.H * a.G + h * a.G + head) * D, there, g);
-        st.clear();
-    };
-    auto finish = [&]() {
-        float l = st.l;
-        auto sum = [](float x, float y) { return x + y; };
-        l = swap_reduce<16>(l, sum);
-        l = swap_reduce<32>(l, sum);
-        if (!there) return;
-        float *dst = a.part + (((int64_t)stretch + u) * cols + col) * (D + 4);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (4 * g + i < Q::VL)
-#pragma unroll
-                for (int t = 0; t < Q::C; t += 4)
-                    *reinterpret_cast<f32x4 *>(dst + (4 * g + i) * Q::C + t) = f32x4{st.o[t][i], st.o[t + 1][i], st.o[t + 2][i], st.o[t + 3][i]};
-        if (g == 0) {
-            dst[D] = st.m - Q::kShift;
-            dst[D + 1] = l;
-        }
-    };
-    begin();
-    int len = clamp_len(a.lens[u], a.max_pages);
-    for (uint32_t i = lo; i < hi; ++i) {
-        const int id = a.table[(int64_t)u * a.max_pages + step * Q::kStep / kRows];
-        if (id >= 0 && id < a.n_pages) {
-            Rows<D, F16, FP4> f;
-            load_rows<D, F16, FP4>(f, a.pool + (int64_t)id * kBytes, (int)(step % (kRows / Q::kStep)), n, g);
-            f32x4 s[Q::kTiles];
-            key_products<D, F16, FP4>(f, q, s);
-            const int rel = len - (int)(step * Q::kStep);                  // rows of the step, and behind it
-            if (rel - (a.n_new - 1) >= Q::kStep) accumulate<D, F16, FP4, false>(st, f, s, a.scale_log2, g, 0, true);
-            else
-                for (int t = token0; t <= token1; ++t)
-                    accumulate<D, F16, FP4, true>(st, f, s, a.scale_log2, g, rel - (a.n_new - 1 - t), token == t);
-        }
-        ++step;
-        if (i + 1 == hi || (int)(step * Q::kStep) >= len) {
-            finish();
-            if (i + 1 < hi) {
-                do len = clamp_len(a.lens[++u], a.max_pages);
-                while (len == 0 && u + 1 < a.n_units);
-                step = 0;
-                begin();
-            }
-        }
-    }
+    p.unit = __builtin_amdgcn_readfirstlane(unit[w]), p.unit0 = __builtin_amdgcn_readfirstlane(unit[0]);
+    p.first = (uint32_t)__builtin_amdgcn_readfirstlane((int)first[w]);
+    p.joined = __builtin_amdgcn_readfirstlane(joined) != 0;
+    return p;
 }
 
-// grid: a workgroup for every unit and column; 256 / D slices of a unit's parts, added up in the slices' order
-template <int D> __global__ __launch_bounds__(256) void pages_combine_kernel(const float *__restrict__ part, const int2 *__restrict__ plan, int cols,
-                                                                             int H, int G, int n_new, float *__restrict__ out, float *__restrict__ lse)
+// grid: (stretches / kWaves, groups of columns)
+template <int D, bool F16, bool FP4, bool FEW> __global__ __launch_bounds__(kThreads, D <= 128 ? 3 : 2) void pages_attend_kernel(const AttendArgs a)
 {
-    constexpr int NS = 256 / D, U = 4;
-    __shared__ float red[4], lds_l[NS], lds_o[NS][D];
-    const int u = blockIdx.x / cols, col = blockIdx.x - u * cols, tid = threadIdx.x, e = tid % D, sl = tid / D;
-    const int2 of = plan[u];
-    const float *src = part + (int64_t)col * (D + 4);
-    const int64_t each = (int64_t)cols * (D + 4);
-    float mm = kNone, ll = 0.f, oo = 0.f;
-    for (int i = of.x + tid; i < of.y; i += 256) mm = fmaxf(mm, src[i * each + D]);
-    mm = wave_max(mm);
-    if ((tid & 63) == 0) red[tid >> 6] = mm;
+    using Q = Geo<D, F16, FP4, FEW>;
+    constexpr int kBytes = FP4 ? Fp4Page<D>::kBytes : WidePage<D>::kBytes;
+    __shared__ __align__(16) float lds_o[kWaves][16][D + 4];
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
+    const Place at = a.n_units <= kWave * kUnitsLane ? placed_by_wave(a, w) : placed_by_workgroup(a, w);
+    const uint32_t total = at.total, run = at.run;
+    const uint32_t group_lo = blockIdx.x * kWaves * run;
+    if (group_lo >= total) return;
+    // ---- columns ----
+    const int cols = a.n_new * a.G, col0 = blockIdx.y * Q::kCols, col = col0 + (FEW ? n % Q::kCols : n);
+    const bool there = col < cols;
+    const int token = (there ? col : cols - 1) / a.G, head = (there ? col : cols - 1) - token * a.G;
+    const int piece = FEW ? n / Q::kCols : 0;
+
+    const uint32_t stretch = blockIdx.x * kWaves + w, lo = group_lo + w * run, hi = min(lo + run, total);
+    int u = at.unit;
+    uint32_t step = lo - at.first;                                         // page of the unit
+    const bool joined = at.joined;
+    const int here = min(Q::kCols, cols - col0);
+    // columns [0, here) of what `waves` wavefronts left, from `first` on, by `threads` threads, to the workspace
+    auto write = [&](int first, int waves, int number, int unit, int thread, int threads) {
+        float *dst = a.part + (((int64_t)number + unit) * cols + col0) * (D + 4);
+        for (int idx = thread; idx < here * (D / 4); idx += threads) {
+            const int c = idx / (D / 4), e = (idx - c * (D / 4)) * 4;
+            float mm = kNone, ll = 0.f;
+            f32x4 oo = {0.f, 0.f, 0.f, 0.f};
+            for (int i = first; i < first + waves; ++i) mm = fmaxf(mm, lds_o[i][c][D]);
+            for (int i = first; i < first + waves; ++i) {
+                const float f = __builtin_amdgcn_exp2f(lds_o[i][c][D] - mm);
+                f32x4 x = *reinterpret_cast<const f32x4 *>(&lds_o[i][c][e]);
+                if constexpr (FEW)
+#pragma unroll
+                    for (int k = 1; k < Q::kPieces; ++k) {
+                        const f32x4 y = *reinterpret_cast<const f32x4 *>(&lds_o[i][c + k * Q::kCols][e]);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) x[r] += y[r];
+                    }
+                ll = fmaf(f, lds_o[i][c][D + 1], ll);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) oo[k] = fmaf(f, x[k], oo[k]);
+            }
+            *reinterpret_cast<f32x4 *>(dst + c * (D + 4) + e) = oo;
+            if (e == 0) {
+                dst[c * (D + 4) + D] = mm;
+                dst[c * (D + 4) + D + 1] = ll;
+            }
+        }
+    };
+    // ---- the stretch, unit by unit ----
+    uint32_t i = lo;
+    do {
+        Query<D, F16, FP4> q;
+        State<D, F16, FP4, FEW> st;
+        st.clear();
+        const int len = clamp_len(a.lens[u], a.max_pages), sq = u / a.H, h = u - sq * a.H;
+        const int32_t *table = a.table + (int64_t)u * a.max_pages;
+        const uint32_t left = (uint32_t)(len + kRows - 1) / kRows - step, end = i < hi ? step + min(hi - i, left) : step;
+        if (i < hi) load_query<D, F16, FP4>(q, a.q + (((int64_t)sq * a.n_new + token) * a.H * a.G + h * a.G + head) * D, there, a.flip, g);
+        i += end - step;
+        auto id_of = [&](uint32_t at) { return at < end ? table[at] : -1; };
+        auto page_of = [&](int id) { return a.pool + (int64_t)(id >= 0 && id < a.n_pages ? id : 0) * kBytes; };
+        auto take = [&](Rows<D, F16, FP4> &f, int row) {
+            const int rel = len - (int)(step * kRows) - row, least = rel - (a.n_new - 1);
+            if (rel <= 0) return;                                          // (its bytes are the page's, if no rows')
+            f32x4 s[Q::kTiles];
+            key_products<D, F16, FP4>(f, q, s);
+            if (least < Q::kStep) mask_rows<D, F16, FP4>(f, s, g, rel, least + token, least);
+            accumulate<D, F16, FP4, FEW>(st, f, s, a.scale_log2, piece);
+        };
+        Rows<D, F16, FP4> even, odd;
+        int id = id_of(step), next = id_of(step + 1);
+        const uint8_t *page = page_of(id);
+        if (Q::kAhead && step < end) load_rows<D, F16, FP4>(even, page, 0, n, g);
+        // the next half's rows are on their way while a half is worked on (behind the last page: some page's)
+        while (step < end) {
+            const int after = id_of(step + 2);
+            const bool counts = id >= 0 && id < a.n_pages;
+            if (!Q::kAhead) load_rows<D, F16, FP4>(even, page, 0, n, g);
+            else load_rows<D, F16, FP4>(odd, page, 1, n, g);
+            if (counts) take(even, 0);
+            if (!Q::kAhead) load_rows<D, F16, FP4>(odd, page, 1, n, g);
+            id = next, next = after, page = page_of(id);
+            if (Q::kAhead) load_rows<D, F16, FP4>(even, page, 0, n, g);
+            if (counts) take(odd, Q::kStep);
+            ++step;
+        }
+        auto sum = [](float x, float y) { return x + y; };
+        const float l = swap_reduce<32>(swap_reduce<16>(st.l, sum), sum);
+        float *mine_o = lds_o[w][n];
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (4 * g + r < Q::VL)
+#pragma unroll
+                for (int t = 0; t < Q::C; t += 4)
+                    *reinterpret_cast<f32x4 *>(mine_o + (4 * g + r) * Q::C + t) = f32x4{st.o[t][r], st.o[t + 1][r], st.o[t + 2][r], st.o[t + 3][r]};
+        if (g == 0) {
+            mine_o[D] = st.m - Q::kShift;
+            mine_o[D + 1] = l;
+        }
+        if (joined) break;
+        __builtin_amdgcn_wave_barrier();                                   // (a wavefront's LDS accesses are done in their order)
+        if (i > lo) write(w, 1, (int)stretch, u, lane, 64);
+        __builtin_amdgcn_wave_barrier();
+        step = 0;
+        do ++u;
+        while (i < hi && u < a.n_units - 1 && a.lens[u] <= 0);
+    } while (i < hi);
+    if (!joined) return;
     __syncthreads();
-    mm = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    write(0, kWaves, blockIdx.x * kWaves, at.unit0, tid, kThreads);
+}
+
+// grid: a workgroup for every unit and column.  D / 4 threads for a part, kThreads / (D / 4) parts at a time, each slice of parts with a running
+// maximum of its own; the slices are added up in their order.
+template <int D> __global__ __launch_bounds__(kThreads) void pages_combine_kernel(const float *__restrict__ part, const Parts *__restrict__ plan, int cols,
+                                                                                  int H, int G, int n_new, float *__restrict__ out, float *__restrict__ lse)
+{
+    constexpr int TH = D / 4, NS = kThreads / TH, U = 4;
+    __shared__ float lds_m[NS], lds_l[NS];
+    __shared__ __align__(16) float lds_o[NS][D];
+    const int u = blockIdx.x / cols, col = blockIdx.x - u * cols, tid = threadIdx.x, e = tid % TH * 4, sl = tid / TH;
+    const Parts of = plan[u];
+    const int count = of.count();
+    float m = kNone, l = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
     if (sl < NS) {
-        for (int i = of.x + sl; i < of.y; i += U * NS) {
-            float pm[U], pl[U], po[U];
+        for (int i = sl; i < count; i += U * NS) {                         // U parts' loads at once
+            f32x4 x[U];
+            float pm[U], pl[U];
 #pragma unroll
             for (int k = 0; k < U; ++k) {
-                const float *p = src + min(i + k * NS, of.y - 1) * each;
-                pm[k] = p[D], pl[k] = p[D + 1], po[k] = p[e];
+                const float *p = part + (((int64_t)of.number(min(i + k * NS, count - 1)) + u) * cols + col) * (D + 4);
+                x[k] = *reinterpret_cast<const f32x4 *>(p + e);
+                pm[k] = p[D], pl[k] = p[D + 1];
             }
 #pragma unroll
-            for (int k = 0; k < U; ++k)
-                if (i + k * NS < of.y) {
-                    const float f = __builtin_amdgcn_exp2f(pm[k] - mm);
-                    ll = fmaf(f, pl[k], ll);
-                    oo = fmaf(f, po[k], oo);
-                }
+            for (int k = 0; k < U; ++k) {
+                if (i + k * NS >= count) break;
+                const float mm = fmaxf(m, pm[k]), f = __builtin_amdgcn_exp2f(m - mm), h = __builtin_amdgcn_exp2f(pm[k] - mm);
+                m = mm;
+                l = fmaf(l, f, h * pl[k]);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[r] = fmaf(o[r], f, h * x[k][r]);
+            }
         }
-        lds_o[sl][e] = oo;
-        if (e == 0) lds_l[sl] = ll;
+        *reinterpret_cast<f32x4 *>(&lds_o[sl][e]) = o;
+        if (e == 0) lds_m[sl] = m, lds_l[sl] = l;
     }
     __syncthreads();
     if (sl > 0) return;
-    for (int i = 1; i < NS; ++i) {
-        oo += lds_o[i][e];
-        ll += lds_l[i];
+#pragma unroll
+    for (int i = 1; i < NS; ++i) m = fmaxf(m, lds_m[i]);
+    l = 0.f, o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+        const float f = __builtin_amdgcn_exp2f(lds_m[i] - m);
+        const f32x4 x = *reinterpret_cast<const f32x4 *>(&lds_o[i][e]);
+        l = fmaf(f, lds_l[i], l);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[k] = fmaf(f, x[k], o[k]);
     }
     const int s = u / H, h = u - s * H, t = col / G, g = col - t * G;
     const int64_t row = ((int64_t)s * n_new + t) * H * G + h * G + g;
-    const bool none = ll == 0.f;                                           // (NaN is handed on)
-    out[row * D + e] = none ? 0.f : oo / ll;
-    if (lse && e == 0) lse[row] = none ? -INFINITY : (mm + log2f(ll)) * kLn2;
+    const bool none = l == 0.f;                                           // (NaN is handed on)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) o[k] = none ? 0.f : o[k] / l;
+    *reinterpret_cast<f32x4 *>(out + row * D + e) = o;
+    if (lse && e == 0) lse[row] = none ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
-int step_rows(int format) { return format == NKV_PAGES_FP4 ? 64 : 32; }
 unsigned groups_of(const nkv_pages &p)
 {
-    const int64_t most = (int64_t)p.n_seqs * p.H * p.max_pages * (kRows / step_rows(p.format));
+    const int64_t most = (int64_t)p.n_seqs * p.H * p.max_pages;
     return (unsigned)std::min<int64_t>(kMostGroups, (most + kWaves - 1) / kWaves);
 }
-size_t plan_bytes(const nkv_pages &p) { return ((size_t)p.n_seqs * p.H * sizeof(int2) + 255) / 256 * 256; }
+size_t plan_bytes(const nkv_pages &p) { return ((size_t)p.n_seqs * p.H * sizeof(Parts) + 255) / 256 * 256; }
 
 }  // namespace
 
@@ -477,17 +655,27 @@ hipError_t launch_pages_attention(const void *q, const nkv_pages &p, int n_q_hea
     AttendArgs a{};
     a.q = (const uint16_t *)q, a.pool = (const uint8_t *)p.pool, a.table = p.table, a.lens = p.lens;
     a.n_units = p.n_seqs * p.H, a.H = p.H, a.G = n_q_heads / p.H, a.n_new = n_new, a.n_pages = p.n_pages, a.max_pages = p.max_pages;
-    a.scale_log2 = (float)(scale * 1.4426950408889634);
-    a.plan = (int2 *)ws;
+    a.scale_log2 = std::max((float)(fabs(scale) * 1.4426950408889634), 0x1p-100f);   // (not 0: rows that are not seen have the product -inf)
+    a.flip = scale < 0 ? 0x80008000u : 0u;
+    a.plan = (Parts *)ws;
     a.part = (float *)((char *)ws + plan_bytes(p));
     const int cols = a.G * n_new;
-    const dim3 grid(groups_of(p), (unsigned)((cols + kCols - 1) / kCols));
     for_head_dim(p.d, [&](auto dim) {
         constexpr int D = decltype(dim)::value;
-        const bool f16 = p.dtype == NKV_DTYPE_F16, fp4 = p.format == NKV_PAGES_FP4;
-        (f16 ? fp4 ? pages_attend_kernel<D, true, true> : pages_attend_kernel<D, true, false>
-             : fp4 ? pages_attend_kernel<D, false, true> : pages_attend_kernel<D, false, false>)<<<grid, kThreads, 0, st>>>(a);
-        pages_combine_kernel<D><<<(unsigned)(a.n_units * cols), 256, 0, st>>>(a.part, a.plan, cols, a.H, a.G, n_new, out, lse);
+        auto go = [&](auto f16, auto fp4) {
+            constexpr bool F16 = decltype(f16)::value, FP4 = decltype(fp4)::value;
+            const dim3 grid(groups_of(p), cols <= Geo<D, F16, FP4, true>::kCols ? 1u : (unsigned)((cols + 15) / 16));
+            if (grid.y == 1 && cols <= 5) pages_attend_kernel<D, F16, FP4, true><<<grid, kThreads, 0, st>>>(a);
+            else pages_attend_kernel<D, F16, FP4, false><<<grid, kThreads, 0, st>>>(a);
+        };
+        using Yes = std::true_type;
+        using No = std::false_type;
+        const bool half = p.dtype == NKV_DTYPE_F16, four = p.format == NKV_PAGES_FP4;
+        if (half && four) go(Yes{}, Yes{});
+        else if (half) go(Yes{}, No{});
+        else if (four) go(No{}, Yes{});
+        else go(No{}, No{});
+        pages_combine_kernel<D><<<(unsigned)(a.n_units * cols), kThreads, 0, st>>>(a.part, a.plan, cols, a.H, a.G, n_new, out, lse);
     });
     return hipGetLastError();
 }
