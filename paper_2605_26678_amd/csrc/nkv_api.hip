@@ -563,9 +563,8 @@ int nkv_pages_append(const nkv_tokens *tokens, const nkv_pages *pages, void *hip
     }
     if ((uintptr_t)t.positions % 4 || (uintptr_t)t.rope % 16) return NKV_EINVAL;
     if (t.n_q_heads > 0 && t.q == t.q_out) return NKV_EINVAL;       // a pair's dims are read by two threads
-    // one thread for every 16 bytes of the tokens, numbered in 32 bits
-    if ((int64_t)pages->n_seqs * t.n_new >= (1ll << 31) ||
-        (int64_t)pages->n_seqs * t.n_new * (2 * pages->H + t.n_q_heads) >= (1ll << 32) / (pages->d / 8))
+    // a workgroup for a token, numbered in 32 bits
+    if ((int64_t)pages->n_seqs * t.n_new >= (1ll << 31) || t.n_q_heads > (1 << 24))
         return NKV_ESHAPE;
     return launch_pages_append(t, *pages, (hipStream_t)hip_stream) == hipSuccess ? NKV_OK : NKV_EHIP;
 }

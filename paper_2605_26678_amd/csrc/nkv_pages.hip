@@ -5,6 +5,8 @@
 // 32 dims, so four neighbouring lanes find its scale among themselves.
 #include "nkv_pages.h"
 
+#include <algorithm>
+
 namespace nkv {
 namespace {
 
@@ -12,7 +14,8 @@ __device__ __forceinline__ int64_t clamp_row(int64_t r, int64_t rows) { return r
 __device__ __forceinline__ int clamp_len(int len, int max_pages) { return max(0, min(len, max_pages * kRows)); }
 
 // Dims 8 c .. 8 c + 7 of one row as fp32 into the page's rows of K (or V), in the cache's form.  Lanes 4 i .. 4 i + 3 hold a block.
-template <int D, bool F16, bool FP4> __device__ __forceinline__ void store_row(uint8_t *page, bool key, int row, int c, const float (&x)[8])
+// (w: the same in 16 bits, for pages that hold those)
+template <int D, bool F16, bool FP4> __device__ __forceinline__ void store_row(uint8_t *page, bool key, int row, int c, const float (&x)[8], const u32x4 &w16)
 {
     if constexpr (FP4) {
         using P = Fp4Page<D>;
@@ -22,8 +25,16 @@ template <int D, bool F16, bool FP4> __device__ __forceinline__ void store_row(u
         if (c % 4 == 0) page[key ? P::k_scale(row, c / 4) : P::v_scale(row, c / 4)] = (uint8_t)scale;
     } else {
         using P = WidePage<D>;
-        *reinterpret_cast<u32x4 *>(page + (key ? P::k(row, 8 * c) : P::v(row, 8 * c))) = pack8<F16>(x);
+        *reinterpret_cast<u32x4 *>(page + (key ? P::k(row, 8 * c) : P::v(row, 8 * c))) = w16;
     }
+}
+
+// To 32 bits, and not on to 16 in one rounding: the compiler would make one of two.
+__device__ __forceinline__ float rounded(double x)
+{
+    float f = (float)x;
+    asm volatile("" : "+v"(f));
+    return f;
 }
 
 struct AppendArgs {
@@ -33,63 +44,103 @@ struct AppendArgs {
     const int32_t *positions;
     const float *rope;
     int32_t n_new, Hq, rot, halves, n_positions, H, n_pages, max_pages;
-    uint32_t threads;
     const int32_t *table, *lens;
     uint8_t *pool;
 };
 
-// A thread for 16 bytes of k, v or q, in the order of a token's heads: K heads, V heads, query heads.  The rotation's partner of a dim
-// is read by both threads of the pair (from the caches), so no thread waits for another.  In 64 bits the products of a 16-bit value and a
-// 24-bit cosine are exact, so the result is one rounding of the sum, then one to 32 bits, whatever the order of the operations.
+// U of a token's rows and their partners' dims, and where they go: all loads at once.  (Everything by value: captured pointers that a lane chooses among
+// would lie in memory.)
+template <int U>
+__device__ __forceinline__ void load_slots(u32x4 (&own)[U], u32x4 (&other)[U], int (&row)[U], int (&page)[U], int from, int step, int slots,
+                                           const uint16_t *kb, const uint16_t *vb, const uint16_t *qb, int64_t kh, int64_t vh, int64_t qh, int H, int Hq,
+                                           int dim, int mate, const int32_t *lens, const int32_t *table, int max_pages, int behind)
+{
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        const int slot = min(from + i * step, slots - 1), h = slot < H ? slot : slot < 2 * H ? slot - H : slot - 2 * H;
+        const bool key = slot < H, value = !key && slot < 2 * H;
+        const uint16_t *src = (key ? kb : value ? vb : qb) + h * (key ? kh : value ? vh : qh) + dim;
+        own[i] = *reinterpret_cast<const u32x4 *>(src);
+        other[i] = *reinterpret_cast<const u32x4 *>(src + (value ? 0 : mate));
+        row[i] = key || value ? lens[h] : 0;
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        const int slot = min(from + i * step, slots - 1), h = slot < H ? slot : slot - H;
+        page[i] = -1;
+        if (slot < 2 * H) {
+            row[i] = clamp_len(row[i], max_pages) + behind;
+            if (row[i] >= 0) page[i] = table[(int64_t)h * max_pages + row[i] / kRows];
+        }
+    }
+}
+
+// A workgroup for a token's heads (K heads, V heads, query heads), or a share of them: kRowsAt rows at a time, a thread for 16 bytes of a row.  A thread keeps its
+// dims' cosines and sines for all of its rows.  The rotation's partner of a dim is read by both threads of the pair (from the caches), so no thread waits
+// for another.  In 64 bits the products of a 16-bit value and a 24-bit cosine are exact, so the result is one rounding of the sum, then one to 32 bits,
+// whatever the order of the operations.
 template <int D, bool F16, bool FP4> __global__ __launch_bounds__(256) void append_kernel(const AppendArgs a)
 {
-    constexpr uint32_t CPR = D / 8;
-    const uint32_t i = blockIdx.x * 256u + threadIdx.x;
-    if (i >= a.threads) return;                                            // (whole rows)
-    const uint32_t item = i / CPR, slots = 2u * a.H + a.Hq, tok = item / slots, slot = item - tok * slots;
-    const int c = (int)(i - item * CPR), s = (int)(tok / (uint32_t)a.n_new), t = (int)(tok - (uint32_t)s * a.n_new);
-    const bool key = slot < (uint32_t)a.H, value = !key && slot < 2u * a.H;
-    const int h = key ? slot : value ? slot - a.H : slot - 2 * a.H;
+    constexpr int CPR = D / 8, kRowsAt = 256 / CPR, U = 3;
+    const int r = threadIdx.x / CPR, c = threadIdx.x % CPR, tok = blockIdx.x, s = tok / a.n_new, t = tok - s * a.n_new, slots = 2 * a.H + a.Hq;
+    if (r >= kRowsAt) return;
+    const int half = a.rot / 2;
+    const bool turns = 8 * c < a.rot, first = 8 * c < half;
+    const int mate = a.halves && turns ? (first ? half : -half) : 0;
+    const int step = gridDim.y * kRowsAt, slot0 = blockIdx.y * kRowsAt + r;
+    const uint16_t *kb = (const uint16_t *)a.k + s * a.k_str[0] + t * a.k_str[1], *vb = (const uint16_t *)a.v + s * a.v_str[0] + t * a.v_str[1],
+                   *qb = (const uint16_t *)a.q + s * a.q_str[0] + t * a.q_str[1];
+    const int64_t kh = a.k_str[2], vh = a.v_str[2], qh = a.q_str[2];
+    u32x4 own[U], other[U];
+    int row[U], page[U];
     const int pos = a.positions ? a.positions[tok] : 0;
+    if (slot0 < slots) load_slots<U>(own, other, row, page, slot0, step, slots, kb, vb, qb, kh, vh, qh, a.H, a.Hq, 8 * c, mate, a.lens + (int64_t)s * a.H, a.table + (int64_t)s * a.H * a.max_pages, a.max_pages, t - a.n_new);
     if (pos < 0 || (a.rot > 0 && pos >= a.n_positions)) return;
-    int row = 0;
-    uint8_t *page = nullptr;
-    if (key || value) {
-        const int u = s * a.H + h;
-        row = clamp_len(a.lens[u], a.max_pages) - a.n_new + t;
-        if (row < 0) return;
-        const int id = a.table[(int64_t)u * a.max_pages + row / kRows];
-        if (id < 0 || id >= a.n_pages) return;
-        page = a.pool + (int64_t)id * (FP4 ? Fp4Page<D>::kBytes : WidePage<D>::kBytes);
-    }
-    const int64_t *str = key ? a.k_str : value ? a.v_str : a.q_str;
-    const uint16_t *src = (const uint16_t *)(key ? a.k : value ? a.v : a.q) + s * str[0] + t * str[1] + h * str[2];
-    float x[8];
-    unpack8<F16>(*reinterpret_cast<const u32x4 *>(src + 8 * c), x);
-    if (!value && 8 * c < a.rot) {
-        const int half = a.rot / 2;
+    double co[8], si[8];
+    if (turns) {
         const float *cs = a.rope + (int64_t)pos * a.rot, *sn = cs + half;
         if (a.halves) {
-            const bool first = 8 * c < half;
             const int e = first ? 8 * c : 8 * c - half;
-            float y[8];
-            unpack8<F16>(*reinterpret_cast<const u32x4 *>(src + (first ? 8 * c + half : e)), y);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const double m = (double)y[k] * (double)sn[e + k];
-                x[k] = (float)fma((double)x[k], (double)cs[e + k], first ? -m : m);
+                co[k] = cs[e + k];
+                si[k] = first ? -sn[e + k] : sn[e + k];
             }
         } else {
 #pragma unroll
             for (int k = 0; k < 8; k += 2) {
-                const double co = cs[4 * c + k / 2], si = sn[4 * c + k / 2], p = x[k], r = x[k + 1];
-                x[k] = (float)fma(p, co, -(r * si));
-                x[k + 1] = (float)fma(r, co, p * si);
+                co[k] = co[k + 1] = cs[4 * c + k / 2];
+                si[k + 1] = sn[4 * c + k / 2];
+                si[k] = -si[k + 1];
             }
         }
     }
-    if (key || value) store_row<D, F16, FP4>(page, key, row & (kRows - 1), c, x);
-    else *reinterpret_cast<u32x4 *>((uint16_t *)a.q_out + ((int64_t)tok * a.Hq + h) * D + 8 * c) = pack8<F16>(x);
+    for (int from = slot0; from < slots;) {
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const int slot = from + i * step;
+            if (slot >= slots) break;
+            const bool key = slot < a.H, value = !key && slot < 2 * a.H;
+            u32x4 w = own[i];
+            float x[8];
+            unpack8<F16>(w, x);
+            if (!value && turns) {
+                float y[8];
+                unpack8<F16>(other[i], y);
+                if (!a.halves)
+#pragma unroll
+                    for (int k = 0; k < 8; k += 2) y[k] = x[k + 1], y[k + 1] = x[k];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) x[k] = rounded(fma((double)x[k], co[k], (double)y[k] * si[k]));
+                w = pack8<F16>(x);
+            }
+            if (!key && !value) *reinterpret_cast<u32x4 *>((uint16_t *)a.q_out + ((int64_t)tok * a.Hq + slot - 2 * a.H) * D + 8 * c) = w;
+            else if (page[i] >= 0 && page[i] < a.n_pages)
+                store_row<D, F16, FP4>(a.pool + (int64_t)page[i] * (FP4 ? Fp4Page<D>::kBytes : WidePage<D>::kBytes), key, row[i] & (kRows - 1), c, x, w);
+        }
+        from += U * step;
+        if (from < slots) load_slots<U>(own, other, row, page, from, step, slots, kb, vb, qb, kh, vh, qh, a.H, a.Hq, 8 * c, mate, a.lens + (int64_t)s * a.H, a.table + (int64_t)s * a.H * a.max_pages, a.max_pages, t - a.n_new);
+    }
 }
 
 // Packed rows to and from the pages.  A workgroup takes one page of one unit: 16 rows at a time, D / 8 threads a row.  The pages that a unit's
@@ -115,39 +166,52 @@ __global__ __launch_bounds__(2 * D) void rows_kernel(uint16_t *__restrict__ pk, 
     uint8_t *page = pool + (there ? (int64_t)id : 0) * (FP4 ? Fp4Page<D>::kBytes : WidePage<D>::kBytes);
     const int c = threadIdx.x % CPR, r = threadIdx.x / CPR;
     const int64_t at0 = off + j * kRows - first;                          // packed row of the page's row 0
+    const int lo = (int)max(first - j * kRows, (int64_t)0), hi = (int)min(len - j * kRows, (int64_t)kRows);   // the page's rows
+    if constexpr (LOAD || !FP4) {
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-        const int row = 16 * t + r;
-        const int64_t unit_row = j * kRows + row, at = (at0 + row) * D + 8 * c;
-        if (unit_row < first || unit_row >= len) continue;
+        for (int t = 0; t < 4; ++t) {
+            const int row = 16 * t + r;
+            if (row < lo || row >= hi) continue;
 #pragma unroll
-        for (int kv = 0; kv < 2; ++kv) {
-            u32x4 *rowp = reinterpret_cast<u32x4 *>((kv == 0 ? pk : pv) + at);
-            if constexpr (LOAD) {
-                if constexpr (FP4) {
+            for (int kv = 0; kv < 2; ++kv) {
+                u32x4 *rowp = reinterpret_cast<u32x4 *>((kv == 0 ? pk : pv) + (at0 + row) * D + 8 * c);
+                if constexpr (LOAD) {
+                    const u32x4 w = __builtin_nontemporal_load(rowp);
                     float x[8];
-                    unpack8<F16>(__builtin_nontemporal_load(rowp), x);
-                    store_row<D, F16, true>(page, kv == 0, row, c, x);
+                    unpack8<F16>(w, x);
+                    store_row<D, F16, FP4>(page, kv == 0, row, c, x, w);
                 } else {
-                    *reinterpret_cast<u32x4 *>(page + (kv == 0 ? WidePage<D>::k(row, 8 * c) : WidePage<D>::v(row, 8 * c))) = __builtin_nontemporal_load(rowp);
+                    u32x4 w = {0u, 0u, 0u, 0u};
+                    if (there) w = *reinterpret_cast<const u32x4 *>(page + (kv == 0 ? WidePage<D>::k(row, 8 * c) : WidePage<D>::v(row, 8 * c)));
+                    __builtin_nontemporal_store(w, rowp);
                 }
-            } else {
-                u32x4 w = {0u, 0u, 0u, 0u};
-                if (there) {
-                    if constexpr (FP4) {
-                        using P = Fp4Page<D>;
-                        float x[8];
-                        fp4_values(kv == 0 ? *reinterpret_cast<const uint32_t *>(page + P::k_code(row, 8 * c)) : load_v_codes<D>(page, row, c),
-                                   page[kv == 0 ? P::k_scale(row, c / 4) : P::v_scale(row, c / 4)], x);
-                        constexpr float top = F16 ? 65504.f : 0x1.fep127f;
+            }
+        }
+    } else {
+        // all of the page's codes and scales first: a row's scales lie with those of the rows 16, 32 and 48 further on
+        using P = Fp4Page<D>;
+        uint32_t code[2][4];
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) x[k] = x[k] > top ? top : x[k] < -top ? -top : x[k];
-                        w = pack8<F16>(x);
-                    } else {
-                        w = *reinterpret_cast<const u32x4 *>(page + (kv == 0 ? WidePage<D>::k(row, 8 * c) : WidePage<D>::v(row, 8 * c)));
-                    }
-                }
-                __builtin_nontemporal_store(w, rowp);
+        for (int t = 0; t < 4; ++t) {
+            code[0][t] = *reinterpret_cast<const uint32_t *>(page + P::k_code(16 * t + r, 8 * c));
+            code[1][t] = load_v_codes<D>(page, 16 * t + r, c);
+        }
+        const uint32_t ks = *reinterpret_cast<const uint32_t *>(page + P::k_scale(r, c / 4));
+        const u32x4 vs = *reinterpret_cast<const u32x4 *>(page + P::v_scale(r / 4 * 4, c / 4));
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int row = 16 * t + r;
+            if (row < lo || row >= hi) continue;
+#pragma unroll
+            for (int kv = 0; kv < 2; ++kv) {
+                float x[8];
+                fp4_values(code[kv][t], kv == 0 ? ks >> (8 * t) & 255u : vs[t] >> (8 * (r % 4)) & 255u, x);
+                constexpr float top = F16 ? 65504.f : 0x1.fep127f;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) x[k] = x[k] > top ? top : x[k] < -top ? -top : x[k];
+                u32x4 w = pack8<F16>(x);
+                if (!there) w = u32x4{0u, 0u, 0u, 0u};
+                __builtin_nontemporal_store(w, reinterpret_cast<u32x4 *>((kv == 0 ? pk : pv) + (at0 + row) * D + 8 * c));
             }
         }
     }
@@ -169,8 +233,10 @@ hipError_t launch_pages_append(const nkv_tokens &t, const nkv_pages &p, hipStrea
     a.n_new = t.n_new, a.Hq = t.n_q_heads, a.rot = t.rot, a.halves = t.rope_style == NKV_ROPE_HALVES, a.n_positions = t.n_positions;
     a.H = p.H, a.n_pages = p.n_pages, a.max_pages = p.max_pages;
     a.table = p.table, a.lens = p.lens, a.pool = (uint8_t *)p.pool;
-    a.threads = (uint32_t)((int64_t)p.n_seqs * t.n_new * (2 * p.H + t.n_q_heads) * (p.d / 8));
-    const unsigned groups = (unsigned)(((int64_t)a.threads + 255) / 256);
+    // Tokens enough to fill the chip: a workgroup takes all of a token's heads, and loads its angles once; fewer: a share of them.
+    const int64_t tokens = (int64_t)p.n_seqs * t.n_new;
+    const int at_once = 256 / (p.d / 8), most = (2 * p.H + t.n_q_heads + at_once - 1) / at_once;
+    const dim3 groups((unsigned)tokens, (unsigned)std::max<int64_t>(1, std::min<int64_t>(most, 2048 / tokens)));
     for_head_dim(p.d, [&](auto dim) {
         constexpr int D = decltype(dim)::value;
         const bool f16 = p.dtype == NKV_DTYPE_F16, fp4 = p.format == NKV_PAGES_FP4;
