@@ -71,6 +71,9 @@ class nkv_tokens(C.Structure):
                 ("rope", C.c_void_p)]
 
 
+_TOKENS_SIZE = C.sizeof(nkv_tokens)
+
+
 class NkvError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -204,10 +207,26 @@ def _ptr(t) -> int:
     return 0 if t is None else int(t.data_ptr())
 
 
+_current_stream = None
+
+
+def _find_current_stream():
+    """The current device's current stream as a number.  torch's own short cut to it where there is one: a Stream object is 3 us of a
+    call's 7."""
+    import torch
+    raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+    torch.cuda.current_stream()                          # (initialises the device)
+    if raw is None or device is None:
+        return lambda: int(torch.cuda.current_stream().cuda_stream)
+    return lambda: raw(device())
+
+
 def _stream(stream) -> int:
     if stream is None:
-        import torch
-        return int(torch.cuda.current_stream().cuda_stream)
+        global _current_stream
+        if _current_stream is None:
+            _current_stream = _find_current_stream()
+        return _current_stream()
     return int(getattr(stream, "cuda_stream", stream))
 
 
@@ -313,8 +332,10 @@ class Pages:
             raise ValueError("pool, table and lens are contiguous")
         self.pool, self.table, self.lens = pool, table, lens
         self.n_seqs, self.H, self.d, self.dtype, self.format = int(n_seqs), int(H), int(d), int(dtype), int(format)
+        self.torch_dtype, self.torch_f32, self.torch_i32 = _torch_dtype(dtype), torch.float32, torch.int32
         self.c = nkv_pages(C.sizeof(nkv_pages), int(n_seqs), int(H), int(d), int(dtype), int(format), nbytes // size,
                            int(table.shape[1]), _ptr(pool), _ptr(table), _ptr(lens))
+        self.ref = C.byref(self.c)
 
 
 def page_bytes(d: int, dtype: int, format: int) -> int:
@@ -330,15 +351,30 @@ def rope_table(n_positions: int, rot: int, base: float = 10000.0, device="cuda")
     return torch.stack([angle.cos(), angle.sin()], 1).float().contiguous()
 
 
-_TORCH_NAMES = {DTYPE_F32: "torch.float32", DTYPE_BF16: "torch.bfloat16", DTYPE_F16: "torch.float16"}
+def _torch_dtype(dtype: int):
+    import torch
+    return {DTYPE_F32: torch.float32, DTYPE_BF16: torch.bfloat16, DTYPE_F16: torch.float16}.get(int(dtype))
 
 
-def _check_rows(t, what: str, dtype: int, shape=None) -> None:
-    """Rows that a call reads or writes: their type, and their shape where it is given, dense but for an append's inputs."""
-    if str(t.dtype) != _TORCH_NAMES.get(int(dtype)):
-        raise ValueError(f"{what} is {t.dtype}, and the pages' rows are {_TORCH_NAMES.get(int(dtype))}")
-    if shape is not None and (tuple(t.shape) != tuple(shape) or not t.is_contiguous()):
+def _check_rows(t, what: str, pages: Pages, shape=None) -> None:
+    """Rows that a call reads or writes: their type, and, where their shape is given, that and that they are dense."""
+    if t.dtype is not pages.torch_dtype:
+        raise ValueError(f"{what} is {t.dtype}, and the pages' rows are {pages.torch_dtype}")
+    if shape is not None and (t.shape != shape or not t.is_contiguous()):
         raise ValueError(f"{what} is dense {list(shape)}")
+
+
+_Strides = C.c_int64 * 3
+
+
+def _strides(t, what: str, pages: Pages, shape):
+    """Strides of a new token's rows [n_seqs, n, heads, d] (0 along a dim of one); their type and shape are checked."""
+    if t.dtype is not pages.torch_dtype or t.shape != shape:
+        raise ValueError(f"{what} is {pages.torch_dtype} {list(shape)}, not {t.dtype} {list(t.shape)}")
+    s, n, h, e = t.stride()
+    if e != 1:
+        raise ValueError(f"{what}: a row's dims lie next to each other")
+    return _Strides(s if shape[0] > 1 else 0, n if shape[1] > 1 else 0, h if shape[2] > 1 else 0)
 
 
 def pages_append(k, v, pages: Pages, positions=None, rope=None, rope_style: int = ROPE_HALVES, q=None, q_out=None,
@@ -346,40 +382,40 @@ def pages_append(k, v, pages: Pages, positions=None, rope=None, rope_style: int 
     """New tokens' k, v [n_seqs, n, H, d] (any strides but the last dim's) to the last n rows of the pages, k rotated
     by ``rope`` [n_positions, 2, rot / 2] at ``positions`` int32 [n_seqs, n] on the way; q [n_seqs, n, Hq, d] rotated
     into q_out; see ``nkv_pages_append`` in nkv.h."""
-    n = int(k.shape[1])
-    Hq = 0 if q is None else int(q.shape[2])
-    for name, t, heads in (("k", k, pages.H), ("v", v, pages.H), ("q", q, Hq)):
-        if t is not None:
-            _check_rows(t, name, pages.dtype)
-            if tuple(t.shape) != (pages.n_seqs, n, heads, pages.d) or t.stride(3) != 1:
-                raise ValueError(f"{name} is [n_seqs, n, heads, d], neighbouring dims next to each other")
-    if (q is None) != (q_out is None):
+    S, n, d = pages.n_seqs, k.shape[1], pages.d
+    shape = (S, n, pages.H, d)
+    ks, vs = _strides(k, "k", pages, shape), _strides(v, "v", pages, shape)
+    Hq, qs, q_at, out_at = 0, _Strides(), 0, 0
+    if q is not None:
+        if q_out is None:
+            raise ValueError("q and q_out are given together")
+        Hq = q.shape[2]
+        shape = (S, n, Hq, d)
+        qs, q_at, out_at = _strides(q, "q", pages, shape), q.data_ptr(), q_out.data_ptr()
+        _check_rows(q_out, "q_out", pages, shape)
+    elif q_out is not None:
         raise ValueError("q and q_out are given together")
-    if q_out is not None:
-        _check_rows(q_out, "q_out", pages.dtype, (pages.n_seqs, n, Hq, pages.d))
-    rot, n_positions = (0, 0) if rope is None else (2 * int(rope.shape[-1]), int(rope.shape[0]))
-    if rope is not None and (str(rope.dtype) != "torch.float32" or rope.dim() != 3 or rope.shape[1] != 2 or
-                             not rope.is_contiguous()):
-        raise ValueError("rope is fp32 [n_positions, 2, rot / 2], contiguous")
-    if positions is not None and (str(positions.dtype) != "torch.int32" or positions.numel() != pages.n_seqs * n or
-                                  not positions.is_contiguous()):
-        raise ValueError("positions is int32 [n_seqs, n], contiguous")
-
-    def strides(t):
-        return (C.c_int64 * 3)(*(0 if t is None or t.shape[i] == 1 else int(t.stride(i)) for i in range(3)))
-
-    tokens = nkv_tokens(C.sizeof(nkv_tokens), n, Hq, rot, int(rope_style), n_positions, _ptr(k), _ptr(v), _ptr(q),
-                        _ptr(q_out), strides(k), strides(v), strides(q), _ptr(positions), _ptr(rope))
-    rc = lib().nkv_pages_append(C.byref(tokens), C.byref(pages.c), _stream(stream))
+    rot = n_positions = rope_at = pos_at = 0
+    if rope is not None:
+        if rope.dtype is not pages.torch_f32 or rope.dim() != 3 or rope.shape[1] != 2 or not rope.is_contiguous():
+            raise ValueError("rope is fp32 [n_positions, 2, rot / 2], contiguous")
+        rot, n_positions, rope_at = 2 * rope.shape[2], rope.shape[0], rope.data_ptr()
+    if positions is not None:
+        if positions.dtype is not pages.torch_i32 or positions.numel() != S * n or not positions.is_contiguous():
+            raise ValueError("positions is int32 [n_seqs, n], contiguous")
+        pos_at = positions.data_ptr()
+    tokens = nkv_tokens(_TOKENS_SIZE, n, Hq, rot, rope_style, n_positions, k.data_ptr(), v.data_ptr(), q_at, out_at,
+                        ks, vs, qs, pos_at, rope_at)
+    rc = lib().nkv_pages_append(C.byref(tokens), pages.ref, _stream(stream))
     if rc:
         raise NkvError(rc, "nkv_pages_append")
 
 
 def pages_load(packed_k, packed_v, head_off, rows: int, pages: Pages, stream=None) -> None:
     """Packed rows [rows, d] (as ``select_compact`` leaves them) to the end of every unit's pages."""
-    _check_rows(packed_k, "packed_k", pages.dtype)
-    _check_rows(packed_v, "packed_v", pages.dtype)
-    rc = lib().nkv_pages_load(_ptr(packed_k), _ptr(packed_v), _ptr(head_off), int(rows), C.byref(pages.c),
+    _check_rows(packed_k, "packed_k", pages)
+    _check_rows(packed_v, "packed_v", pages)
+    rc = lib().nkv_pages_load(_ptr(packed_k), _ptr(packed_v), _ptr(head_off), int(rows), pages.ref,
                               _stream(stream))
     if rc:
         raise NkvError(rc, "nkv_pages_load")
@@ -387,9 +423,9 @@ def pages_load(packed_k, packed_v, head_off, rows: int, pages: Pages, stream=Non
 
 def pages_read(packed_k, packed_v, head_off, rows: int, pages: Pages, stream=None) -> None:
     """The last head_off[u + 1] - head_off[u] rows of every unit to packed rows [rows, d]."""
-    _check_rows(packed_k, "packed_k", pages.dtype)
-    _check_rows(packed_v, "packed_v", pages.dtype)
-    rc = lib().nkv_pages_read(_ptr(packed_k), _ptr(packed_v), _ptr(head_off), int(rows), C.byref(pages.c),
+    _check_rows(packed_k, "packed_k", pages)
+    _check_rows(packed_v, "packed_v", pages)
+    rc = lib().nkv_pages_read(_ptr(packed_k), _ptr(packed_v), _ptr(head_off), int(rows), pages.ref,
                               _stream(stream))
     if rc:
         raise NkvError(rc, "nkv_pages_read")
@@ -397,7 +433,7 @@ def pages_read(packed_k, packed_v, head_off, rows: int, pages: Pages, stream=Non
 
 def pages_workspace_bytes(pages: Pages, n_q_heads: int, n_new: int = 1) -> int:
     out = C.c_size_t(0)
-    rc = lib().nkv_pages_workspace_bytes(C.byref(pages.c), int(n_q_heads), int(n_new), C.byref(out))
+    rc = lib().nkv_pages_workspace_bytes(pages.ref, int(n_q_heads), int(n_new), C.byref(out))
     if rc:
         raise NkvError(rc, "nkv_pages_workspace_bytes")
     return int(out.value)
@@ -407,8 +443,8 @@ def pages_attention(q, pages: Pages, n_q_heads: int, n_new: int, scale: float, o
                     stream=None) -> None:
     """The last n_new tokens' attention over the pages: q [n_seqs, n_new, Hq, d] -> out fp32 of that shape (and lse
     [n_seqs, n_new, Hq]); see ``nkv_pages_attention`` in nkv.h."""
-    _check_rows(q, "q", pages.dtype, (pages.n_seqs, n_new, n_q_heads, pages.d))
-    rc = lib().nkv_pages_attention(_ptr(q), C.byref(pages.c), int(n_q_heads), int(n_new), float(scale), _ptr(out),
+    _check_rows(q, "q", pages, (pages.n_seqs, n_new, n_q_heads, pages.d))
+    rc = lib().nkv_pages_attention(_ptr(q), pages.ref, int(n_q_heads), int(n_new), float(scale), _ptr(out),
                                    _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(),
                                    _stream(stream))
     if rc:
