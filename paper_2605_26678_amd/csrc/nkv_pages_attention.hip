@@ -107,10 +107,6 @@ __device__ __forceinline__ void load_rows(Rows<D, F16, FP4> &f, const uint8_t *_
 #pragma unroll
         for (int t = 0; t < Q::kTiles; ++t) load_words<Q::kVWords>(f.v[t], page + P::v_code(half * Q::kStep + 16 * t + 4 * g, Q::C * vn));
         load_words<Q::kTiles>(f.vs, page + P::v_scale(half * Q::kStep + 4 * g, Q::C * vn / kBlock));
-        if (half) {
-#pragma unroll
-            for (int i = 0; i < Q::kScales; ++i) f.ks[i] >>= 16;
-        }
     } else {
         using P = WidePage<D>;
 #pragma unroll
@@ -157,6 +153,9 @@ __device__ __forceinline__ void load_query(Query<D, F16, FP4> &f, const uint16_t
     }
 }
 
+// The conversions read a scale's exponent field alone: the byte is moved there, whatever comes with it.
+__device__ __forceinline__ float scale_bits(uint32_t word, int byte) { return __uint_as_float(byte < 3 ? word << (23 - 8 * byte) : word >> 1); }
+
 // Two dims (2 i, 2 i + 1 of the word) as bf16
 __device__ __forceinline__ uint32_t two_codes(uint32_t w, float scale, int i)
 {
@@ -177,7 +176,7 @@ template <bool HALF> __device__ __forceinline__ f32x4 product(const u32x4 &a, co
 
 // s[t][i]: <k, q> of row 16 t + 4 g + i and column n
 template <int D, bool F16, bool FP4>
-__device__ __forceinline__ void key_products(const Rows<D, F16, FP4> &f, const Query<D, F16, FP4> &q, f32x4 (&s)[Geo<D, F16, FP4>::kTiles])
+__device__ __forceinline__ void key_products(const Rows<D, F16, FP4> &f, const Query<D, F16, FP4> &q, int half, f32x4 (&s)[Geo<D, F16, FP4>::kTiles])
 {
     using Q = Geo<D, F16, FP4>;
 #pragma unroll
@@ -187,7 +186,7 @@ __device__ __forceinline__ void key_products(const Rows<D, F16, FP4> &f, const Q
 #pragma unroll
         for (int t = 0; t < Q::kTiles; ++t) {
             if constexpr (FP4) {
-                const float scale = scale_value(f.ks[Q::kScales == Q::J ? j : j * Q::kScales / Q::J] >> (8 * t) & 255u);
+                const float scale = scale_bits(f.ks[Q::kScales == Q::J ? j : j * Q::kScales / Q::J], Q::kTiles * half + t);
                 u32x4 x;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) x[i] = two_codes(f.k[t][j], scale, i);
@@ -207,10 +206,10 @@ __device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return
 template <int D, bool F16, bool FP4, bool FEW> struct State {
     using Q = Geo<D, F16, FP4, FEW>;
     float m, l;
-    f32x4 o[Q::C];
+    f32x4 o[Q::C], sums;                 // FEW: the sum of a column's piece in every element of sums, l is not used
     __device__ __forceinline__ void clear()
     {
-        m = kNone, l = 0.f;
+        m = kNone, l = 0.f, sums = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int t = 0; t < Q::C; ++t) o[t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -255,8 +254,6 @@ __device__ __forceinline__ void accumulate(State<D, F16, FP4, FEW> &st, const Ro
                                            float scale_log2, int piece)
 {
     using Q = Geo<D, F16, FP4, FEW>;
-    constexpr int kSets = FEW ? 1 : Q::kPieces;                            // products with V a pair of dims
-    const uint32_t cut1 = piece >= 1 ? 0xffff0000u : 0u, cut2 = piece >= 2 ? 0xffff0000u : 0u;
     float p[4 * Q::kTiles], top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 4 * Q::kTiles; ++i) {
@@ -271,36 +268,64 @@ __device__ __forceinline__ void accumulate(State<D, F16, FP4, FEW> &st, const Ro
         st.m = m;
         st.l *= f0;
 #pragma unroll
+        for (int i = 0; i < 4; ++i) st.sums[i] *= f0;
+#pragma unroll
         for (int t = 0; t < Q::C; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i) st.o[t][i] *= f0;
     }
     const float base = Q::kShift - st.m;
-    float l = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4 * Q::kTiles; ++i) {
-        p[i] = __builtin_amdgcn_exp2f(fmaf(p[i], scale_log2, base));
-        l += p[i];
-    }
-    st.l += l;
+    for (int i = 0; i < 4 * Q::kTiles; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(p[i], scale_log2, base));
+    // dims 2 k and 2 k + 1 of row 16 t + 4 g + i, next to each other
+    auto values = [&](int t, int i, int k) {
+        const int at = i * (Q::C / 2) + k;
+        if constexpr (FP4) return two_codes(f.v[t][at / 4], scale_bits(f.vs[t], i), at % 4);
+        else return f.v[t][at];
+    };
+    if constexpr (FEW) {
+        // A lane takes its own piece of a weight: bits 24 .. 17, 16 .. 9 and 8 .. 1 of it.  A row's two dims stay side by side, as a product's two
+        // rows: beside (piece, 0) for the first dim, (0, piece) for the second.  Twice the products, of which there are few, and no
+        // exchange of halves between rows' words.  The sum of the weights is one more product, with ones.
+        const uint32_t above = piece == 0 ? 0u : piece == 1 ? 0xffff0000u : 0xffffff00u, upto = piece == 0 ? 0xffff0000u : piece == 1 ? 0xffffff00u : ~0u;
+        const uint32_t one = Q::kHalfP ? 0x3c003c00u : 0x3f803f80u;
 #pragma unroll
-    for (int h = 0; h < Q::kTiles / 2; ++h) {
-        // the 32 rows of tiles 2 h and 2 h + 1: words of two rows' weights, a piece at a time
-        u32x4 w[kSets];
+        for (int t = 0; t < Q::kTiles; ++t) {
+            u32x4 low, high;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float x = p[4 * t + i];
+                if constexpr (Q::kHalfP) {
+                    const _Float16 hi = (_Float16)x, lo = (_Float16)(x - (float)hi);
+                    low[i] = (uint32_t)__builtin_bit_cast(uint16_t, piece == 0 ? hi : lo);
+                    high[i] = low[i] << 16;
+                } else {
+                    const uint32_t own = __float_as_uint(__uint_as_float(__float_as_uint(x) & upto) - __uint_as_float(__float_as_uint(x) & above));
+                    high[i] = own & 0xffff0000u;                           // (a piece under 2^-126 has bits down there)
+                    low[i] = own >> 16;
+                }
+            }
+            st.sums = product<Q::kHalfP>(u32x4{one, one, one, one}, low, st.sums);
+#pragma unroll
+            for (int k = 0; k < Q::C / 2; ++k) {
+                const u32x4 v = {values(t, 0, k), values(t, 1, k), values(t, 2, k), values(t, 3, k)};
+                st.o[2 * k] = product<Q::kHalfP>(v, low, st.o[2 * k]);
+                st.o[2 * k + 1] = product<Q::kHalfP>(v, high, st.o[2 * k + 1]);
+            }
+        }
+    } else {
+        float l = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4 * Q::kTiles; ++i) l += p[i];
+        st.l += l;
+        // the 32 rows of two tiles: words of two rows' weights, a piece at a time
+        u32x4 w[Q::kPieces];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            float a = p[8 * h + 2 * j], b = p[8 * h + 2 * j + 1];
+            float a = p[2 * j], b = p[2 * j + 1];
             if constexpr (Q::kHalfP) {
-                const f16x2 hi = {(_Float16)a, (_Float16)b};
-                const f16x2 lo = {(_Float16)(a - (float)hi.x), (_Float16)(b - (float)hi.y)};
-                if constexpr (FEW) w[0][j] = __builtin_bit_cast(uint32_t, piece == 0 ? hi : lo);
-                else w[0][j] = __builtin_bit_cast(uint32_t, hi), w[1][j] = __builtin_bit_cast(uint32_t, lo);
-            } else if constexpr (FEW) {                                    // a lane's own piece
-                a -= __uint_as_float(__float_as_uint(a) & cut1);
-                b -= __uint_as_float(__float_as_uint(b) & cut1);
-                a -= __uint_as_float(__float_as_uint(a) & cut2);
-                b -= __uint_as_float(__float_as_uint(b) & cut2);
-                w[0][j] = high_halves(__float_as_uint(a), __float_as_uint(b));
+                const f16x2 hi = {(_Float16)a, (_Float16)b}, lo = {(_Float16)(a - (float)hi.x), (_Float16)(b - (float)hi.y)};
+                w[0][j] = __builtin_bit_cast(uint32_t, hi), w[1][j] = __builtin_bit_cast(uint32_t, lo);
             } else {
 #pragma unroll
                 for (int k = 0; k < 3; ++k) {                              // cut off, not rounded: three times eight bits are all 24
@@ -310,36 +335,18 @@ __device__ __forceinline__ void accumulate(State<D, F16, FP4, FEW> &st, const Ro
                 }
             }
         }
-        float scale[8];
-        if constexpr (FP4) {
-#pragma unroll
-            for (int r = 0; r < 8; ++r) {
-                scale[r] = scale_value(f.vs[2 * h + r / 4] >> (8 * (r % 4)) & 255u);
-            }
-        }
 #pragma unroll
         for (int k = 0; k < Q::C / 2; ++k) {
             uint32_t x[8];
 #pragma unroll
-            for (int r = 0; r < 8; ++r) {
-                const int t = 2 * h + r / 4, i = r % 4;
-                if constexpr (FP4) {
-                    const int at = i * (Q::C / 2) + k;
-                    x[r] = two_codes(f.v[t][at / 4], scale[r], at % 4);
-                } else {
-                    x[r] = f.v[t][i * (Q::C / 2) + k];
-                }
-            }
+            for (int r = 0; r < 8; ++r) x[r] = values(r / 4, r % 4, k);
             const u32x4 lo = {low_halves(x[0], x[1]), low_halves(x[2], x[3]), low_halves(x[4], x[5]), low_halves(x[6], x[7])};
             const u32x4 hi = {high_halves(x[0], x[1]), high_halves(x[2], x[3]), high_halves(x[4], x[5]), high_halves(x[6], x[7])};
-            f32x4 a = st.o[2 * k], b = st.o[2 * k + 1];
 #pragma unroll
-            for (int c = kSets - 1; c >= 0; --c) {
-                a = product<Q::kHalfP>(lo, w[c], a);
-                b = product<Q::kHalfP>(hi, w[c], b);
+            for (int c = Q::kPieces - 1; c >= 0; --c) {
+                st.o[2 * k] = product<Q::kHalfP>(lo, w[c], st.o[2 * k]);
+                st.o[2 * k + 1] = product<Q::kHalfP>(hi, w[c], st.o[2 * k + 1]);
             }
-            st.o[2 * k] = a;
-            st.o[2 * k + 1] = b;
         }
     }
 }
@@ -501,7 +508,11 @@ template <int D, bool F16, bool FP4, bool FEW> __global__ __launch_bounds__(kThr
 #pragma unroll
                         for (int r = 0; r < 4; ++r) x[r] += y[r];
                     }
-                ll = fmaf(f, lds_o[i][c][D + 1], ll);
+                float l = lds_o[i][c][D + 1];
+                if constexpr (FEW)
+#pragma unroll
+                    for (int k = 1; k < Q::kPieces; ++k) l += lds_o[i][c + k * Q::kCols][D + 1];
+                ll = fmaf(f, l, ll);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) oo[k] = fmaf(f, x[k], oo[k]);
             }
@@ -525,11 +536,11 @@ template <int D, bool F16, bool FP4, bool FEW> __global__ __launch_bounds__(kThr
         i += end - step;
         auto id_of = [&](uint32_t at) { return at < end ? table[at] : -1; };
         auto page_of = [&](int id) { return a.pool + (int64_t)(id >= 0 && id < a.n_pages ? id : 0) * kBytes; };
-        auto take = [&](Rows<D, F16, FP4> &f, int row) {
+        auto take = [&](Rows<D, F16, FP4> &f, const int row) {
             const int rel = len - (int)(step * kRows) - row, least = rel - (a.n_new - 1);
             if (rel <= 0) return;                                          // (its bytes are the page's, if no rows')
             f32x4 s[Q::kTiles];
-            key_products<D, F16, FP4>(f, q, s);
+            key_products<D, F16, FP4>(f, q, row / Q::kStep, s);
             if (least < Q::kStep) mask_rows<D, F16, FP4>(f, s, g, rel, least + token, least);
             accumulate<D, F16, FP4, FEW>(st, f, s, a.scale_log2, piece);
         };
@@ -551,7 +562,7 @@ template <int D, bool F16, bool FP4, bool FEW> __global__ __launch_bounds__(kThr
             ++step;
         }
         auto sum = [](float x, float y) { return x + y; };
-        const float l = swap_reduce<32>(swap_reduce<16>(st.l, sum), sum);
+        const float l = FEW ? st.sums[0] : swap_reduce<32>(swap_reduce<16>(st.l, sum), sum);
         float *mine_o = lds_o[w][n];
 #pragma unroll
         for (int r = 0; r < 4; ++r)
