@@ -143,6 +143,37 @@ template <int D, bool F16, bool FP4> __global__ __launch_bounds__(256) void appe
     }
 }
 
+// The unit that number i belongs to: its packed rows off .. off + n - 1, its length, and its first number.
+struct Span {
+    int unit, len;
+    int64_t off, n, number;
+};
+__device__ __forceinline__ int64_t of_lane(int64_t x, int lane)
+{
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, lane), hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)((uint64_t)x >> 32), lane);
+    return (int64_t)((uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ Span span_of(const int64_t *head_off, const int32_t *lens, int n_units, int64_t rows, int max_pages, int64_t i)
+{
+    Span s;
+    if (n_units <= kWave) {                                                // everything that may be asked for at once
+        const int lane = threadIdx.x & (kWave - 1), u = min(lane, n_units - 1);
+        const int64_t from = clamp_row(head_off[u], rows), to = clamp_row(head_off[u + 1], rows);
+        const int len = lens[u];
+        const int64_t number = lane == 0 ? 0 : from / kRows + 2 * (int64_t)lane;
+        s.unit = 63 - __builtin_clzll(__ballot(lane < n_units && number <= i));   // (lane 0 is always among them)
+        s.off = of_lane(from, s.unit), s.n = of_lane(to, s.unit) - s.off, s.number = of_lane(number, s.unit);
+        s.len = clamp_len(__builtin_amdgcn_readlane(len, s.unit), max_pages);
+    } else {
+        s.unit = __builtin_amdgcn_readfirstlane(
+            wave_search_fn(n_units, i, [&](int x) { return x == 0 ? (int64_t)0 : clamp_row(head_off[x], rows) / kRows + 2 * (int64_t)x; }));
+        s.off = clamp_row(head_off[s.unit], rows), s.n = clamp_row(head_off[s.unit + 1], rows) - s.off;
+        s.number = s.unit == 0 ? 0 : s.off / kRows + 2 * (int64_t)s.unit;
+        s.len = clamp_len(lens[s.unit], max_pages);
+    }
+    return s;
+}
+
 // Packed rows to and from the pages.  A workgroup takes one page of one unit: 16 rows at a time, D / 8 threads a row.  The pages that a unit's
 // rows touch are numbered from off[u] / 64 + 2 u on, which leaves room for all of them (n rows touch at most n / 64 + 2 pages), so no kernel plans in front.
 // grid: as many numbers as there are.
@@ -153,37 +184,41 @@ __global__ __launch_bounds__(2 * D) void rows_kernel(uint16_t *__restrict__ pk, 
 {
     constexpr int CPR = D / 8;
     const int64_t i = blockIdx.x;
-    const int u = __builtin_amdgcn_readfirstlane(
-        wave_search_fn(n_units, i, [&](int x) { return x == 0 ? (int64_t)0 : clamp_row(head_off[x], rows) / kRows + 2 * (int64_t)x; }));
-    const int64_t off = clamp_row(head_off[u], rows), n = clamp_row(head_off[u + 1], rows) - off;
-    const int len = clamp_len(lens[u], max_pages);
-    const int64_t first = len - n;                                        // of the unit's rows, the one that `off` is
-    const int64_t j = (first >= 0 ? first / kRows : -((-first + kRows - 1) / kRows)) + i - (u == 0 ? 0 : off / kRows + 2 * (int64_t)u);
-    if (n <= 0 || j * kRows >= len) return;
+    const Span sp = span_of(head_off, lens, n_units, rows, max_pages, i);
+    const int u = sp.unit, len = sp.len;
+    const int64_t first = len - sp.n;                                     // of the unit's rows, the one that the first packed one is
+    const int64_t j = (first >= 0 ? first / kRows : -((-first + kRows - 1) / kRows)) + i - sp.number;
+    if (sp.n <= 0 || j * kRows >= len) return;
     const int id = j >= 0 ? table[(int64_t)u * max_pages + j] : -1;
     const bool there = id >= 0 && id < n_pages;
     if (LOAD && !there) return;
     uint8_t *page = pool + (there ? (int64_t)id : 0) * (FP4 ? Fp4Page<D>::kBytes : WidePage<D>::kBytes);
     const int c = threadIdx.x % CPR, r = threadIdx.x / CPR;
-    const int64_t at0 = off + j * kRows - first;                          // packed row of the page's row 0
+    const int64_t at0 = sp.off + j * kRows - first;                       // packed row of the page's row 0
     const int lo = (int)max(first - j * kRows, (int64_t)0), hi = (int)min(len - j * kRows, (int64_t)kRows);   // the page's rows
     if constexpr (LOAD || !FP4) {
+        u32x4 w[2][4];                                                    // (rows outside: others' that are asked for anyway)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int row = min(max(16 * t + r, lo), hi - 1);
+#pragma unroll
+            for (int kv = 0; kv < 2; ++kv) {
+                if constexpr (LOAD) w[kv][t] = __builtin_nontemporal_load(reinterpret_cast<u32x4 *>((kv == 0 ? pk : pv) + (at0 + row) * D + 8 * c));
+                else w[kv][t] = *reinterpret_cast<const u32x4 *>(page + (kv == 0 ? WidePage<D>::k(row, 8 * c) : WidePage<D>::v(row, 8 * c)));
+            }
+        }
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
             const int row = 16 * t + r;
             if (row < lo || row >= hi) continue;
 #pragma unroll
             for (int kv = 0; kv < 2; ++kv) {
-                u32x4 *rowp = reinterpret_cast<u32x4 *>((kv == 0 ? pk : pv) + (at0 + row) * D + 8 * c);
                 if constexpr (LOAD) {
-                    const u32x4 w = __builtin_nontemporal_load(rowp);
                     float x[8];
-                    unpack8<F16>(w, x);
-                    store_row<D, F16, FP4>(page, kv == 0, row, c, x, w);
+                    unpack8<F16>(w[kv][t], x);
+                    store_row<D, F16, FP4>(page, kv == 0, row, c, x, w[kv][t]);
                 } else {
-                    u32x4 w = {0u, 0u, 0u, 0u};
-                    if (there) w = *reinterpret_cast<const u32x4 *>(page + (kv == 0 ? WidePage<D>::k(row, 8 * c) : WidePage<D>::v(row, 8 * c)));
-                    __builtin_nontemporal_store(w, rowp);
+                    __builtin_nontemporal_store(there ? w[kv][t] : u32x4{0u, 0u, 0u, 0u}, reinterpret_cast<u32x4 *>((kv == 0 ? pk : pv) + (at0 + row) * D + 8 * c));
                 }
             }
         }
