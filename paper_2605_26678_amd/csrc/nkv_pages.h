@@ -85,16 +85,31 @@ __device__ __forceinline__ uint32_t fp4_codes(const float (&x)[8], uint32_t scal
     w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], s, 3);
     return scale == 255u ? 0u : w;
 }
-__device__ __forceinline__ void fp4_values(uint32_t w, uint32_t scale, float (&x)[8])
+// Eight values in the rows' type, those beyond its largest finite one as that, NaN for scale 255.
+template <bool F16> __device__ __forceinline__ u32x4 fp4_rows(uint32_t w, uint32_t scale)
 {
-    using f32x2 = float __attribute__((ext_vector_type(2)));
     const float s = scale_value(scale);
-    const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 1),
-                c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 3);
-    x[0] = a.x, x[1] = a.y, x[2] = b.x, x[3] = b.y, x[4] = c.x, x[5] = c.y, x[6] = d.x, x[7] = d.y;
-    if (scale == 255u)
+    u32x4 r;
+    if constexpr (F16) {
+        r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 0)), r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 1));
+        r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 2)), r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 3));
+    } else {
+        r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0)), r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1));
+        r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2)), r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3));
+    }
+    if (scale >= (F16 ? 141u : 253u)) {                                    // seldom: 6 * 2^14 and 6 * 2^126 are beyond the types
+        constexpr uint32_t most = F16 ? 0x7bffu : 0x7f7fu;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(0x7fc00000u);
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t code = w >> (4 * i) & 15u, sign = (code & 8u) << 12;
+            // magnitudes as 2^(e) * 1 or 1.5, e relative to the scale
+            const int e = (int)scale - 127 + (int)((code & 7u) >> 1) - 1;
+            const bool beyond = (code & 7u) >= 2u && e > (F16 ? 15 : 127);
+            const uint32_t h = scale == 255u ? 0x7fffu : sign | most;
+            if (scale == 255u || beyond) r[i / 2] = i % 2 ? (r[i / 2] & 0xffffu) | h << 16 : (r[i / 2] & 0xffff0000u) | h;
+        }
+    }
+    return r;
 }
 
 // The eight codes of dims 8 c .. 8 c + 7 of V row `row`, which lie in one piece (or two, of head dims up to 64).

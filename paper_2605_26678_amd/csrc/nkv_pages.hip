@@ -239,12 +239,7 @@ __global__ __launch_bounds__(2 * D) void rows_kernel(uint16_t *__restrict__ pk, 
             if (row < lo || row >= hi) continue;
 #pragma unroll
             for (int kv = 0; kv < 2; ++kv) {
-                float x[8];
-                fp4_values(code[kv][t], kv == 0 ? ks >> (8 * t) & 255u : vs[t] >> (8 * (r % 4)) & 255u, x);
-                constexpr float top = F16 ? 65504.f : 0x1.fep127f;
-#pragma unroll
-                for (int k = 0; k < 8; ++k) x[k] = x[k] > top ? top : x[k] < -top ? -top : x[k];
-                u32x4 w = pack8<F16>(x);
+                u32x4 w = fp4_rows<F16>(code[kv][t], kv == 0 ? ks >> (8 * t) & 255u : vs[t] >> (8 * (r % 4)) & 255u);
                 if (!there) w = u32x4{0u, 0u, 0u, 0u};
                 __builtin_nontemporal_store(w, reinterpret_cast<u32x4 *>((kv == 0 ? pk : pv) + (at0 + row) * D + 8 * c));
             }

@@ -191,6 +191,29 @@ def test_4_bit_codes_of_ties_zeros_extremes_and_nan(dtype):
         assert torch.equal(got.cpu().isnan(), as_type.isnan())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_every_code_with_every_scale_reads_as_its_value(dtype):
+    """Rows of all 16 codes under all 256 scale bytes, as K and as V; values between the type's steps are rounded to nearest, ties to even."""
+    c = Cache(1, 1, 64, dtype, "fp4", [256], seed=10)
+    codes = np.tile(np.arange(16, dtype=np.uint8), 4)
+    k, v, ks, vs = op.places(64)
+    for j in range(4):
+        page = c.pool[c.table[0, j]]
+        for r in range(64):
+            for at in (k, v):
+                page[at[r, 0::2]] = codes[0::2] | codes[1::2] << 4
+            page[ks[r]], page[vs[r]] = 64 * j + r, 255 - (64 * j + r)
+    off = torch.tensor([0, 256], device=DEV)
+    back = [torch.empty(256, 64, dtype=c.torch_dtype, device=DEV) for _ in range(2)]
+    nkv.pages_read(back[0], back[1], off, 256, c.on(DEV))
+    top = torch.finfo(c.torch_dtype).max
+    for got, scales in zip(back, (np.arange(256), 255 - np.arange(256))):
+        exact = op.values(np.tile(codes, (256, 1)), np.repeat(scales[:, None], 2, 1).astype(np.uint8))
+        want = torch.from_numpy(np.clip(exact, -top, top)).to(c.torch_dtype)
+        assert torch.equal(got.cpu().isnan(), want.isnan())
+        assert torch.equal(got.cpu().nan_to_num(7.0)[scales >= 1], want.nan_to_num(7.0)[scales >= 1])   # (0 is no scale that is written)
+
+
 @pytest.mark.parametrize("d", [64, 96, 128, 192, 256])
 @pytest.mark.parametrize("fmt,dtype", [("fp4", "bf16"), ("fp4", "fp16"), ("16bit", "bf16")])
 @pytest.mark.parametrize("behind", [0, 37])
