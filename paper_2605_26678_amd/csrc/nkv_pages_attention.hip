@@ -24,7 +24,8 @@ using bf16x8 = __bf16 __attribute__((ext_vector_type(8)));
 using f16x8 = _Float16 __attribute__((ext_vector_type(8)));
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
-constexpr int kMostGroups = 768;         // workgroups: three for every compute unit
+// Workgroups that a compute unit holds at once, by the registers that a head dim takes, and no more than that are launched.
+__host__ __device__ constexpr int groups_at_once(int D) { return D == 64 ? 4 : D <= 128 ? 3 : 2; }
 constexpr float kNone = -1.0e30f;        // running maximum before any row was seen
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -52,8 +53,6 @@ template <int D, bool F16, bool FP4, bool FEW = false> struct Geo {
     // 4 bits: lane g holds dims D / 4 * g on, J words of a row; one scale byte or two if that is no more than a block or two
     static constexpr int kScales = D == 64 || D == 128 ? 1 : D == 256 ? 2 : J;
     static constexpr int kVWords = FP4 ? C / 2 : 2 * C;
-    // two halves' rows at once, where the registers are there for it
-    static constexpr bool kAhead = FP4 || D == 64;
     // fp16 weights are of up to 2^14, so that their second piece does not run out of exponents
     static constexpr bool kHalfP = F16 && !FP4;
     static constexpr float kShift = kHalfP ? 14.f : 0.f;
@@ -69,20 +68,27 @@ template <int D, bool F16, bool FP4> struct Rows {
     uint32_t vs[Q::kTiles];              // 4 bits: scale bytes of those rows, a word a tile
 };
 
-// N words from an address that is a multiple of the largest load that divides them.
-template <int N> __device__ __forceinline__ void load_words(uint32_t *w, const uint8_t *at)
+// N words from an address that is a multiple of the largest load that divides them.  ONCE: no cache keeps them; not where a wavefront's load takes
+// parts of lines whose rest the next one takes (head dims from 192 on: 36 x 8 x 4096 rows of 256 dims of 4 bits 78.8 us that way, 74.5 without; of 128 dims
+// of 4 bits 61.4 and 69.3).
+template <bool ONCE, typename T> __device__ __forceinline__ T load_from(const uint8_t *at)
+{
+    if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const T *>(at));
+    else return *reinterpret_cast<const T *>(at);
+}
+template <int N, bool ONCE> __device__ __forceinline__ void load_words(uint32_t *w, const uint8_t *at)
 {
     using u32x3 = unsigned int __attribute__((ext_vector_type(3), aligned(4)));
     if constexpr (N % 4 == 0) {
 #pragma unroll
         for (int i = 0; i < N; i += 4) {
-            const u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(at + 4 * i));
+            const u32x4 x = load_from<ONCE, u32x4>(at + 4 * i);
             w[i] = x.x, w[i + 1] = x.y, w[i + 2] = x.z, w[i + 3] = x.w;
         }
     } else if constexpr (N % 2 == 0) {
 #pragma unroll
         for (int i = 0; i < N; i += 2) {
-            const u32x2 x = __builtin_nontemporal_load(reinterpret_cast<const u32x2 *>(at + 4 * i));
+            const u32x2 x = load_from<ONCE, u32x2>(at + 4 * i);
             w[i] = x.x, w[i + 1] = x.y;
         }
     } else {
@@ -93,30 +99,40 @@ template <int N> __device__ __forceinline__ void load_words(uint32_t *w, const u
 }
 
 template <int D, bool F16, bool FP4>
-__device__ __forceinline__ void load_rows(Rows<D, F16, FP4> &f, const uint8_t *__restrict__ page, int half, int n, int g)
+__device__ __forceinline__ void load_keys(Rows<D, F16, FP4> &f, const uint8_t *__restrict__ page, int half, int n, int g)
+{
+    using Q = Geo<D, F16, FP4>;
+    if constexpr (FP4) {
+        using P = Fp4Page<D>;
+#pragma unroll
+        for (int t = 0; t < Q::kTiles; ++t) load_words<Q::J, D <= 128>(f.k[t], page + P::k_code(half * Q::kStep + 16 * t + n, D / 4 * g));
+#pragma unroll
+        for (int i = 0; i < Q::kScales; ++i)
+            f.ks[i] = *reinterpret_cast<const uint32_t *>(page + P::k_scale(n, (D / 4 * g + (Q::kScales == Q::J ? 8 : 32) * i) / kBlock));
+    } else {
+        using P = WidePage<D>;
+#pragma unroll
+        for (int t = 0; t < Q::kTiles; ++t)
+#pragma unroll
+            for (int b = 0; b < Q::J; ++b) load_words<4, D <= 128>(f.k[t] + 4 * b, page + P::k(half * Q::kStep + 16 * t + n, 32 * b + 8 * g));
+    }
+}
+template <int D, bool F16, bool FP4>
+__device__ __forceinline__ void load_values(Rows<D, F16, FP4> &f, const uint8_t *__restrict__ page, int half, int n, int g)
 {
     using Q = Geo<D, F16, FP4>;
     const int vn = min(n, Q::VL - 1);                                     // lanes without dims of V take another's
     if constexpr (FP4) {
         using P = Fp4Page<D>;
 #pragma unroll
-        for (int t = 0; t < Q::kTiles; ++t) load_words<Q::J>(f.k[t], page + P::k_code(half * Q::kStep + 16 * t + n, D / 4 * g));
-#pragma unroll
-        for (int i = 0; i < Q::kScales; ++i)
-            f.ks[i] = *reinterpret_cast<const uint32_t *>(page + P::k_scale(n, (D / 4 * g + (Q::kScales == Q::J ? 8 : 32) * i) / kBlock));
-#pragma unroll
-        for (int t = 0; t < Q::kTiles; ++t) load_words<Q::kVWords>(f.v[t], page + P::v_code(half * Q::kStep + 16 * t + 4 * g, Q::C * vn));
-        load_words<Q::kTiles>(f.vs, page + P::v_scale(half * Q::kStep + 4 * g, Q::C * vn / kBlock));
+        for (int t = 0; t < Q::kTiles; ++t) load_words<Q::kVWords, D <= 128>(f.v[t], page + P::v_code(half * Q::kStep + 16 * t + 4 * g, Q::C * vn));
+        load_words<Q::kTiles, D <= 128>(f.vs, page + P::v_scale(half * Q::kStep + 4 * g, Q::C * vn / kBlock));
     } else {
         using P = WidePage<D>;
 #pragma unroll
         for (int t = 0; t < Q::kTiles; ++t)
 #pragma unroll
-            for (int b = 0; b < Q::J; ++b) load_words<4>(f.k[t] + 4 * b, page + P::k(half * Q::kStep + 16 * t + n, 32 * b + 8 * g));
-#pragma unroll
-        for (int t = 0; t < Q::kTiles; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) load_words<Q::C / 2>(f.v[t] + i * (Q::C / 2), page + P::v(half * Q::kStep + 16 * t + 4 * g + i, Q::C * vn));
+            for (int i = 0; i < 4; ++i) load_words<Q::C / 2, D <= 128>(f.v[t] + i * (Q::C / 2), page + P::v(half * Q::kStep + 16 * t + 4 * g + i, Q::C * vn));
     }
 }
 
@@ -469,7 +485,7 @@ __device__ __forceinline__ Place placed_by_workgroup(const AttendArgs &a, int w)
 }
 
 // grid: (stretches / kWaves, groups of columns)
-template <int D, bool F16, bool FP4, bool FEW> __global__ __launch_bounds__(kThreads, D <= 128 ? 3 : 2) void pages_attend_kernel(const AttendArgs a)
+template <int D, bool F16, bool FP4, bool FEW> __global__ __launch_bounds__(kThreads, groups_at_once(D)) void pages_attend_kernel(const AttendArgs a)
 {
     using Q = Geo<D, F16, FP4, FEW>;
     constexpr int kBytes = FP4 ? Fp4Page<D>::kBytes : WidePage<D>::kBytes;
@@ -536,29 +552,44 @@ template <int D, bool F16, bool FP4, bool FEW> __global__ __launch_bounds__(kThr
         i += end - step;
         auto id_of = [&](uint32_t at) { return at < end ? table[at] : -1; };
         auto page_of = [&](int id) { return a.pool + (int64_t)(id >= 0 && id < a.n_pages ? id : 0) * kBytes; };
-        auto take = [&](Rows<D, F16, FP4> &f, const int row) {
-            const int rel = len - (int)(step * kRows) - row, least = rel - (a.n_new - 1);
-            if (rel <= 0) return;                                          // (its bytes are the page's, if no rows')
-            f32x4 s[Q::kTiles];
-            key_products<D, F16, FP4>(f, q, row / Q::kStep, s);
-            if (least < Q::kStep) mask_rows<D, F16, FP4>(f, s, g, rel, least + token, least);
-            accumulate<D, F16, FP4, FEW>(st, f, s, a.scale_log2, piece);
-        };
-        Rows<D, F16, FP4> even, odd;
         int id = id_of(step), next = id_of(step + 1);
         const uint8_t *page = page_of(id);
-        if (Q::kAhead && step < end) load_rows<D, F16, FP4>(even, page, 0, n, g);
-        // the next half's rows are on their way while a half is worked on (behind the last page: some page's)
+        // A half's rows, while the next half's are on their way.  4 bits: in a second set of registers.  16 bits: in the same ones, keys as soon as their
+        // products are made, values after theirs.  (Behind the last page: some page's.)
+        Rows<D, F16, FP4> even, odd;
+        auto take = [&](Rows<D, F16, FP4> &f, const int half, bool counts, auto keys_on, auto values_on) {
+            const int rel = len - (int)(step * kRows) - half * Q::kStep, least = rel - (a.n_new - 1);
+            const bool works = counts && rel > 0;                          // (a half without rows is loaded too: its bytes are the page's)
+            f32x4 s[Q::kTiles];
+            if (works) key_products<D, F16, FP4>(f, q, half, s);
+            keys_on();
+            if (works) {
+                if (least < Q::kStep) mask_rows<D, F16, FP4>(f, s, g, rel, least + token, least);
+                accumulate<D, F16, FP4, FEW>(st, f, s, a.scale_log2, piece);
+            }
+            values_on();
+        };
+        if (step < end) {
+            load_keys<D, F16, FP4>(even, page, 0, n, g);
+            load_values<D, F16, FP4>(even, page, 0, n, g);
+        }
         while (step < end) {
             const int after = id_of(step + 2);
             const bool counts = id >= 0 && id < a.n_pages;
-            if (!Q::kAhead) load_rows<D, F16, FP4>(even, page, 0, n, g);
-            else load_rows<D, F16, FP4>(odd, page, 1, n, g);
-            if (counts) take(even, 0);
-            if (!Q::kAhead) load_rows<D, F16, FP4>(odd, page, 1, n, g);
+            const uint8_t *const this_page = page;
             id = next, next = after, page = page_of(id);
-            if (Q::kAhead) load_rows<D, F16, FP4>(even, page, 0, n, g);
-            if (counts) take(odd, Q::kStep);
+            auto nothing = [] {};
+            if constexpr (FP4) {
+                load_keys<D, F16, FP4>(odd, this_page, 1, n, g);
+                load_values<D, F16, FP4>(odd, this_page, 1, n, g);
+                take(even, 0, counts, nothing, nothing);
+                load_keys<D, F16, FP4>(even, page, 0, n, g);
+                load_values<D, F16, FP4>(even, page, 0, n, g);
+                take(odd, 1, counts, nothing, nothing);
+            } else {
+                take(even, 0, counts, [&] { load_keys<D, F16, FP4>(even, this_page, 1, n, g); }, [&] { load_values<D, F16, FP4>(even, this_page, 1, n, g); });
+                take(even, 1, counts, [&] { load_keys<D, F16, FP4>(even, page, 0, n, g); }, [&] { load_values<D, F16, FP4>(even, page, 0, n, g); });
+            }
             ++step;
         }
         auto sum = [](float x, float y) { return x + y; };
@@ -648,7 +679,7 @@ template <int D> __global__ __launch_bounds__(kThreads) void pages_combine_kerne
 unsigned groups_of(const nkv_pages &p)
 {
     const int64_t most = (int64_t)p.n_seqs * p.H * p.max_pages;
-    return (unsigned)std::min<int64_t>(kMostGroups, (most + kWaves - 1) / kWaves);
+    return (unsigned)std::min<int64_t>(256 * groups_at_once(p.d), (most + kWaves - 1) / kWaves);
 }
 size_t plan_bytes(const nkv_pages &p) { return ((size_t)p.n_seqs * p.H * sizeof(Parts) + 255) / 256 * 256; }
 
@@ -675,9 +706,13 @@ hipError_t launch_pages_attention(const void *q, const nkv_pages &p, int n_q_hea
         constexpr int D = decltype(dim)::value;
         auto go = [&](auto f16, auto fp4) {
             constexpr bool F16 = decltype(f16)::value, FP4 = decltype(fp4)::value;
-            const dim3 grid(groups_of(p), cols <= Geo<D, F16, FP4, true>::kCols ? 1u : (unsigned)((cols + 15) / 16));
-            if (grid.y == 1 && cols <= 5) pages_attend_kernel<D, F16, FP4, true><<<grid, kThreads, 0, st>>>(a);
-            else pages_attend_kernel<D, F16, FP4, false><<<grid, kThreads, 0, st>>>(a);
+            if constexpr (FP4) {                                           // (16-bit rows are bound by memory either way)
+                if (cols <= Geo<D, F16, FP4, true>::kCols) {
+                    pages_attend_kernel<D, F16, FP4, true><<<groups_of(p), kThreads, 0, st>>>(a);
+                    return;
+                }
+            }
+            pages_attend_kernel<D, F16, FP4, false><<<dim3(groups_of(p), (unsigned)((cols + 15) / 16)), kThreads, 0, st>>>(a);
         };
         using Yes = std::true_type;
         using No = std::false_type;
