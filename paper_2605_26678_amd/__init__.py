@@ -557,3 +557,58 @@ class Compressor:
                        self.packed_v, self.kept_idx, self.head_off, self.rows, self.near, self.ws, stream)
         return Compressed(self.scores, self.k_per_head, self.head_off, self.kept_idx[:self.rows],
                           self.packed_k[:self.rows], self.packed_v[:self.rows], self.near)
+
+
+class PagedCache:
+    """Owns a paged cache's pool, table and lengths and hands out its pages, on the host: ``pages`` is what the calls
+    take.  ``lens`` (device) is the program's to write; ``reserve`` only sees to it that there are pages."""
+
+    def __init__(self, n_seqs: int, H: int, d: int, dtype: int, format: int, n_pages: int, max_rows: int,
+                 device="cuda:0"):
+        import torch
+        self.n_seqs, self.H = int(n_seqs), int(H)
+        size = page_bytes(d, dtype, format)
+        if size < 0:
+            raise NkvError(NKV_EUNSUPPORTED, "nkv_page_bytes")
+        self.pool = torch.zeros(n_pages, size, dtype=torch.uint8, device=device)
+        width = max(1, (int(max_rows) + PAGE_ROWS - 1) // PAGE_ROWS)
+        self.table = torch.full((n_seqs * H, width), -1, dtype=torch.int32, device=device)
+        self.lens = torch.zeros(n_seqs * H, dtype=torch.int32, device=device)
+        self.pages = Pages(n_seqs, H, d, dtype, format, self.pool, self.table, self.lens)
+        self._free = list(range(int(n_pages) - 1, -1, -1))
+        self._held = [[] for _ in range(n_seqs * H)]
+
+    @property
+    def free_pages(self) -> int:
+        return len(self._free)
+
+    def reserve(self, rows: Sequence[int]) -> None:
+        """Pages for that many rows of every unit (as many as it has, if that is more): all of them or, when the pool has
+        too few or a unit's row of the table is too short, none."""
+        rows = [int(x) for x in rows]
+        if len(rows) != len(self._held):
+            raise ValueError("one number of rows per unit")
+        more = [max(0, (n + PAGE_ROWS - 1) // PAGE_ROWS - len(h)) for n, h in zip(rows, self._held)]
+        if max(m + len(h) for m, h in zip(more, self._held)) > self.table.shape[1]:
+            raise ValueError(f"a unit holds {self.table.shape[1] * PAGE_ROWS} rows")
+        if sum(more) > len(self._free):
+            raise MemoryError(f"{sum(more)} pages are wanted and {len(self._free)} free")
+        for h, m in zip(self._held, more):
+            h.extend(self._free.pop() for _ in range(m))
+        if any(more):
+            self._write()
+
+    def release(self, seq: int) -> None:
+        """Gives a sequence's pages back; its lengths become 0."""
+        for u in range(seq * self.H, (seq + 1) * self.H):
+            self._free.extend(reversed(self._held[u]))
+            self._held[u] = []
+        self.lens[seq * self.H:(seq + 1) * self.H] = 0
+        self._write()
+
+    def _write(self) -> None:
+        import torch
+        host = torch.full(tuple(self.table.shape), -1, dtype=torch.int32)
+        for u, h in enumerate(self._held):
+            host[u, :len(h)] = torch.tensor(h, dtype=torch.int32)
+        self.table.copy_(host)

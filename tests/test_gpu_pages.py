@@ -513,3 +513,17 @@ def test_the_compressors_rows_through_pages(fmt):
         torch.cuda.synchronize()
         assert float((out.reshape(want.shape) - want).abs().max()) <= 2 * TOL * 6
         assert float((lse.reshape(want_lse.shape) - want_lse).abs().max()) <= 2 * TOL * 10
+
+
+@pytest.mark.parametrize("fmt", ["fp4", "16bit"])
+def test_the_example_runs(fmt, monkeypatch, capsys):
+    import importlib.util
+    import os
+    import sys
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "paged_decode.py")
+    spec = importlib.util.spec_from_file_location("paged_decode", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    monkeypatch.setattr(sys, "argv", [path, "--format", fmt, "--prompt", "700", "--tokens", "6", "--layers", "2"])
+    assert example.main() == 0
+    assert f"{fmt} pages hold" in capsys.readouterr().out

@@ -177,3 +177,27 @@ def test_oracle_attention_is_softmax_attention():
         want = torch.nn.functional.scaled_dot_product_attention(torch.from_numpy(q[0, t, :2]), k, v, scale=0.125)
         assert np.allclose(out[0, t, :2], want.numpy(), atol=1e-12)
     assert np.isneginf(lse[1, :, :2]).all() and (out[1, :, :2] == 0).all() and np.isfinite(lse[0]).all()
+
+
+def test_paged_cache_hands_out_every_page_once():
+    c = nkv.PagedCache(2, 2, 64, nkv.DTYPE_BF16, nkv.PAGES_FP4, n_pages=9, max_rows=200, device="cpu")
+    assert c.table.shape == (4, 4) and bool((c.table == -1).all()) and c.free_pages == 9
+    c.reserve([1, 64, 65, 0])
+    held = c.table[c.table >= 0].tolist()
+    assert (c.table >= 0).sum(1).tolist() == [1, 1, 2, 0] and len(set(held)) == 4 and c.free_pages == 5
+    c.reserve([1, 10, 129, 0])                                              # what is held stays where it is
+    assert c.table[c.table >= 0].tolist()[:4] == held and c.free_pages == 4
+    with pytest.raises(MemoryError):
+        c.reserve([200, 200, 0, 0])
+    with pytest.raises(ValueError):
+        c.reserve([257, 0, 0, 0])
+    with pytest.raises(ValueError):
+        c.reserve([1, 1])
+    assert c.free_pages == 4
+    c.lens[2:] = 7
+    c.release(1)
+    assert c.free_pages == 7 and c.lens.tolist() == [0, 0, 0, 0] and (c.table >= 0).sum(1).tolist() == [1, 1, 0, 0]
+    c.reserve([256, 64, 0, 0])
+    assert c.free_pages == 4 and len(set(c.table[c.table >= 0].tolist())) == 5
+    with pytest.raises(nkv.NkvError):
+        nkv.PagedCache(1, 1, 80, nkv.DTYPE_BF16, nkv.PAGES_FP4, 1, 64, device="cpu")
