@@ -484,6 +484,17 @@ __device__ __forceinline__ Place placed_by_workgroup(const AttendArgs &a, int w)
     return p;
 }
 
+// Older wavefronts of a SIMD are served first, and stretches are equally long: a compute unit's first workgroup was done after 40 us, its third after 51
+// (36 x 8 x 8192 rows of 4 bits).  So those with more of their stretch left go first, by quarters: 60.4 -> 60.1 us, with 8 query heads a KV head 66.1 ->
+// 62.5, of 64 dims 38.3 -> 35.9, of 256 dims of 16 bits 137 -> 131.
+__device__ __forceinline__ void by_what_is_left(uint32_t left, uint32_t run)
+{
+    if (4u * left > 3u * run) __builtin_amdgcn_s_setprio(3);
+    else if (2u * left > run) __builtin_amdgcn_s_setprio(2);
+    else if (4u * left > run) __builtin_amdgcn_s_setprio(1);
+    else __builtin_amdgcn_s_setprio(0);
+}
+
 // grid: (stretches / kWaves, groups of columns)
 template <int D, bool F16, bool FP4, bool FEW> __global__ __launch_bounds__(kThreads, groups_at_once(D)) void pages_attend_kernel(const AttendArgs a)
 {
@@ -491,6 +502,7 @@ template <int D, bool F16, bool FP4, bool FEW> __global__ __launch_bounds__(kThr
     constexpr int kBytes = FP4 ? Fp4Page<D>::kBytes : WidePage<D>::kBytes;
     __shared__ __align__(16) float lds_o[kWaves][16][D + 4];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
+    __builtin_amdgcn_s_setprio(3);
     const Place at = a.n_units <= kWave * kUnitsLane ? placed_by_wave(a, w) : placed_by_workgroup(a, w);
     const uint32_t total = at.total, run = at.run;
     const uint32_t group_lo = blockIdx.x * kWaves * run;
@@ -591,6 +603,7 @@ template <int D, bool F16, bool FP4, bool FEW> __global__ __launch_bounds__(kThr
                 take(even, 1, counts, [&] { load_keys<D, F16, FP4>(even, page, 0, n, g); }, [&] { load_values<D, F16, FP4>(even, page, 0, n, g); });
             }
             ++step;
+            by_what_is_left(hi - i + end - step, run);
         }
         auto sum = [](float x, float y) { return x + y; };
         const float l = FEW ? st.sums[0] : swap_reduce<32>(swap_reduce<16>(st.l, sum), sum);
