@@ -6,12 +6,18 @@
 //   S = K Q^T     4-bit values become bf16, which holds them exactly (an fp16 query then in two bf16 pieces); 16 x 16 x 32 products
 //                 over a lane's dims in turn.  (The scaled product of 4-bit rows as they lie in the page and 8-bit pieces of a query
 //                 loses bits of small terms beside large ones: up to 6e-6 of the terms' sum, 2e-7 in the mean.)
-//   O^T = V^T P   two rows' dims are put side by side as the operand wants them; a weight is split into three bf16 pieces (two of fp16), which hold its 24 (22) bits.
+//   O^T = V^T P   a weight is split into three bf16 pieces (two of fp16 for rows of those), which hold its 24 (22) bits.
 // A column's running maximum, sum and weighted values stay in registers; with rows as the operands' other axis no lane
 // exchange is needed between the products: the rows that a lane holds of S are those it holds of P, and V's rows are taken in that order.
 //
-// Work is cut into stretches of steps (64 rows of 4 bits, 32 of 16 bits) across units, one for every wavefront; a stretch's part of a unit
-// goes to the workspace as (maximum, sum, weighted values) and pages_combine_kernel joins a unit's.
+// The pages of all units are cut into stretches of the same length, one for every wavefront that the device holds, whichever units they belong to: the lengths
+// are on the device, so every wavefront finds its own by counting.  A stretch's part of a unit goes to the workspace as (maximum, sum, weighted
+// values), that of a workgroup's four stretches in one unit as one, and pages_combine_kernel joins a unit's.  A wavefront works on 32 rows, half a page,
+// while the next ones are on their way.
+//
+// Whole calls, us, and what reading the same bytes alone takes (6.8 TB/s): 36 x 8 units of about 8192 rows, head dim 128, 4 query heads a KV head, bf16, 4
+// bits 65 (kernel 59.5), 49; one layer of them 10.3, 1.4: the launches, and three trips to memory one after the other (lengths, page, rows).  A call that
+// fills the device takes some 10 us beside 4.1 a page and wavefront (6.5 TB/s); the vector and matrix instructions of that page take 2.8.
 #include "nkv_pages.h"
 
 #include <algorithm>
@@ -26,7 +32,7 @@ using f16x8 = _Float16 __attribute__((ext_vector_type(8)));
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 // Workgroups that a compute unit holds at once, by the registers that a head dim takes, and no more than that are launched.
 __host__ __device__ constexpr int groups_at_once(int D) { return D == 64 ? 4 : D <= 128 ? 3 : 2; }
-constexpr float kNone = -1.0e30f;        // running maximum before any row was seen
+constexpr float kNone = -3.0e38f;        // running maximum before any row was seen
 constexpr float kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ int clamp_len(int len, int max_pages) { return max(0, min(len, max_pages * kRows)); }
@@ -44,9 +50,10 @@ struct AttendArgs {
     float *part;                         // [part][column][D + 4]: weighted values, maximum, sum
 };
 
-// FEW: up to five columns, whose weights' pieces lie side by side in the 16 columns of a product.
-template <int D, bool F16, bool FP4, bool FEW = false> struct Geo {
-    static constexpr int kCols = FEW ? 5 : 16;
+// COLS: columns a workgroup takes, 16, or of 4-bit pages 5 where there are no more: their weights' three pieces then lie side by side in the 16 columns of a
+// product.  (Two pieces side by side for up to 8 columns gain nothing: 8 query heads a KV head, fp16, 64.6 us and 65.9 with 16 columns, bf16 62.6 and 62.4.)
+template <int D, bool F16, bool FP4, int COLS = 16> struct Geo {
+    static constexpr int kSlots = COLS == 5 ? 3 : 1;
     static constexpr int NB = D / kBlock, C = chunk_of(D), VL = D / C;        // VL lanes of 16 hold dims of V
     static constexpr int kTiles = 2, kStep = 16 * kTiles;           // rows of a step
     static constexpr int J = D / 32;                                          // products over the dims of a row
@@ -56,7 +63,7 @@ template <int D, bool F16, bool FP4, bool FEW = false> struct Geo {
     // fp16 weights are of up to 2^14, so that their second piece does not run out of exponents
     static constexpr bool kHalfP = F16 && !FP4;
     static constexpr float kShift = kHalfP ? 14.f : 0.f;
-    static constexpr int kPieces = kHalfP ? 2 : 3;
+    static constexpr int kPieces = kHalfP ? 2 : 3, kSets = (kPieces + kSlots - 1) / kSlots;   // products a pair of a row's dims
 };
 
 // What a lane (n = lane % 16, g = lane / 16) holds of a step's rows.
@@ -138,6 +145,7 @@ __device__ __forceinline__ void load_values(Rows<D, F16, FP4> &f, const uint8_t 
 
 // A column's query as the products take it: word j of a lane holds the dims that k's does.  A negative scale's sign goes to the query (flip:
 // 0x80008000), so that the largest logit is that of the largest product.
+// An fp16 query against 4-bit keys is two bf16 pieces.
 template <int D, bool F16, bool FP4> struct Query {
     u32x4 w[F16 && FP4 ? 2 : 1][D / 32];
 };
@@ -219,10 +227,10 @@ __device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return
 
 // Running state of 16 columns: lane (n, g) holds column n's maximum, its own rows' share of the sum, and the weighted values of dims
 // (4 g + i) C + t in o[t][i].
-template <int D, bool F16, bool FP4, bool FEW> struct State {
-    using Q = Geo<D, F16, FP4, FEW>;
+template <int D, bool F16, bool FP4, int COLS> struct State {
+    using Q = Geo<D, F16, FP4, COLS>;
     float m, l;
-    f32x4 o[Q::C], sums;                 // FEW: the sum of a column's piece in every element of sums, l is not used
+    f32x4 o[Q::C], sums;                 // COLS = 5: the sum of a column's piece in every element of sums, l is not used
     __device__ __forceinline__ void clear()
     {
         m = kNone, l = 0.f, sums = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -265,11 +273,11 @@ __device__ __forceinline__ void mask_rows(Rows<D, F16, FP4> &f, f32x4 (&s)[Geo<D
         }
 }
 
-template <int D, bool F16, bool FP4, bool FEW>
-__device__ __forceinline__ void accumulate(State<D, F16, FP4, FEW> &st, const Rows<D, F16, FP4> &f, const f32x4 (&products)[Geo<D, F16, FP4>::kTiles],
-                                           float scale_log2, int piece)
+template <int D, bool F16, bool FP4, int COLS>
+__device__ __forceinline__ void accumulate(State<D, F16, FP4, COLS> &st, const Rows<D, F16, FP4> &f, const f32x4 (&products)[Geo<D, F16, FP4>::kTiles],
+                                           float scale_log2, int slot)
 {
-    using Q = Geo<D, F16, FP4, FEW>;
+    using Q = Geo<D, F16, FP4, COLS>;
     float p[4 * Q::kTiles], top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 4 * Q::kTiles; ++i) {
@@ -299,34 +307,32 @@ __device__ __forceinline__ void accumulate(State<D, F16, FP4, FEW> &st, const Ro
         if constexpr (FP4) return two_codes(f.v[t][at / 4], scale_bits(f.vs[t], i), at % 4);
         else return f.v[t][at];
     };
-    if constexpr (FEW) {
-        // A lane takes its own piece of a weight: bits 24 .. 17, 16 .. 9 and 8 .. 1 of it.  A row's two dims stay side by side, as a product's two
-        // rows: beside (piece, 0) for the first dim, (0, piece) for the second.  Twice the products, of which there are few, and no
-        // exchange of halves between rows' words.  The sum of the weights is one more product, with ones.
-        const uint32_t above = piece == 0 ? 0u : piece == 1 ? 0xffff0000u : 0xffffff00u, upto = piece == 0 ? 0xffff0000u : piece == 1 ? 0xffffff00u : ~0u;
-        const uint32_t one = Q::kHalfP ? 0x3c003c00u : 0x3f803f80u;
+    // The three pieces of a weight are its bits 24 .. 17, 16 .. 9 and 8 .. 1, the differences between it cut off behind them: exact, and cut to bf16 as
+    // they are.  A lane of COLS = 5 takes the one of its slot.
+    constexpr uint32_t kTop = 0xffff0000u, kMid = 0xffffff00u;
+    auto between = [](float x, uint32_t upto, uint32_t above) {
+        return __float_as_uint(__uint_as_float(__float_as_uint(x) & upto) - __uint_as_float(__float_as_uint(x) & above));
+    };
+    if constexpr (COLS == 5) {
+        // A row's two dims stay side by side, as a product's two rows: beside (piece, 0) for the first dim, (0, piece) for the second.  Twice the
+        // products, of which there are few, and no exchange of halves between rows' words.  The sum of the weights is one more product, with ones.
+        constexpr uint32_t one = 0x3f803f80u;
+        const uint32_t upto = slot == 0 ? kTop : slot == 1 ? kMid : ~0u, above = slot == 0 ? 0u : slot == 1 ? kTop : kMid;
 #pragma unroll
         for (int t = 0; t < Q::kTiles; ++t) {
             u32x4 low, high;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float x = p[4 * t + i];
-                if constexpr (Q::kHalfP) {
-                    const _Float16 hi = (_Float16)x, lo = (_Float16)(x - (float)hi);
-                    low[i] = (uint32_t)__builtin_bit_cast(uint16_t, piece == 0 ? hi : lo);
-                    high[i] = low[i] << 16;
-                } else {
-                    const uint32_t own = __float_as_uint(__uint_as_float(__float_as_uint(x) & upto) - __uint_as_float(__float_as_uint(x) & above));
-                    high[i] = own & 0xffff0000u;                           // (a piece under 2^-126 has bits down there)
-                    low[i] = own >> 16;
-                }
+                const uint32_t own = between(p[4 * t + i], upto, above);
+                high[i] = own & kTop;                                      // (a piece under 2^-126 has bits down there)
+                low[i] = own >> 16;
             }
-            st.sums = product<Q::kHalfP>(u32x4{one, one, one, one}, low, st.sums);
+            st.sums = product<false>(u32x4{one, one, one, one}, low, st.sums);
 #pragma unroll
             for (int k = 0; k < Q::C / 2; ++k) {
                 const u32x4 v = {values(t, 0, k), values(t, 1, k), values(t, 2, k), values(t, 3, k)};
-                st.o[2 * k] = product<Q::kHalfP>(v, low, st.o[2 * k]);
-                st.o[2 * k + 1] = product<Q::kHalfP>(v, high, st.o[2 * k + 1]);
+                st.o[2 * k] = product<false>(v, low, st.o[2 * k]);
+                st.o[2 * k + 1] = product<false>(v, high, st.o[2 * k + 1]);
             }
         }
     } else {
@@ -335,20 +341,17 @@ __device__ __forceinline__ void accumulate(State<D, F16, FP4, FEW> &st, const Ro
         for (int i = 0; i < 4 * Q::kTiles; ++i) l += p[i];
         st.l += l;
         // the 32 rows of two tiles: words of two rows' weights, a piece at a time
-        u32x4 w[Q::kPieces];
+        u32x4 w[Q::kSets];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            float a = p[2 * j], b = p[2 * j + 1];
+            const float a = p[2 * j], b = p[2 * j + 1];
             if constexpr (Q::kHalfP) {
                 const f16x2 hi = {(_Float16)a, (_Float16)b}, lo = {(_Float16)(a - (float)hi.x), (_Float16)(b - (float)hi.y)};
                 w[0][j] = __builtin_bit_cast(uint32_t, hi), w[1][j] = __builtin_bit_cast(uint32_t, lo);
             } else {
-#pragma unroll
-                for (int k = 0; k < 3; ++k) {                              // cut off, not rounded: three times eight bits are all 24
-                    w[k][j] = high_halves(__float_as_uint(a), __float_as_uint(b));
-                    a -= __uint_as_float(__float_as_uint(a) & 0xffff0000u);
-                    b -= __uint_as_float(__float_as_uint(b) & 0xffff0000u);
-                }
+                w[0][j] = high_halves(__float_as_uint(a), __float_as_uint(b));
+                w[1][j] = high_halves(between(a, kMid, kTop), between(b, kMid, kTop));
+                w[2][j] = high_halves(between(a, ~0u, kMid), between(b, ~0u, kMid));
             }
         }
 #pragma unroll
@@ -359,7 +362,7 @@ __device__ __forceinline__ void accumulate(State<D, F16, FP4, FEW> &st, const Ro
             const u32x4 lo = {low_halves(x[0], x[1]), low_halves(x[2], x[3]), low_halves(x[4], x[5]), low_halves(x[6], x[7])};
             const u32x4 hi = {high_halves(x[0], x[1]), high_halves(x[2], x[3]), high_halves(x[4], x[5]), high_halves(x[6], x[7])};
 #pragma unroll
-            for (int c = Q::kPieces - 1; c >= 0; --c) {
+            for (int c = Q::kSets - 1; c >= 0; --c) {
                 st.o[2 * k] = product<Q::kHalfP>(lo, w[c], st.o[2 * k]);
                 st.o[2 * k + 1] = product<Q::kHalfP>(hi, w[c], st.o[2 * k + 1]);
             }
@@ -496,9 +499,9 @@ __device__ __forceinline__ void by_what_is_left(uint32_t left, uint32_t run)
 }
 
 // grid: (stretches / kWaves, groups of columns)
-template <int D, bool F16, bool FP4, bool FEW> __global__ __launch_bounds__(kThreads, groups_at_once(D)) void pages_attend_kernel(const AttendArgs a)
+template <int D, bool F16, bool FP4, int COLS> __global__ __launch_bounds__(kThreads, groups_at_once(D)) void pages_attend_kernel(const AttendArgs a)
 {
-    using Q = Geo<D, F16, FP4, FEW>;
+    using Q = Geo<D, F16, FP4, COLS>;
     constexpr int kBytes = FP4 ? Fp4Page<D>::kBytes : WidePage<D>::kBytes;
     __shared__ __align__(16) float lds_o[kWaves][16][D + 4];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
@@ -508,16 +511,15 @@ template <int D, bool F16, bool FP4, bool FEW> __global__ __launch_bounds__(kThr
     const uint32_t group_lo = blockIdx.x * kWaves * run;
     if (group_lo >= total) return;
     // ---- columns ----
-    const int cols = a.n_new * a.G, col0 = blockIdx.y * Q::kCols, col = col0 + (FEW ? n % Q::kCols : n);
+    const int cols = a.n_new * a.G, col0 = blockIdx.y * COLS, col = col0 + n % COLS, slot = n / COLS;
     const bool there = col < cols;
     const int token = (there ? col : cols - 1) / a.G, head = (there ? col : cols - 1) - token * a.G;
-    const int piece = FEW ? n / Q::kCols : 0;
 
     const uint32_t stretch = blockIdx.x * kWaves + w, lo = group_lo + w * run, hi = min(lo + run, total);
     int u = at.unit;
     uint32_t step = lo - at.first;                                         // page of the unit
     const bool joined = at.joined;
-    const int here = min(Q::kCols, cols - col0);
+    const int here = min(COLS, cols - col0);
     // columns [0, here) of what `waves` wavefronts left, from `first` on, by `threads` threads, to the workspace
     auto write = [&](int first, int waves, int number, int unit, int thread, int threads) {
         float *dst = a.part + (((int64_t)number + unit) * cols + col0) * (D + 4);
@@ -529,17 +531,16 @@ template <int D, bool F16, bool FP4, bool FEW> __global__ __launch_bounds__(kThr
             for (int i = first; i < first + waves; ++i) {
                 const float f = __builtin_amdgcn_exp2f(lds_o[i][c][D] - mm);
                 f32x4 x = *reinterpret_cast<const f32x4 *>(&lds_o[i][c][e]);
-                if constexpr (FEW)
 #pragma unroll
-                    for (int k = 1; k < Q::kPieces; ++k) {
-                        const f32x4 y = *reinterpret_cast<const f32x4 *>(&lds_o[i][c + k * Q::kCols][e]);
+                for (int k = 1; k < Q::kSlots; ++k) {
+                    const f32x4 y = *reinterpret_cast<const f32x4 *>(&lds_o[i][c + k * COLS][e]);
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) x[r] += y[r];
-                    }
+                    for (int r = 0; r < 4; ++r) x[r] += y[r];
+                }
                 float l = lds_o[i][c][D + 1];
-                if constexpr (FEW)
+                if constexpr (COLS == 5)
 #pragma unroll
-                    for (int k = 1; k < Q::kPieces; ++k) l += lds_o[i][c + k * Q::kCols][D + 1];
+                    for (int k = 1; k < Q::kSlots; ++k) l += lds_o[i][c + k * COLS][D + 1];
                 ll = fmaf(f, l, ll);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) oo[k] = fmaf(f, x[k], oo[k]);
@@ -555,7 +556,7 @@ template <int D, bool F16, bool FP4, bool FEW> __global__ __launch_bounds__(kThr
     uint32_t i = lo;
     do {
         Query<D, F16, FP4> q;
-        State<D, F16, FP4, FEW> st;
+        State<D, F16, FP4, COLS> st;
         st.clear();
         const int len = clamp_len(a.lens[u], a.max_pages), sq = u / a.H, h = u - sq * a.H;
         const int32_t *table = a.table + (int64_t)u * a.max_pages;
@@ -577,7 +578,7 @@ template <int D, bool F16, bool FP4, bool FEW> __global__ __launch_bounds__(kThr
             keys_on();
             if (works) {
                 if (least < Q::kStep) mask_rows<D, F16, FP4>(f, s, g, rel, least + token, least);
-                accumulate<D, F16, FP4, FEW>(st, f, s, a.scale_log2, piece);
+                accumulate<D, F16, FP4, COLS>(st, f, s, a.scale_log2, slot);
             }
             values_on();
         };
@@ -606,7 +607,7 @@ template <int D, bool F16, bool FP4, bool FEW> __global__ __launch_bounds__(kThr
             by_what_is_left(hi - i + end - step, run);
         }
         auto sum = [](float x, float y) { return x + y; };
-        const float l = FEW ? st.sums[0] : swap_reduce<32>(swap_reduce<16>(st.l, sum), sum);
+        const float l = COLS == 5 ? st.sums[0] : swap_reduce<32>(swap_reduce<16>(st.l, sum), sum);
         float *mine_o = lds_o[w][n];
 #pragma unroll
         for (int r = 0; r < 4; ++r)
@@ -719,13 +720,14 @@ hipError_t launch_pages_attention(const void *q, const nkv_pages &p, int n_q_hea
         constexpr int D = decltype(dim)::value;
         auto go = [&](auto f16, auto fp4) {
             constexpr bool F16 = decltype(f16)::value, FP4 = decltype(fp4)::value;
-            if constexpr (FP4) {                                           // (16-bit rows are bound by memory either way)
-                if (cols <= Geo<D, F16, FP4, true>::kCols) {
-                    pages_attend_kernel<D, F16, FP4, true><<<groups_of(p), kThreads, 0, st>>>(a);
-                    return;
-                }
+            auto launch = [&](auto columns) {
+                constexpr int COLS = decltype(columns)::value;
+                pages_attend_kernel<D, F16, FP4, COLS><<<dim3(groups_of(p), (unsigned)((cols + COLS - 1) / COLS)), kThreads, 0, st>>>(a);
+            };
+            if constexpr (FP4) {                                           // (16-bit rows are bound by memory with 16 columns too)
+                if (cols <= 5) return launch(std::integral_constant<int, 5>{});
             }
-            pages_attend_kernel<D, F16, FP4, false><<<dim3(groups_of(p), (unsigned)((cols + 15) / 16)), kThreads, 0, st>>>(a);
+            launch(std::integral_constant<int, 16>{});
         };
         using Yes = std::true_type;
         using No = std::false_type;
