@@ -382,20 +382,34 @@ struct Parts {
         return i < front ? x + i : i < front + (b - a) ? kWaves * (a + i - front) : kWaves * b + (i - front - (b - a));
     }
 };
-// of a unit whose c > 0 steps are the at-th on; total: of all units
-__device__ __forceinline__ Parts parts_of(uint32_t at, uint32_t c, uint32_t run, uint32_t total)
+// All units' pages in n stretches, the first `rem` one page longer than the others.  (Rounded up alike, 37 440 pages for 3072 wavefronts took 2880 of them.)
+struct Cut {
+    uint32_t base, rem;
+    __device__ Cut() {}
+    __device__ Cut(uint32_t total, uint32_t n) : base(total / n), rem(total - total / n * n) {}
+    __device__ uint32_t first(uint32_t i) const { return i * base + min(i, rem); }
+    __device__ uint32_t of(uint32_t at) const                              // the stretch that holds a page
+    {
+        const uint32_t wide = rem * (base + 1);
+        return at < wide ? at / (base + 1) : rem + (at - wide) / base;
+    }
+};
+// of a unit whose c > 0 pages are the at-th on; total: of all units
+__device__ __forceinline__ Parts parts_of(uint32_t at, uint32_t c, const Cut &cut, uint32_t total)
 {
     Parts p;
-    p.x = (int)(at / run);
-    p.y = (int)((at + c - 1) / run) + 1;
-    p.a = (int)((at + kWaves * run - 1) / (kWaves * run));
-    p.b = at + c == total ? (p.y + kWaves - 1) / kWaves : (int)((at + c) / (run * kWaves));
+    p.x = (int)cut.of(at);
+    p.y = (int)cut.of(at + c - 1) + 1;
+    const int whole = p.x + (cut.first(p.x) < at ? 1 : 0), upto = p.y - (cut.first(p.y) > at + c ? 1 : 0);   // the stretches that lie in the unit altogether
+    p.a = (whole + kWaves - 1) / kWaves;
+    p.b = at + c == total ? (p.y + kWaves - 1) / kWaves : upto / kWaves;   // (behind the last page stretches are empty)
     return p;
 }
 
-// Where a wavefront's stretch begins.  Stretches are of `run` pages; the pages of all units are counted in their order.
+// Where a wavefront's stretch begins.  The pages of all units are counted in their order.
 struct Place {
-    uint32_t total, run;
+    uint32_t total;
+    Cut cut;
     int unit, unit0;                     // the unit that holds the stretch's first page, and that of the workgroup's first stretch
     uint32_t first;                      // the first page of `unit`
     bool joined;                         // all of the workgroup's pages lie in unit0: its wavefronts' parts become one
@@ -422,8 +436,8 @@ __device__ __forceinline__ Place placed_by_wave(const AttendArgs &a, int w)
         p.total += (uint32_t)__builtin_amdgcn_readlane((int)incl, kWave - 1);
     }
     const uint32_t stretches = gridDim.x * kWaves;
-    p.run = max(1u, (p.total + stretches - 1) / stretches);
-    const uint32_t lo0 = blockIdx.x * kWaves * p.run, lo = lo0 + w * p.run, hi = min(lo0 + kWaves * p.run, p.total);
+    p.cut = Cut(p.total, stretches);
+    const uint32_t lo0 = p.cut.first(blockIdx.x * kWaves), lo = p.cut.first(blockIdx.x * kWaves + w), hi = p.cut.first((blockIdx.x + 1) * kWaves);
     p.unit = p.unit0 = 0, p.first = 0u, p.joined = false;
 #pragma unroll
     for (int k = 0; k < kUnitsLane; ++k) {
@@ -439,7 +453,7 @@ __device__ __forceinline__ Place placed_by_wave(const AttendArgs &a, int w)
             p.unit0 = k * kWave + l;
             p.joined = (uint32_t)__builtin_amdgcn_readlane((int)(at[k] + c[k]), l) >= hi;
         }
-        if (plans() && w == 0 && k * kWave + lane < a.n_units) a.plan[k * kWave + lane] = c[k] ? parts_of(at[k], c[k], p.run, p.total) : Parts{0, 0, 0, 0};
+        if (plans() && w == 0 && k * kWave + lane < a.n_units) a.plan[k * kWave + lane] = c[k] ? parts_of(at[k], c[k], p.cut, p.total) : Parts{0, 0, 0, 0};
     }
     return p;
 }
@@ -464,15 +478,15 @@ __device__ __forceinline__ Place placed_by_workgroup(const AttendArgs &a, int w)
         p.total += wsum[i];
     }
     const uint32_t stretches = gridDim.x * kWaves;
-    p.run = max(1u, (p.total + stretches - 1) / stretches);
-    const uint32_t lo0 = blockIdx.x * kWaves * p.run, hi = min(lo0 + kWaves * p.run, p.total);
+    p.cut = Cut(p.total, stretches);
+    const uint32_t lo0 = p.cut.first(blockIdx.x * kWaves), hi = p.cut.first((blockIdx.x + 1) * kWaves);
     if (plans() || (at < hi && at + mine > lo0)) {
         for (int u = u0; u < u1; ++u) {
             const uint32_t c = pages_of(a, u);
-            if (plans()) a.plan[u] = c ? parts_of(at, c, p.run, p.total) : Parts{0, 0, 0, 0};
+            if (plans()) a.plan[u] = c ? parts_of(at, c, p.cut, p.total) : Parts{0, 0, 0, 0};
 #pragma unroll
             for (int i = 0; i < kWaves; ++i)
-                if (at <= lo0 + i * p.run && lo0 + i * p.run < at + c) {
+                if (const uint32_t lo = p.cut.first(blockIdx.x * kWaves + i); at <= lo && lo < at + c) {
                     unit[i] = u;
                     first[i] = at;
                     if (i == 0) joined = at + c >= hi;
@@ -507,15 +521,14 @@ template <int D, bool F16, bool FP4, int COLS> __global__ __launch_bounds__(kThr
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
     __builtin_amdgcn_s_setprio(3);
     const Place at = a.n_units <= kWave * kUnitsLane ? placed_by_wave(a, w) : placed_by_workgroup(a, w);
-    const uint32_t total = at.total, run = at.run;
-    const uint32_t group_lo = blockIdx.x * kWaves * run;
-    if (group_lo >= total) return;
+    const uint32_t group_lo = at.cut.first(blockIdx.x * kWaves);
+    if (group_lo >= at.total) return;
     // ---- columns ----
     const int cols = a.n_new * a.G, col0 = blockIdx.y * COLS, col = col0 + n % COLS, slot = n / COLS;
     const bool there = col < cols;
     const int token = (there ? col : cols - 1) / a.G, head = (there ? col : cols - 1) - token * a.G;
 
-    const uint32_t stretch = blockIdx.x * kWaves + w, lo = group_lo + w * run, hi = min(lo + run, total);
+    const uint32_t stretch = blockIdx.x * kWaves + w, lo = at.cut.first(stretch), hi = at.cut.first(stretch + 1);
     int u = at.unit;
     uint32_t step = lo - at.first;                                         // page of the unit
     const bool joined = at.joined;
@@ -604,7 +617,7 @@ template <int D, bool F16, bool FP4, int COLS> __global__ __launch_bounds__(kThr
                 take(even, 1, counts, [&] { load_keys<D, F16, FP4>(even, page, 0, n, g); }, [&] { load_values<D, F16, FP4>(even, page, 0, n, g); });
             }
             ++step;
-            by_what_is_left(hi - i + end - step, run);
+            by_what_is_left(hi - i + end - step, hi - lo);
         }
         auto sum = [](float x, float y) { return x + y; };
         const float l = COLS == 5 ? st.sums[0] : swap_reduce<32>(swap_reduce<16>(st.l, sum), sum);
