@@ -48,58 +48,57 @@ struct AppendArgs {
     uint8_t *pool;
 };
 
-// U of a token's rows and their partners' dims, and where they go: all loads at once.  (Everything by value: captured pointers that a lane chooses among
-// would lie in memory.)
-template <int U>
-__device__ __forceinline__ void load_slots(u32x4 (&own)[U], u32x4 (&other)[U], int (&row)[U], int (&page)[U], int from, int step, int slots,
-                                           const uint16_t *kb, const uint16_t *vb, const uint16_t *qb, int64_t kh, int64_t vh, int64_t qh, int H, int Hq,
-                                           int dim, int mate, const int32_t *lens, const int32_t *table, int max_pages, int behind)
+// A token's row in `slot`, 16 bytes from dim d0 and from d1 on, and where it goes: row and page of its unit.  (Everything by value: captured pointers that a lane
+// chooses among would lie in memory.)
+struct Slot {
+    u32x4 a, b;
+    int row, page;
+};
+__device__ __forceinline__ Slot load_slot(int slot, const uint16_t *kb, const uint16_t *vb, const uint16_t *qb, int64_t kh, int64_t vh, int64_t qh, int H,
+                                          int d0, int d1, const int32_t *lens, const int32_t *table, int max_pages, int behind)
 {
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-        const int slot = min(from + i * step, slots - 1), h = slot < H ? slot : slot < 2 * H ? slot - H : slot - 2 * H;
-        const bool key = slot < H, value = !key && slot < 2 * H;
-        const uint16_t *src = (key ? kb : value ? vb : qb) + h * (key ? kh : value ? vh : qh) + dim;
-        own[i] = *reinterpret_cast<const u32x4 *>(src);
-        other[i] = *reinterpret_cast<const u32x4 *>(src + (value ? 0 : mate));
-        row[i] = key || value ? lens[h] : 0;
+    const bool key = slot < H, value = !key && slot < 2 * H;
+    const int h = key ? slot : value ? slot - H : slot - 2 * H;
+    const uint16_t *src = (key ? kb : value ? vb : qb) + h * (key ? kh : value ? vh : qh);
+    Slot s{*reinterpret_cast<const u32x4 *>(src + d0), *reinterpret_cast<const u32x4 *>(src + d1), 0, -1};
+    if (key || value) {
+        s.row = clamp_len(lens[h], max_pages) + behind;
+        if (s.row >= 0) s.page = table[(int64_t)h * max_pages + s.row / kRows];
     }
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-        const int slot = min(from + i * step, slots - 1), h = slot < H ? slot : slot - H;
-        page[i] = -1;
-        if (slot < 2 * H) {
-            row[i] = clamp_len(row[i], max_pages) + behind;
-            if (row[i] >= 0) page[i] = table[(int64_t)h * max_pages + row[i] / kRows];
-        }
-    }
+    return s;
 }
 
-// A workgroup for a token's heads (K heads, V heads, query heads), or a share of them: kRowsAt rows at a time, a thread for 16 bytes of a row.  A thread keeps its
-// dims' cosines and sines for all of its rows.  The rotation's partner of a dim is read by both threads of the pair (from the caches), so no thread waits
-// for another.  In 64 bits the products of a 16-bit value and a 24-bit cosine are exact, so the result is one rounding of the sum, then one to 32 bits,
-// whatever the order of the operations.
-template <int D, bool F16, bool FP4> __global__ __launch_bounds__(256) void append_kernel(const AppendArgs a)
+// A workgroup for a token's heads (K heads, V heads, query heads), or a share of them: kRowsAt rows at a time.  A thread keeps its dims' cosines and sines for
+// all of its rows, and takes eight dims of a row, or, BOTH, two times eight: both dims of eight pairs (or eight and eight that are not rotated), so that each is
+// read and widened once.  In 64 bits the products of a 16-bit value and a 24-bit cosine are exact, so the result is one rounding of the sum, then one to 32 bits,
+// whatever the order of the operations.  3 x 2731 tokens of 8 + 32 heads, head dim 128: eight dims a thread 46.6 us, twice eight 36.9 (4.8 TB/s), with the next
+// rows asked for before a row is worked on 41.8: it is wavefronts, and their instructions, half of them in 64 bits, that it takes, not loads in flight.
+template <int D, bool F16, bool FP4, bool BOTH> __global__ __launch_bounds__(256) void append_kernel(const AppendArgs a)
 {
-    constexpr int CPR = D / 8, kRowsAt = 256 / CPR, U = 3;
-    const int r = threadIdx.x / CPR, c = threadIdx.x % CPR, tok = blockIdx.x, s = tok / a.n_new, t = tok - s * a.n_new, slots = 2 * a.H + a.Hq;
+    constexpr int CPR = D / 8, kLanes = BOTH ? CPR / 2 : CPR, kRowsAt = 256 / kLanes;
+    const int r = threadIdx.x / kLanes, c = threadIdx.x % kLanes, tok = blockIdx.x, s = tok / a.n_new, t = tok - s * a.n_new, slots = 2 * a.H + a.Hq;
     if (r >= kRowsAt) return;
     const int half = a.rot / 2;
-    const bool turns = 8 * c < a.rot, first = 8 * c < half;
-    const int mate = a.halves && turns ? (first ? half : -half) : 0;
+    // the thread's dims from d0, and, BOTH, from d1 on; else d1 is the partner of d0
+    bool turns = 8 * c < (BOTH ? half : a.rot), first = true;
+    int d0 = 8 * c, d1 = 8 * c + half;
+    if (BOTH) {
+        if (!turns) d0 += half, d1 = d0 + D / 2 - half;
+    } else {
+        first = 8 * c < half;
+        d1 = !turns || !a.halves ? d0 : first ? d0 + half : d0 - half;
+    }
     const int step = gridDim.y * kRowsAt, slot0 = blockIdx.y * kRowsAt + r;
     const uint16_t *kb = (const uint16_t *)a.k + s * a.k_str[0] + t * a.k_str[1], *vb = (const uint16_t *)a.v + s * a.v_str[0] + t * a.v_str[1],
                    *qb = (const uint16_t *)a.q + s * a.q_str[0] + t * a.q_str[1];
     const int64_t kh = a.k_str[2], vh = a.v_str[2], qh = a.q_str[2];
-    u32x4 own[U], other[U];
-    int row[U], page[U];
+    const int32_t *lens = a.lens + (int64_t)s * a.H, *table = a.table + (int64_t)s * a.H * a.max_pages;
     const int pos = a.positions ? a.positions[tok] : 0;
-    if (slot0 < slots) load_slots<U>(own, other, row, page, slot0, step, slots, kb, vb, qb, kh, vh, qh, a.H, a.Hq, 8 * c, mate, a.lens + (int64_t)s * a.H, a.table + (int64_t)s * a.H * a.max_pages, a.max_pages, t - a.n_new);
     if (pos < 0 || (a.rot > 0 && pos >= a.n_positions)) return;
     double co[8], si[8];
     if (turns) {
         const float *cs = a.rope + (int64_t)pos * a.rot, *sn = cs + half;
-        if (a.halves) {
+        if (BOTH || a.halves) {
             const int e = first ? 8 * c : 8 * c - half;
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
@@ -115,31 +114,38 @@ template <int D, bool F16, bool FP4> __global__ __launch_bounds__(256) void appe
             }
         }
     }
-    for (int from = slot0; from < slots;) {
+    auto put = [&](int slot, int page_id, int page_row, int dim, const float (&x)[8], const u32x4 &w) {
+        if (slot >= 2 * a.H) *reinterpret_cast<u32x4 *>((uint16_t *)a.q_out + ((int64_t)tok * a.Hq + slot - 2 * a.H) * D + dim) = w;
+        else if (page_id >= 0 && page_id < a.n_pages)
+            store_row<D, F16, FP4>(a.pool + (int64_t)page_id * (FP4 ? Fp4Page<D>::kBytes : WidePage<D>::kBytes), slot < a.H, page_row & (kRows - 1), dim / 8, x, w);
+    };
+    for (int slot = slot0; slot < slots; slot += step) {
+        const Slot at = load_slot(slot, kb, vb, qb, kh, vh, qh, a.H, d0, d1, lens, table, a.max_pages, t - a.n_new);
+        const bool rotated = turns && (slot < a.H || slot >= 2 * a.H);
+        u32x4 w = at.a, v = at.b;
+        float x[8], y[8];
+        unpack8<F16>(w, x);
+        unpack8<F16>(v, y);
+        if (rotated) {
+            if constexpr (BOTH) {
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
-            const int slot = from + i * step;
-            if (slot >= slots) break;
-            const bool key = slot < a.H, value = !key && slot < 2 * a.H;
-            u32x4 w = own[i];
-            float x[8];
-            unpack8<F16>(w, x);
-            if (!value && turns) {
-                float y[8];
-                unpack8<F16>(other[i], y);
+                for (int k = 0; k < 8; ++k) {
+                    const double p = x[k], q = y[k];
+                    x[k] = rounded(fma(p, co[k], q * si[k]));
+                    y[k] = rounded(fma(q, co[k], p * -si[k]));
+                }
+                v = pack8<F16>(y);
+            } else {
                 if (!a.halves)
 #pragma unroll
                     for (int k = 0; k < 8; k += 2) y[k] = x[k + 1], y[k + 1] = x[k];
 #pragma unroll
                 for (int k = 0; k < 8; ++k) x[k] = rounded(fma((double)x[k], co[k], (double)y[k] * si[k]));
-                w = pack8<F16>(x);
             }
-            if (!key && !value) *reinterpret_cast<u32x4 *>((uint16_t *)a.q_out + ((int64_t)tok * a.Hq + slot - 2 * a.H) * D + 8 * c) = w;
-            else if (page[i] >= 0 && page[i] < a.n_pages)
-                store_row<D, F16, FP4>(a.pool + (int64_t)page[i] * (FP4 ? Fp4Page<D>::kBytes : WidePage<D>::kBytes), key, row[i] & (kRows - 1), c, x, w);
+            w = pack8<F16>(x);
         }
-        from += U * step;
-        if (from < slots) load_slots<U>(own, other, row, page, from, step, slots, kb, vb, qb, kh, vh, qh, a.H, a.Hq, 8 * c, mate, a.lens + (int64_t)s * a.H, a.table + (int64_t)s * a.H * a.max_pages, a.max_pages, t - a.n_new);
+        put(slot, at.page, at.row, d0, x, w);
+        if (BOTH) put(slot, at.page, at.row, d1, y, v);
     }
 }
 
@@ -263,14 +269,28 @@ hipError_t launch_pages_append(const nkv_tokens &t, const nkv_pages &p, hipStrea
     a.n_new = t.n_new, a.Hq = t.n_q_heads, a.rot = t.rot, a.halves = t.rope_style == NKV_ROPE_HALVES, a.n_positions = t.n_positions;
     a.H = p.H, a.n_pages = p.n_pages, a.max_pages = p.max_pages;
     a.table = p.table, a.lens = p.lens, a.pool = (uint8_t *)p.pool;
-    // Tokens enough to fill the chip: a workgroup takes all of a token's heads, and loads its angles once; fewer: a share of them.
     const int64_t tokens = (int64_t)p.n_seqs * t.n_new;
-    const int at_once = 256 / (p.d / 8), most = (2 * p.H + t.n_q_heads + at_once - 1) / at_once;
+    // both dims of a pair in a thread: where the four threads of a block of the 4-bit format still lie side by side
+    const bool both = t.rot > 0 && a.halves && t.rot % 64 == 0 && p.d % 64 == 0;
+    // Tokens enough to fill the chip: a workgroup takes all of a token's heads, and loads its angles once; fewer: a share of them.
+    const int at_once = 256 / (p.d / (both ? 16 : 8)), most = (2 * p.H + t.n_q_heads + at_once - 1) / at_once;
     const dim3 groups((unsigned)tokens, (unsigned)std::max<int64_t>(1, std::min<int64_t>(most, 2048 / tokens)));
     for_head_dim(p.d, [&](auto dim) {
         constexpr int D = decltype(dim)::value;
+        auto go = [&](auto f16, auto fp4) {
+            constexpr bool F16 = decltype(f16)::value, FP4 = decltype(fp4)::value;
+            if constexpr (D % 64 == 0) {
+                if (both) return append_kernel<D, F16, FP4, true><<<groups, 256, 0, st>>>(a);
+            }
+            append_kernel<D, F16, FP4, false><<<groups, 256, 0, st>>>(a);
+        };
+        using Yes = std::true_type;
+        using No = std::false_type;
         const bool f16 = p.dtype == NKV_DTYPE_F16, fp4 = p.format == NKV_PAGES_FP4;
-        (f16 ? fp4 ? append_kernel<D, true, true> : append_kernel<D, true, false> : fp4 ? append_kernel<D, false, true> : append_kernel<D, false, false>)<<<groups, 256, 0, st>>>(a);
+        if (f16 && fp4) go(Yes{}, Yes{});
+        else if (f16) go(Yes{}, No{});
+        else if (fp4) go(No{}, Yes{});
+        else go(No{}, No{});
     });
     return hipGetLastError();
 }
