@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from dataclasses import dataclass
 from typing import Optional, Sequence, Tuple
 
@@ -72,6 +73,8 @@ class nkv_tokens(C.Structure):
 
 
 _TOKENS_SIZE = C.sizeof(nkv_tokens)
+_TOKENS = struct.Struct("Iiiiii4P9q2P")        # nkv_tokens' fields in their order, packed in half the time of a ctypes structure
+assert _TOKENS.size == _TOKENS_SIZE
 
 
 class NkvError(RuntimeError):
@@ -115,7 +118,7 @@ def lib() -> C.CDLL:
                                            C.c_int32, f64, vp, vp, vp, C.c_size_t, vp]
         L.nkv_page_bytes.argtypes = [C.c_int32, C.c_int32, C.c_int32]
         L.nkv_page_bytes.restype = i64
-        L.nkv_pages_append.argtypes = [C.POINTER(nkv_tokens), C.POINTER(nkv_pages), vp]
+        L.nkv_pages_append.argtypes = [vp, C.POINTER(nkv_pages), vp]           # nkv_tokens *, by a structure or its bytes
         L.nkv_pages_load.argtypes = [vp, vp, vp, i64, C.POINTER(nkv_pages), vp]
         L.nkv_pages_read.argtypes = [vp, vp, vp, i64, C.POINTER(nkv_pages), vp]
         L.nkv_pages_workspace_bytes.argtypes = [C.POINTER(nkv_pages), C.c_int32, C.c_int32, C.POINTER(C.c_size_t)]
@@ -364,9 +367,6 @@ def _check_rows(t, what: str, pages: Pages, shape=None) -> None:
         raise ValueError(f"{what} is dense {list(shape)}")
 
 
-_Strides = C.c_int64 * 3
-
-
 def _strides(t, what: str, pages: Pages, shape):
     """Strides of a new token's rows [n_seqs, n, heads, d] (0 along a dim of one); their type and shape are checked."""
     if t.dtype is not pages.torch_dtype or t.shape != shape:
@@ -374,7 +374,7 @@ def _strides(t, what: str, pages: Pages, shape):
     s, n, h, e = t.stride()
     if e != 1:
         raise ValueError(f"{what}: a row's dims lie next to each other")
-    return _Strides(s if shape[0] > 1 else 0, n if shape[1] > 1 else 0, h if shape[2] > 1 else 0)
+    return s if shape[0] > 1 else 0, n if shape[1] > 1 else 0, h if shape[2] > 1 else 0
 
 
 def pages_append(k, v, pages: Pages, positions=None, rope=None, rope_style: int = ROPE_HALVES, q=None, q_out=None,
@@ -385,7 +385,7 @@ def pages_append(k, v, pages: Pages, positions=None, rope=None, rope_style: int 
     S, n, d = pages.n_seqs, k.shape[1], pages.d
     shape = (S, n, pages.H, d)
     ks, vs = _strides(k, "k", pages, shape), _strides(v, "v", pages, shape)
-    Hq, qs, q_at, out_at = 0, _Strides(), 0, 0
+    Hq, qs, q_at, out_at = 0, (0, 0, 0), 0, 0
     if q is not None:
         if q_out is None:
             raise ValueError("q and q_out are given together")
@@ -404,9 +404,9 @@ def pages_append(k, v, pages: Pages, positions=None, rope=None, rope_style: int 
         if positions.dtype is not pages.torch_i32 or positions.numel() != S * n or not positions.is_contiguous():
             raise ValueError("positions is int32 [n_seqs, n], contiguous")
         pos_at = positions.data_ptr()
-    tokens = nkv_tokens(_TOKENS_SIZE, n, Hq, rot, rope_style, n_positions, k.data_ptr(), v.data_ptr(), q_at, out_at,
-                        ks, vs, qs, pos_at, rope_at)
-    rc = lib().nkv_pages_append(C.byref(tokens), pages.ref, _stream(stream))
+    tokens = _TOKENS.pack(_TOKENS_SIZE, n, Hq, rot, rope_style, n_positions, k.data_ptr(), v.data_ptr(), q_at, out_at,
+                          *ks, *vs, *qs, pos_at, rope_at)
+    rc = lib().nkv_pages_append(tokens, pages.ref, _stream(stream))
     if rc:
         raise NkvError(rc, "nkv_pages_append")
 
