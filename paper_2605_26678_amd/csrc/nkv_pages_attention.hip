@@ -382,7 +382,8 @@ struct Parts {
         return i < front ? x + i : i < front + (b - a) ? kWaves * (a + i - front) : kWaves * b + (i - front - (b - a));
     }
 };
-// All units' pages in n stretches, the first `rem` one page longer than the others.  (Rounded up alike, 37 440 pages for 3072 wavefronts took 2880 of them.)
+// All units' pages in n stretches, the first `rem` one page longer than the others.  (All of the rounded-up length left up to one wavefront in sixteen
+// without pages where the stretches are short: twelve or thirteen pages each.)
 struct Cut {
     uint32_t base, rem;
     __device__ Cut() {}
