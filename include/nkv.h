@@ -325,6 +325,8 @@ int nkv_decode_attention(const void *q, const void *packed_k, const void *packed
  *                      V scales [4][d / 32][4][4], of row 16 t + 4 g + i at [g][block][t][i]
  * Rows of d = 64, 96, 128, 192 or 256 dims (K and V alike) of bf16 or fp16; others are refused with NKV_EUNSUPPORTED.
  * Inputs must be finite, as everywhere; rows behind a unit's last one may hold anything.
+ * What one launch cannot hold is refused with NKV_ESHAPE: from 2^24 tokens of an append or output rows of the attention on, and
+ * from 2^31 / d pages of packed rows on.
  */
 #define NKV_PAGE_ROWS 64
 enum { NKV_PAGES_16BIT = 0, NKV_PAGES_FP4 = 1 };

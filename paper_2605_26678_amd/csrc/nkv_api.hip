@@ -255,6 +255,9 @@ int prepare_budget(const float *scores, const nkv_shape *shape, const nkv_params
     return NKV_OK;
 }
 
+// A launch has less than 2^32 threads along x.
+bool one_launch(int64_t groups, int threads) { return groups < ((1ll << 32) + threads - 1) / threads; }
+
 int check_pages(const nkv_pages *p)
 {
     if (!p || p->struct_size != sizeof(nkv_pages)) return NKV_EINVAL;
@@ -273,7 +276,7 @@ int check_packed(const void *k, const void *v, const int64_t *head_off, int64_t 
     const int rc = check_pages(pages);
     if (rc) return rc;
     if (!head_off || rows < 0 || (rows > 0 && (!k || !v)) || (uintptr_t)k % 16 || (uintptr_t)v % 16 || (uintptr_t)head_off % 8) return NKV_EINVAL;
-    if (rows / NKV_PAGE_ROWS + 2 * (int64_t)pages->n_seqs * pages->H >= (1ll << 31)) return NKV_ESHAPE;
+    if (!one_launch(rows / NKV_PAGE_ROWS + 2 * (int64_t)pages->n_seqs * pages->H, 2 * pages->d)) return NKV_ESHAPE;   // a workgroup for a page
     return NKV_OK;
 }
 
@@ -282,9 +285,9 @@ int check_attention(const nkv_pages *pages, int32_t n_q_heads, int32_t n_new)
     const int rc = check_pages(pages);
     if (rc) return rc;
     if (n_new < 1 || n_q_heads < pages->H || n_q_heads % pages->H) return NKV_EINVAL;
-    // a workgroup for every output row, at most 65535 groups of 16 of a unit's
+    // a workgroup of 256 for every output row, at most 65535 groups of 16 of a unit's
     const int64_t cols = (int64_t)n_q_heads / pages->H * n_new;
-    if (cols > 16 * 65535 || (int64_t)pages->n_seqs * pages->H * cols >= (1ll << 31)) return NKV_ESHAPE;
+    if (cols > 16 * 65535 || !one_launch((int64_t)pages->n_seqs * pages->H * cols, 256)) return NKV_ESHAPE;
     return NKV_OK;
 }
 
@@ -563,8 +566,8 @@ int nkv_pages_append(const nkv_tokens *tokens, const nkv_pages *pages, void *hip
     }
     if ((uintptr_t)t.positions % 4 || (uintptr_t)t.rope % 16) return NKV_EINVAL;
     if (t.n_q_heads > 0 && t.q == t.q_out) return NKV_EINVAL;       // a pair's dims are read by two threads
-    // a workgroup for a token, numbered in 32 bits
-    if ((int64_t)pages->n_seqs * t.n_new >= (1ll << 31) || t.n_q_heads > (1 << 24))
+    // a workgroup of 256 for a token
+    if (!one_launch((int64_t)pages->n_seqs * t.n_new, 256) || t.n_q_heads > (1 << 24))
         return NKV_ESHAPE;
     return launch_pages_append(t, *pages, (hipStream_t)hip_stream) == hipSuccess ? NKV_OK : NKV_EHIP;
 }

@@ -80,6 +80,23 @@ def test_the_other_calls_refuse_bad_arguments():
         assert L.nkv_pages_attention(FAKE, C.byref(p), 8, 1, 1.0, FAKE, 0, ws, size, 0) == nkv.NKV_EWORKSPACE
 
 
+def test_calls_that_one_launch_cannot_hold_are_refused():
+    # a launch has less than 2^32 threads along x: 256 a token of an append and an output row of the attention, 2 d a page of packed rows
+    L, n, top = nkv.lib(), C.c_size_t(0), 1 << 24
+    for n_seqs, n_new in ((1, top), (2, top // 2), (top // 8, 8)):
+        assert L.nkv_pages_append(C.byref(_tokens(n_new=n_new)), C.byref(_pages(n_seqs=n_seqs, H=1, max_pages=1)), 0) == nkv.NKV_ESHAPE
+    for d in (64, 96, 128, 192, 256):
+        pages = -(-(1 << 32) // (2 * d))
+        p = _pages(n_seqs=1, H=1, d=d)
+        for call in (L.nkv_pages_load, L.nkv_pages_read):
+            assert call(FAKE, FAKE, FAKE, (pages - 2) * nkv.PAGE_ROWS, C.byref(p), 0) == nkv.NKV_ESHAPE
+    for n_seqs, heads, new, status in ((1 << 15, 32, 16, nkv.NKV_ESHAPE), (1 << 15, 32, 15, 0), (1 << 18, 64, 1, nkv.NKV_ESHAPE), ((1 << 18) - 1, 64, 1, 0)):
+        p = _pages(n_seqs=n_seqs, H=32, max_pages=1)
+        assert L.nkv_pages_workspace_bytes(C.byref(p), heads, new, C.byref(n)) == status
+        if status:
+            assert L.nkv_pages_attention(FAKE, C.byref(p), heads, new, 1.0, FAKE, 0, FAKE, 1 << 50, 0) == status
+
+
 def test_binding_refuses_what_the_library_cannot_see():
     z = lambda *s, dt=torch.bfloat16: torch.zeros(*s, dtype=dt)  # noqa: E731
     table, lens = z(2, 3, dt=torch.int32), z(2, dt=torch.int32)
