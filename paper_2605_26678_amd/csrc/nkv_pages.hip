@@ -270,8 +270,9 @@ hipError_t launch_pages_append(const nkv_tokens &t, const nkv_pages &p, hipStrea
     a.H = p.H, a.n_pages = p.n_pages, a.max_pages = p.max_pages;
     a.table = p.table, a.lens = p.lens, a.pool = (uint8_t *)p.pool;
     const int64_t tokens = (int64_t)p.n_seqs * t.n_new;
-    // both dims of a pair in a thread: where the four threads of a block of the 4-bit format still lie side by side
-    const bool both = t.rot > 0 && a.halves && t.rot % 64 == 0 && p.d % 64 == 0;
+    // Both dims of a pair in a thread; in 4 bits where the four threads of a block still lie side by side.  (3 x 2731 tokens of 16 bits, 32 of 128 dims rotated:
+    // 39.8 us, and 42.9 with eight dims a thread.  Neighbouring dims as pairs, or no rotation: eight a thread 37.6 and 34.6 us, sixteen 39.3 and 35.8.)
+    const bool both = t.rot > 0 && a.halves && (p.format != NKV_PAGES_FP4 || (t.rot % 64 == 0 && p.d % 64 == 0));
     // Tokens enough to fill the chip: a workgroup takes all of a token's heads, and loads its angles once; fewer: a share of them.
     const int at_once = 256 / (p.d / (both ? 16 : 8)), most = (2 * p.H + t.n_q_heads + at_once - 1) / at_once;
     const dim3 groups((unsigned)tokens, (unsigned)std::max<int64_t>(1, std::min<int64_t>(most, 2048 / tokens)));
@@ -279,7 +280,7 @@ hipError_t launch_pages_append(const nkv_tokens &t, const nkv_pages &p, hipStrea
         constexpr int D = decltype(dim)::value;
         auto go = [&](auto f16, auto fp4) {
             constexpr bool F16 = decltype(f16)::value, FP4 = decltype(fp4)::value;
-            if constexpr (D % 64 == 0) {
+            if constexpr (!FP4 || D % 64 == 0) {
                 if (both) return append_kernel<D, F16, FP4, true><<<groups, 256, 0, st>>>(a);
             }
             append_kernel<D, F16, FP4, false><<<groups, 256, 0, st>>>(a);
