@@ -102,9 +102,9 @@ template <bool F16> __device__ __forceinline__ u32x4 fp4_rows(uint32_t w, uint32
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const uint32_t code = w >> (4 * i) & 15u, sign = (code & 8u) << 12;
-            // magnitudes as 2^(e) * 1 or 1.5, e relative to the scale
+            // magnitudes but 0 as 2^e * 1 or 1.5: the codes 1, 2 .. 7 are 2^-1, 2^0 .. 1.5 * 2^2 times the scale
             const int e = (int)scale - 127 + (int)((code & 7u) >> 1) - 1;
-            const bool beyond = (code & 7u) >= 2u && e > (F16 ? 15 : 127);
+            const bool beyond = (code & 7u) != 0u && e > (F16 ? 15 : 127);
             const uint32_t h = scale == 255u ? 0x7fffu : sign | most;
             if (scale == 255u || beyond) r[i / 2] = i % 2 ? (r[i / 2] & 0xffffu) | h << 16 : (r[i / 2] & 0xffff0000u) | h;
         }

@@ -214,6 +214,59 @@ def test_every_code_with_every_scale_reads_as_its_value(dtype):
         assert torch.equal(got.cpu().nan_to_num(7.0)[scales >= 1], want.nan_to_num(7.0)[scales >= 1])   # (0 is no scale that is written)
 
 
+def _bits(t):
+    """A 16-bit tensor's bits, of NaN all the same (and not those of an infinity, which is no largest finite value)."""
+    return torch.where(t.isnan(), torch.full_like(t, float("nan")), t).cpu().contiguous().view(torch.int16)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_values_beyond_the_type_read_as_its_largest_finite_one(dtype):
+    """All 16 codes under all scale bytes that are written (1 .. 255), as K and as V, compared as bits: no infinity comes out.  The smallest magnitude, 0.5,
+    is beyond fp16 from scale byte 144 on."""
+    c = Cache(1, 1, 64, dtype, "fp4", [256], seed=30)
+    codes = np.tile(np.arange(16, dtype=np.uint8), 4)
+    k, v, ks, vs = op.places(64)
+    scales = np.maximum(np.arange(256), 1).astype(np.uint8)
+    for row in range(256):
+        page, r = c.pool[c.table[0, row // 64]], row % 64
+        for at in (k, v):
+            page[at[r, 0::2]] = codes[0::2] | codes[1::2] << 4
+        page[ks[r]], page[vs[r]] = scales[row], scales[255 - row]
+    off = torch.tensor([0, 256], device=DEV)
+    back = [torch.empty(256, 64, dtype=c.torch_dtype, device=DEV) for _ in range(2)]
+    nkv.pages_read(back[0], back[1], off, 256, c.on(DEV))
+    top = torch.finfo(c.torch_dtype).max
+    for got, s in zip(back, (scales, scales[::-1])):
+        exact = op.values(np.tile(codes, (256, 1)), np.repeat(s[:, None], 2, 1))
+        want = torch.from_numpy(np.clip(exact, -top, top)).to(c.torch_dtype)
+        differ = (_bits(got) != _bits(want)).nonzero()
+        assert differ.numel() == 0, [(int(s[r]), int(codes[d]), float(got[r, d]), float(want[r, d])) for r, d in differ[:6].tolist()]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_the_types_extremes_go_into_4_bits_and_back(dtype):
+    """Blocks of the type's largest, smallest normal and subnormal values: the pool's bytes, and the rows' bits after a read."""
+    c = Cache(1, 1, 64, dtype, "fp4", [64], seed=31)
+    f = torch.finfo(c.torch_dtype)
+    x = torch.zeros(64, 64)
+    for i, m in enumerate((f.max, f.max / 2, f.tiny, f.tiny / 2, f.smallest_normal * 1.75, f.tiny * 0.75, f.tiny * 0.53125, f.tiny / 4, f.tiny * 7)):
+        part = torch.tensor([1.0, 0.875, 0.75, 0.625, 0.5, 0.375, 0.3125, 0.25, 0.1875, 0.125, 0.0625, 0.0])
+        x[i, :12], x[i, 16:28], x[i, 32:44] = m * part, -m * part, m * part.flip(0)
+    rows = x.to(c.torch_dtype)
+    pages, off = c.on(DEV), torch.tensor([0, 64], device=DEV)
+    nkv.pages_load(rows.to(DEV), rows.flip(0).contiguous().to(DEV), off, 64, pages)
+    torch.cuda.synchronize()
+    want, y = c.pool.copy(), _f64(rows)
+    for r in range(64):
+        op.write_row(want[c.table[0, 0]], r, True, y[r], True, None)
+        op.write_row(want[c.table[0, 0]], r, False, y[63 - r], True, None)
+    assert np.array_equal(c.d_pool.cpu().numpy(), want)
+    k, v = torch.empty_like(rows, device=DEV), torch.empty_like(rows, device=DEV)
+    nkv.pages_read(k, v, off, 64, pages)
+    for got, exact in zip((k, v), op.read_rows(want[c.table[0, 0]], 64, True, None)):
+        assert torch.equal(_bits(got), _bits(torch.from_numpy(np.clip(exact, -f.max, f.max)).to(c.torch_dtype)))
+
+
 @pytest.mark.parametrize("d", [64, 96, 128, 192, 256])
 @pytest.mark.parametrize("fmt,dtype", [("fp4", "bf16"), ("fp4", "fp16"), ("16bit", "bf16")])
 @pytest.mark.parametrize("behind", [0, 37])
