@@ -367,6 +367,12 @@ def _check_rows(t, what: str, pages: Pages, shape=None) -> None:
         raise ValueError(f"{what} is dense {list(shape)}")
 
 
+def _check_dense(t, what: str, dtype, numbers: int) -> None:
+    """A buffer that a call indexes by itself: its type, that it is contiguous, and how much it holds."""
+    if t.dtype is not dtype or not t.is_contiguous() or t.numel() < numbers:
+        raise ValueError(f"{what} is contiguous {dtype} of {numbers} numbers, not {t.dtype} {list(t.shape)} by strides {list(t.stride())}")
+
+
 def _strides(t, what: str, pages: Pages, shape):
     """Strides of a new token's rows [n_seqs, n, heads, d] (0 along a dim of one); their type and shape are checked."""
     if t.dtype is not pages.torch_dtype or t.shape != shape:
@@ -444,6 +450,12 @@ def pages_attention(q, pages: Pages, n_q_heads: int, n_new: int, scale: float, o
     """The last n_new tokens' attention over the pages: q [n_seqs, n_new, Hq, d] -> out fp32 of that shape (and lse
     [n_seqs, n_new, Hq]); see ``nkv_pages_attention`` in nkv.h."""
     _check_rows(q, "q", pages, (pages.n_seqs, n_new, n_q_heads, pages.d))
+    columns = pages.n_seqs * n_new * n_q_heads
+    _check_dense(out, "out", pages.torch_f32, columns * pages.d)
+    if lse is not None:
+        _check_dense(lse, "lse", pages.torch_f32, columns)
+    if ws is not None and not ws.is_contiguous():
+        raise ValueError("ws is contiguous")
     rc = lib().nkv_pages_attention(_ptr(q), pages.ref, int(n_q_heads), int(n_new), float(scale), _ptr(out),
                                    _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(),
                                    _stream(stream))

@@ -218,3 +218,23 @@ def test_paged_cache_hands_out_every_page_once():
     assert c.free_pages == 4 and len(set(c.table[c.table >= 0].tolist())) == 5
     with pytest.raises(nkv.NkvError):
         nkv.PagedCache(1, 1, 80, nkv.DTYPE_BF16, nkv.PAGES_FP4, 1, 64, device="cpu")
+
+
+def _attention_args():
+    """An attention's arguments, on the CPU: good ones but for that, and nothing is launched where a ValueError comes first."""
+    c = nkv.PagedCache(2, 2, 64, nkv.DTYPE_BF16, nkv.PAGES_FP4, n_pages=4, max_rows=64, device="cpu")
+    q = torch.zeros(2, 3, 4, 64, dtype=torch.bfloat16)
+    return dict(q=q, pages=c.pages, n_q_heads=4, n_new=3, scale=1.0, out=torch.zeros(2, 3, 4, 64), lse=torch.zeros(2, 3, 4),
+                ws=torch.zeros(1 << 16, dtype=torch.uint8), stream=0)
+
+
+@pytest.mark.parametrize("bad", [
+    dict(out=torch.zeros(2, 3, 4, 64, dtype=torch.bfloat16)),             # fp32 rows are twice as long
+    dict(out=torch.zeros(2, 3, 4, 64, dtype=torch.float64)), dict(out=torch.zeros(2, 3, 4, 32)), dict(out=torch.zeros(2, 3, 2, 64)),
+    dict(out=torch.zeros(3, 2, 4, 64).transpose(0, 1)), dict(out=torch.zeros(2, 3, 4, 128)[..., ::2]),
+    dict(lse=torch.zeros(2, 3, 4, dtype=torch.bfloat16)), dict(lse=torch.zeros(2, 3)), dict(lse=torch.zeros(2, 3, 8)[..., ::2]),
+    dict(ws=torch.zeros(4, 1 << 16, dtype=torch.uint8)[:, ::2]),          # counted as larger than the piece that it begins
+], ids=lambda b: str({k: (tuple(t.shape), t.dtype, t.stride()) for k, t in b.items()}))
+def test_binding_refuses_outputs_that_an_attention_would_write_beside(bad):
+    with pytest.raises(ValueError, match=next(iter(bad))):
+        nkv.pages_attention(**{**_attention_args(), **bad})
