@@ -335,7 +335,7 @@ class Pages:
             raise ValueError("pool, table and lens are contiguous")
         self.pool, self.table, self.lens = pool, table, lens
         self.n_seqs, self.H, self.d, self.dtype, self.format = int(n_seqs), int(H), int(d), int(dtype), int(format)
-        self.torch_dtype, self.torch_f32, self.torch_i32 = _torch_dtype(dtype), torch.float32, torch.int32
+        self.torch_dtype, self.torch_f32, self.torch_i32, self.torch_i64 = _torch_dtype(dtype), torch.float32, torch.int32, torch.int64
         self.c = nkv_pages(C.sizeof(nkv_pages), int(n_seqs), int(H), int(d), int(dtype), int(format), nbytes // size,
                            int(table.shape[1]), _ptr(pool), _ptr(table), _ptr(lens))
         self.ref = C.byref(self.c)
@@ -359,11 +359,11 @@ def _torch_dtype(dtype: int):
     return {DTYPE_F32: torch.float32, DTYPE_BF16: torch.bfloat16, DTYPE_F16: torch.float16}.get(int(dtype))
 
 
-def _check_rows(t, what: str, pages: Pages, shape=None) -> None:
-    """Rows that a call reads or writes: their type, and, where their shape is given, that and that they are dense."""
+def _check_rows(t, what: str, pages: Pages, shape) -> None:
+    """Rows that a call reads or writes: their type, their shape, and that they are dense."""
     if t.dtype is not pages.torch_dtype:
         raise ValueError(f"{what} is {t.dtype}, and the pages' rows are {pages.torch_dtype}")
-    if shape is not None and (t.shape != shape or not t.is_contiguous()):
+    if t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{what} is dense {list(shape)}")
 
 
@@ -417,10 +417,15 @@ def pages_append(k, v, pages: Pages, positions=None, rope=None, rope_style: int 
         raise NkvError(rc, "nkv_pages_append")
 
 
+def _check_packed(packed_k, packed_v, head_off, rows: int, pages: Pages) -> None:
+    _check_dense(packed_k, "packed_k", pages.torch_dtype, rows * pages.d)
+    _check_dense(packed_v, "packed_v", pages.torch_dtype, rows * pages.d)
+    _check_dense(head_off, "head_off", pages.torch_i64, pages.n_seqs * pages.H + 1)
+
+
 def pages_load(packed_k, packed_v, head_off, rows: int, pages: Pages, stream=None) -> None:
     """Packed rows [rows, d] (as ``select_compact`` leaves them) to the end of every unit's pages."""
-    _check_rows(packed_k, "packed_k", pages)
-    _check_rows(packed_v, "packed_v", pages)
+    _check_packed(packed_k, packed_v, head_off, rows, pages)
     rc = lib().nkv_pages_load(_ptr(packed_k), _ptr(packed_v), _ptr(head_off), int(rows), pages.ref,
                               _stream(stream))
     if rc:
@@ -429,8 +434,7 @@ def pages_load(packed_k, packed_v, head_off, rows: int, pages: Pages, stream=Non
 
 def pages_read(packed_k, packed_v, head_off, rows: int, pages: Pages, stream=None) -> None:
     """The last head_off[u + 1] - head_off[u] rows of every unit to packed rows [rows, d]."""
-    _check_rows(packed_k, "packed_k", pages)
-    _check_rows(packed_v, "packed_v", pages)
+    _check_packed(packed_k, packed_v, head_off, rows, pages)
     rc = lib().nkv_pages_read(_ptr(packed_k), _ptr(packed_v), _ptr(head_off), int(rows), pages.ref,
                               _stream(stream))
     if rc:

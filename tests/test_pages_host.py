@@ -238,3 +238,19 @@ def _attention_args():
 def test_binding_refuses_outputs_that_an_attention_would_write_beside(bad):
     with pytest.raises(ValueError, match=next(iter(bad))):
         nkv.pages_attention(**{**_attention_args(), **bad})
+
+
+@pytest.mark.parametrize("call", [nkv.pages_load, nkv.pages_read], ids=["load", "read"])
+@pytest.mark.parametrize("bad", [
+    dict(head_off=torch.zeros(5, dtype=torch.int32)),                     # half as long as what is read
+    dict(head_off=torch.zeros(4, dtype=torch.int64)), dict(head_off=torch.zeros(10, dtype=torch.int64)[::2]),
+    dict(packed_k=torch.zeros(9, 64, dtype=torch.bfloat16)), dict(packed_v=torch.zeros(10, 32, dtype=torch.bfloat16)),
+    dict(packed_v=torch.zeros(10, 128, dtype=torch.bfloat16)[:, :64]), dict(packed_k=torch.zeros(64, 10, dtype=torch.bfloat16).T),
+    dict(packed_k=torch.zeros(10, 64)),
+], ids=lambda b: str({k: (tuple(t.shape), t.dtype, t.stride()) for k, t in b.items()}))
+def test_binding_refuses_packed_rows_that_a_call_would_leave(call, bad):
+    c = nkv.PagedCache(2, 2, 64, nkv.DTYPE_BF16, nkv.PAGES_FP4, n_pages=4, max_rows=64, device="cpu")
+    rows = torch.zeros(10, 64, dtype=torch.bfloat16)
+    good = dict(packed_k=rows, packed_v=rows.clone(), head_off=torch.zeros(5, dtype=torch.int64), rows=10, pages=c.pages, stream=0)
+    with pytest.raises(ValueError, match=next(iter(bad))):
+        call(**{**good, **bad})
