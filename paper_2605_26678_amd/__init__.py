@@ -333,8 +333,12 @@ class Pages:
             raise ValueError("table is int32 [n_seqs * H, max_pages], lens int32 [n_seqs * H], the pool a page or more")
         if not (pool.is_contiguous() and table.is_contiguous() and lens.is_contiguous()):
             raise ValueError("pool, table and lens are contiguous")
+        if not pool.device == table.device == lens.device:
+            raise ValueError("pool, table and lens are on one device")
         self.pool, self.table, self.lens = pool, table, lens
         self.n_seqs, self.H, self.d, self.dtype, self.format = int(n_seqs), int(H), int(d), int(dtype), int(format)
+        self.units = self.n_seqs * self.H
+        self.index = pool.get_device()                   # of the GPU; -1: the CPU
         self.torch_dtype, self.torch_f32, self.torch_i32, self.torch_i64 = _torch_dtype(dtype), torch.float32, torch.int32, torch.int64
         self.c = nkv_pages(C.sizeof(nkv_pages), int(n_seqs), int(H), int(d), int(dtype), int(format), nbytes // size,
                            int(table.shape[1]), _ptr(pool), _ptr(table), _ptr(lens))
@@ -359,27 +363,43 @@ def _torch_dtype(dtype: int):
     return {DTYPE_F32: torch.float32, DTYPE_BF16: torch.bfloat16, DTYPE_F16: torch.float16}.get(int(dtype))
 
 
+def _elsewhere(t, what: str, pages: Pages) -> ValueError:
+    return ValueError(f"{what} is on device {t.device}, and the pages are on {pages.pool.device}")
+
+
+def _check_gpu(pages: Pages) -> None:
+    """What ends a call's checks: tensors are where the pages are, and those are not on the CPU."""
+    if pages.index < 0:
+        raise ValueError("the pages are not on a GPU")
+
+
 def _check_rows(t, what: str, pages: Pages, shape) -> None:
     """Rows that a call reads or writes: their type, their shape, and that they are dense."""
     if t.dtype is not pages.torch_dtype:
         raise ValueError(f"{what} is {t.dtype}, and the pages' rows are {pages.torch_dtype}")
     if t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{what} is dense {list(shape)}")
+    if t.get_device() != pages.index:
+        raise _elsewhere(t, what, pages)
 
 
-def _check_dense(t, what: str, dtype, numbers: int) -> None:
+def _check_dense(t, what: str, pages: Pages, dtype, numbers: int) -> None:
     """A buffer that a call indexes by itself: its type, that it is contiguous, and how much it holds."""
     if t.dtype is not dtype or not t.is_contiguous() or t.numel() < numbers:
         raise ValueError(f"{what} is contiguous {dtype} of {numbers} numbers, not {t.dtype} {list(t.shape)} by strides {list(t.stride())}")
+    if t.get_device() != pages.index:
+        raise _elsewhere(t, what, pages)
 
 
-def _strides(t, what: str, pages: Pages, shape):
-    """Strides of a new token's rows [n_seqs, n, heads, d] (0 along a dim of one); their type and shape are checked."""
-    if t.dtype is not pages.torch_dtype or t.shape != shape:
-        raise ValueError(f"{what} is {pages.torch_dtype} {list(shape)}, not {t.dtype} {list(t.shape)}")
+def _strides(t, what: str, pages: Pages, given, shape):
+    """Strides of a new token's rows [n_seqs, n, heads, d] (0 along a dim of one); their type, shape (`given`) and device are checked."""
+    if t.dtype is not pages.torch_dtype or given != shape:
+        raise ValueError(f"{what} is {pages.torch_dtype} {list(shape)}, not {t.dtype} {list(given)}")
     s, n, h, e = t.stride()
     if e != 1:
         raise ValueError(f"{what}: a row's dims lie next to each other")
+    if t.get_device() != pages.index:
+        raise _elsewhere(t, what, pages)
     return s if shape[0] > 1 else 0, n if shape[1] > 1 else 0, h if shape[2] > 1 else 0
 
 
@@ -388,28 +408,36 @@ def pages_append(k, v, pages: Pages, positions=None, rope=None, rope_style: int 
     """New tokens' k, v [n_seqs, n, H, d] (any strides but the last dim's) to the last n rows of the pages, k rotated
     by ``rope`` [n_positions, 2, rot / 2] at ``positions`` int32 [n_seqs, n] on the way; q [n_seqs, n, Hq, d] rotated
     into q_out; see ``nkv_pages_append`` in nkv.h."""
-    S, n, d = pages.n_seqs, k.shape[1], pages.d
+    given = k.shape                                      # (a tensor's shape, device or type is some 0.1 us of a call's 7 each time)
+    S, n, d = pages.n_seqs, given[1], pages.d
     shape = (S, n, pages.H, d)
-    ks, vs = _strides(k, "k", pages, shape), _strides(v, "v", pages, shape)
+    ks, vs = _strides(k, "k", pages, given, shape), _strides(v, "v", pages, v.shape, shape)
     Hq, qs, q_at, out_at = 0, (0, 0, 0), 0, 0
     if q is not None:
         if q_out is None:
             raise ValueError("q and q_out are given together")
-        Hq = q.shape[2]
+        given = q.shape
+        Hq = given[2]
         shape = (S, n, Hq, d)
-        qs, q_at, out_at = _strides(q, "q", pages, shape), q.data_ptr(), q_out.data_ptr()
+        qs, q_at, out_at = _strides(q, "q", pages, given, shape), q.data_ptr(), q_out.data_ptr()
         _check_rows(q_out, "q_out", pages, shape)
     elif q_out is not None:
         raise ValueError("q and q_out are given together")
     rot = n_positions = rope_at = pos_at = 0
     if rope is not None:
-        if rope.dtype is not pages.torch_f32 or rope.dim() != 3 or rope.shape[1] != 2 or not rope.is_contiguous():
+        given = rope.shape
+        if rope.dtype is not pages.torch_f32 or len(given) != 3 or given[1] != 2 or not rope.is_contiguous():
             raise ValueError("rope is fp32 [n_positions, 2, rot / 2], contiguous")
-        rot, n_positions, rope_at = 2 * rope.shape[2], rope.shape[0], rope.data_ptr()
+        if rope.get_device() != pages.index:
+            raise _elsewhere(rope, "rope", pages)
+        rot, n_positions, rope_at = 2 * given[2], given[0], rope.data_ptr()
     if positions is not None:
         if positions.dtype is not pages.torch_i32 or positions.numel() != S * n or not positions.is_contiguous():
             raise ValueError("positions is int32 [n_seqs, n], contiguous")
+        if positions.get_device() != pages.index:
+            raise _elsewhere(positions, "positions", pages)
         pos_at = positions.data_ptr()
+    _check_gpu(pages)
     tokens = _TOKENS.pack(_TOKENS_SIZE, n, Hq, rot, rope_style, n_positions, k.data_ptr(), v.data_ptr(), q_at, out_at,
                           *ks, *vs, *qs, pos_at, rope_at)
     rc = lib().nkv_pages_append(tokens, pages.ref, _stream(stream))
@@ -418,25 +446,32 @@ def pages_append(k, v, pages: Pages, positions=None, rope=None, rope_style: int 
 
 
 def _check_packed(packed_k, packed_v, head_off, rows: int, pages: Pages) -> None:
-    _check_dense(packed_k, "packed_k", pages.torch_dtype, rows * pages.d)
-    _check_dense(packed_v, "packed_v", pages.torch_dtype, rows * pages.d)
-    _check_dense(head_off, "head_off", pages.torch_i64, pages.n_seqs * pages.H + 1)
+    at, dtype, numbers = pages.index, pages.torch_dtype, rows * pages.d
+    if packed_k.dtype is dtype and packed_k.is_contiguous() and packed_k.numel() >= numbers and packed_k.get_device() == at and \
+            packed_v.dtype is dtype and packed_v.is_contiguous() and packed_v.numel() >= numbers and packed_v.get_device() == at and \
+            head_off.dtype is pages.torch_i64 and head_off.is_contiguous() and head_off.numel() > pages.units and \
+            head_off.get_device() == at >= 0:
+        return                                           # (the same one after the other takes a microsecond more)
+    _check_dense(packed_k, "packed_k", pages, dtype, numbers)
+    _check_dense(packed_v, "packed_v", pages, dtype, numbers)
+    _check_dense(head_off, "head_off", pages, pages.torch_i64, pages.units + 1)
+    _check_gpu(pages)
 
 
 def pages_load(packed_k, packed_v, head_off, rows: int, pages: Pages, stream=None) -> None:
     """Packed rows [rows, d] (as ``select_compact`` leaves them) to the end of every unit's pages."""
+    rows = int(rows)
     _check_packed(packed_k, packed_v, head_off, rows, pages)
-    rc = lib().nkv_pages_load(_ptr(packed_k), _ptr(packed_v), _ptr(head_off), int(rows), pages.ref,
-                              _stream(stream))
+    rc = lib().nkv_pages_load(packed_k.data_ptr(), packed_v.data_ptr(), head_off.data_ptr(), rows, pages.ref, _stream(stream))
     if rc:
         raise NkvError(rc, "nkv_pages_load")
 
 
 def pages_read(packed_k, packed_v, head_off, rows: int, pages: Pages, stream=None) -> None:
     """The last head_off[u + 1] - head_off[u] rows of every unit to packed rows [rows, d]."""
+    rows = int(rows)
     _check_packed(packed_k, packed_v, head_off, rows, pages)
-    rc = lib().nkv_pages_read(_ptr(packed_k), _ptr(packed_v), _ptr(head_off), int(rows), pages.ref,
-                              _stream(stream))
+    rc = lib().nkv_pages_read(packed_k.data_ptr(), packed_v.data_ptr(), head_off.data_ptr(), rows, pages.ref, _stream(stream))
     if rc:
         raise NkvError(rc, "nkv_pages_read")
 
@@ -455,14 +490,19 @@ def pages_attention(q, pages: Pages, n_q_heads: int, n_new: int, scale: float, o
     [n_seqs, n_new, Hq]); see ``nkv_pages_attention`` in nkv.h."""
     _check_rows(q, "q", pages, (pages.n_seqs, n_new, n_q_heads, pages.d))
     columns = pages.n_seqs * n_new * n_q_heads
-    _check_dense(out, "out", pages.torch_f32, columns * pages.d)
+    _check_dense(out, "out", pages, pages.torch_f32, columns * pages.d)
     if lse is not None:
-        _check_dense(lse, "lse", pages.torch_f32, columns)
-    if ws is not None and not ws.is_contiguous():
-        raise ValueError("ws is contiguous")
-    rc = lib().nkv_pages_attention(_ptr(q), pages.ref, int(n_q_heads), int(n_new), float(scale), _ptr(out),
-                                   _ptr(lse), _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(),
-                                   _stream(stream))
+        _check_dense(lse, "lse", pages, pages.torch_f32, columns)
+    ws_at = ws_bytes = 0
+    if ws is not None:
+        if not ws.is_contiguous():
+            raise ValueError("ws is contiguous")
+        if ws.get_device() != pages.index:
+            raise _elsewhere(ws, "ws", pages)
+        ws_at, ws_bytes = ws.data_ptr(), ws.nbytes
+    _check_gpu(pages)
+    rc = lib().nkv_pages_attention(q.data_ptr(), pages.ref, int(n_q_heads), int(n_new), float(scale), out.data_ptr(),
+                                   0 if lse is None else lse.data_ptr(), ws_at, ws_bytes, _stream(stream))
     if rc:
         raise NkvError(rc, "nkv_pages_attention")
 

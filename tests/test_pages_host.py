@@ -254,3 +254,26 @@ def test_binding_refuses_packed_rows_that_a_call_would_leave(call, bad):
     good = dict(packed_k=rows, packed_v=rows.clone(), head_off=torch.zeros(5, dtype=torch.int64), rows=10, pages=c.pages, stream=0)
     with pytest.raises(ValueError, match=next(iter(bad))):
         call(**{**good, **bad})
+
+
+def test_binding_refuses_tensors_that_are_not_where_the_pages_are():
+    """A host address handed to a kernel faults the GPU.  (Pages on the CPU and a tensor that says it is on a GPU stand for the two places.)"""
+    class OnGpu(torch.Tensor):
+        def get_device(self):
+            return 0
+    c = nkv.PagedCache(2, 2, 64, nkv.DTYPE_BF16, nkv.PAGES_FP4, n_pages=4, max_rows=64, device="cpu")
+    for other in ("pool", "table", "lens"):
+        with pytest.raises(ValueError, match="device"):
+            nkv.Pages(2, 2, 64, nkv.DTYPE_BF16, nkv.PAGES_FP4, **{**dict(pool=c.pool, table=c.table, lens=c.lens), other: getattr(c, other).to("meta")})
+    row = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)  # noqa: E731
+    append = dict(k=row(2, 3, 2, 64), v=row(2, 3, 2, 64), positions=torch.zeros(2, 3, dtype=torch.int32), rope=torch.zeros(9, 2, 32), q=row(2, 3, 4, 64),
+                  q_out=row(2, 3, 4, 64))
+    packed = dict(packed_k=row(10, 64), packed_v=row(10, 64), head_off=torch.zeros(5, dtype=torch.int64))
+    attend = {x: y for x, y in _attention_args().items() if isinstance(y, torch.Tensor)}
+    for call, tensors, rest in ((nkv.pages_append, append, {}), (nkv.pages_load, packed, dict(rows=10)), (nkv.pages_read, packed, dict(rows=10)),
+                                (nkv.pages_attention, attend, dict(n_q_heads=4, n_new=3, scale=1.0))):
+        for name in tensors:
+            with pytest.raises(ValueError, match=f"{name}.*device"):
+                call(**{**tensors, **rest, name: tensors[name].as_subclass(OnGpu)}, pages=c.pages, stream=0)
+        with pytest.raises(ValueError, match="not on a GPU"):             # all of them in the same wrong place
+            call(**tensors, **rest, pages=c.pages, stream=0)
