@@ -656,6 +656,8 @@ class PagedCache:
 
     def release(self, seq: int) -> None:
         """Gives a sequence's pages back; its lengths become 0."""
+        if not 0 <= seq < self.n_seqs:
+            raise IndexError(f"sequence {seq} of {self.n_seqs}")
         for u in range(seq * self.H, (seq + 1) * self.H):
             self._free.extend(reversed(self._held[u]))
             self._held[u] = []

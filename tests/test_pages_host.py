@@ -277,3 +277,17 @@ def test_binding_refuses_tensors_that_are_not_where_the_pages_are():
                 call(**{**tensors, **rest, name: tensors[name].as_subclass(OnGpu)}, pages=c.pages, stream=0)
         with pytest.raises(ValueError, match="not on a GPU"):             # all of them in the same wrong place
             call(**tensors, **rest, pages=c.pages, stream=0)
+
+
+@pytest.mark.parametrize("seq", [-1, -2, 2, 7])
+def test_release_refuses_what_is_no_sequence(seq):
+    """(-1 would give the last sequence's pages back and leave its lengths: rows on no page.)"""
+    c = nkv.PagedCache(2, 2, 64, nkv.DTYPE_BF16, nkv.PAGES_FP4, n_pages=9, max_rows=200, device="cpu")
+    c.reserve([1, 1, 70, 70])
+    c.lens.copy_(torch.tensor([1, 1, 70, 70]))
+    before = c.table.clone()
+    with pytest.raises(IndexError):
+        c.release(seq)
+    assert c.free_pages == 3 and torch.equal(c.table, before) and c.lens.tolist() == [1, 1, 70, 70]
+    c.release(1)
+    assert c.free_pages == 7 and c.lens.tolist() == [1, 1, 0, 0] and c.table[:2].tolist() == before[:2].tolist() and bool((c.table[2:] == -1).all())
