@@ -5,7 +5,7 @@
 
 For every prompt and layer: Compressor (score, budgets, selection) -> pages_load.  Then, token by token, each layer appends the
 new token's key and value, rotated by its position in the text, and attends over its pages; a step of all layers is one
-HIP graph.  There is no model: queries, keys and values are synthetic.  At the end the last step is compared with attention in
+HIP graph, and the cache is given more pages between steps as it grows.  There is no model: queries, keys and values are synthetic.  At the end the last step is compared with attention in
 64 bits over the pages' rows (pages_read), and the cache's size and a step's time are printed.
 """
 from __future__ import annotations
@@ -43,15 +43,12 @@ def main() -> int:
     r = comp.run(K, V)
     kept = (r.head_off[1:] - r.head_off[:-1]).cpu()
     room = [int(n) + args.tokens + 1 for n in kept]
-    cache = nkv.PagedCache(P * L, H, d, nkv.DTYPE_BF16, fmt, sum((n + 63) // 64 for n in room), max(room))
-    cache.reserve(room)
+    cache = nkv.PagedCache(P * L, H, d, nkv.DTYPE_BF16, fmt, sum((n + nkv.PAGE_ROWS - 1) // nkv.PAGE_ROWS for n in room), max(room))
+    cache.reserve(kept.tolist())
     cache.lens.copy_(kept.int())
     nkv.pages_load(r.packed_k, r.packed_v, r.head_off, comp.rows, cache.pages)
 
-    # one Pages a layer: layer l of prompt p is sequence p * L + l, so a layer's table and lengths are gathered once
-    table = cache.table.view(P, L, H, -1)
-    lens = cache.lens.view(P, L, H).transpose(0, 1).contiguous()              # [L, P, H], what the steps count in
-    layers = [nkv.Pages(P, H, d, nkv.DTYPE_BF16, fmt, cache.pool, table[:, l].reshape(P * H, -1).contiguous(), lens[l].reshape(-1)) for l in range(L)]
+    layers, lens = cache.layers(L), cache.layer_lens                          # one Pages a layer, and what the steps count in
 
     g = torch.Generator(device=dev).manual_seed(7)
     qkv = torch.randn(L, P, 1, Hq + 2 * H, d, device=dev, generator=g).to(bf16)
@@ -69,16 +66,27 @@ def main() -> int:
             nkv.pages_append(x[:, :, Hq:Hq + H], x[:, :, Hq + H:], layers[l], positions=positions, rope=rope, q=x[:, :, :Hq], q_out=q[l])
             nkv.pages_attention(q[l], layers[l], Hq, 1, scale, out[l], lse[l], ws)
 
+    done = 0
+
+    def grow():                                                               # every 32 tokens, pages for 32 more
+        nonlocal done
+        if done % 32 == 0:
+            cache.reserve([min(int(n) + done + 32, most) for n, most in zip(kept, room)])
+        done += 1
+
+    grow()
     step()                                                                    # once outside the capture
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         step()
     for _ in range(args.tokens // 2):
+        grow()
         graph.replay()
     start, stop = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
     start.record()
     timed = args.tokens - 1 - args.tokens // 2
     for _ in range(timed):
+        grow()
         qkv.mul_(-1)                                                          # another token
         graph.replay()
     stop.record()

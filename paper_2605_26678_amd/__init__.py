@@ -617,7 +617,9 @@ class Compressor:
 
 class PagedCache:
     """Owns a paged cache's pool, table and lengths and hands out its pages, on the host: ``pages`` is what the calls
-    take.  ``lens`` (device) is the program's to write; ``reserve`` only sees to it that there are pages."""
+    take.  ``lens`` (device) is the program's to write; ``reserve`` only sees to it that there are pages.  ``layers`` gives a
+    ``Pages`` for every layer where the sequences are (prompt, layer).  ``reserve`` and ``release`` write tables and lengths
+    where they lie, so recorded graphs go by them, in the current stream's order: that of the calls on the pages."""
 
     def __init__(self, n_seqs: int, H: int, d: int, dtype: int, format: int, n_pages: int, max_rows: int,
                  device="cuda:0"):
@@ -633,6 +635,26 @@ class PagedCache:
         self.pages = Pages(n_seqs, H, d, dtype, format, self.pool, self.table, self.lens)
         self._free = list(range(int(n_pages) - 1, -1, -1))
         self._held = [[] for _ in range(n_seqs * H)]
+        self._layers, self.layer_table, self.layer_lens = [], None, None
+
+    def layers(self, n_layers: int) -> list:
+        """A ``Pages`` for every layer, for calls layer by layer; sequence p * n_layers + l is prompt p in layer l, as the
+        units of a pass over several layers are numbered.  A layer's units do not lie side by side in ``table`` and ``lens``, so
+        the layers have copies: ``layer_table`` [n_layers, prompts * H, ...], which follows ``table``, and ``layer_lens``
+        [n_layers, prompts * H], which begins as ``lens`` is at the first call and is the program's to write from then on, beside
+        ``lens``, by which ``pages`` goes (``release`` clears both)."""
+        if n_layers < 1 or self.n_seqs % n_layers or self._layers and len(self._layers) != n_layers:
+            raise ValueError(f"{self.n_seqs} sequences in {n_layers} layers, the same number at every call")
+        if not self._layers:
+            self.layer_table, self.layer_lens = self._by_layer(self.table, n_layers), self._by_layer(self.lens, n_layers)
+            p = self.pages
+            self._layers = [Pages(self.n_seqs // n_layers, p.H, p.d, p.dtype, p.format, self.pool, t, n)
+                            for t, n in zip(self.layer_table, self.layer_lens)]
+        return list(self._layers)
+
+    def _by_layer(self, x, n_layers: int):
+        """[(prompt, layer, head), ...] as a copy [layer, (prompt, head), ...]."""
+        return x.unflatten(0, (self.n_seqs // n_layers, n_layers, self.H)).transpose(0, 1).flatten(1, 2).clone()
 
     @property
     def free_pages(self) -> int:
@@ -662,6 +684,9 @@ class PagedCache:
             self._free.extend(reversed(self._held[u]))
             self._held[u] = []
         self.lens[seq * self.H:(seq + 1) * self.H] = 0
+        if self._layers:
+            p, l = divmod(seq, len(self._layers))
+            self.layer_lens[l, p * self.H:(p + 1) * self.H] = 0
         self._write()
 
     def _write(self) -> None:
@@ -670,3 +695,5 @@ class PagedCache:
         for u, h in enumerate(self._held):
             host[u, :len(h)] = torch.tensor(h, dtype=torch.int32)
         self.table.copy_(host)
+        if self._layers:
+            self.layer_table.copy_(self._by_layer(host, len(self._layers)))

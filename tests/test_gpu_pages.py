@@ -569,6 +569,96 @@ def test_the_compressors_rows_through_pages(fmt):
 
 
 @pytest.mark.parametrize("fmt", ["fp4", "16bit"])
+def test_a_cache_that_grows_and_gives_back_while_it_decodes_layer_by_layer(fmt):
+    """Steps of all layers in one graph.  Pages are reserved as units fill theirs; in the middle a prompt is released, its pages go to the others, and another
+    prompt comes into its place.  After every step each layer's output is that of the rows appended so far, by the oracle."""
+    P, L, H, G, d, steps = 3, 2, 2, 2, 64, 12
+    Hq, scale = G * H, d ** -0.5
+    c = nkv.PagedCache(P * L, H, d, nkv.DTYPE_BF16, nkv.PAGES_FP4 if fmt == "fp4" else nkv.PAGES_16BIT, n_pages=27, max_rows=200, device=DEV)
+    lens = [60, 61, 125, 58, 3, 64, 62, 63, 1, 120, 59, 57]
+    assert len(lens) == P * L * H
+    g = torch.Generator().manual_seed(5)
+
+    def fill(units, n):                                     # packed rows into those units' pages
+        off = np.concatenate([[0], np.cumsum([n[u] if u in units else 0 for u in range(P * L * H)])])
+        k, v = (torch.randn(int(off[-1]), d, generator=g).to(torch.bfloat16) for _ in range(2))
+        c.lens.copy_(torch.tensor(n, dtype=torch.int32))
+        nkv.pages_load(k.to(DEV), v.to(DEV), torch.from_numpy(off).to(DEV), int(off[-1]), c.pages)
+
+    c.reserve(lens)
+    fill(range(P * L * H), lens)
+    layers = c.layers(L)
+    qkv = torch.empty(L, P, 1, Hq + 2 * H, d, dtype=torch.bfloat16, device=DEV)
+    q = torch.empty(L, P, 1, Hq, d, dtype=torch.bfloat16, device=DEV)
+    out, lse = torch.empty(L, P, 1, Hq, d, device=DEV), torch.empty(L, P, 1, Hq, device=DEV)
+    rope, positions = nkv.rope_table(400, d, device=DEV), torch.tensor([[70], [80], [90]], dtype=torch.int32, device=DEV)
+    alive = torch.ones(P * H, dtype=torch.int32, device=DEV)
+    ws = torch.empty(nkv.pages_workspace_bytes(layers[0], Hq), dtype=torch.uint8, device=DEV)
+
+    def step():
+        c.layer_lens.add_(alive)
+        positions.add_(1)
+        for l in range(L):
+            x = qkv[l]
+            nkv.pages_append(x[:, :, Hq:Hq + H], x[:, :, Hq + H:], layers[l], positions=positions, rope=rope, q=x[:, :, :Hq], q_out=q[l])
+            nkv.pages_attention(q[l], layers[l], Hq, 1, scale, out[l], lse[l], ws)
+
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step()
+    lens, live = np.array(lens), np.ones(P * L * H, int)
+    bits, halves = to_bits(torch.bfloat16), True
+    for t in range(steps):
+        if t == 5:                                          # prompt 1 ends
+            for l in range(L):
+                c.release(1 * L + l)
+            alive.view(P, H)[1] = 0
+            positions[1] = -1000
+            live.reshape(P, L, H)[1], lens.reshape(P, L, H)[1] = 0, 0
+        if t == 8:                                          # another one in its place
+            n = lens.copy()
+            n.reshape(P, L, H)[1] = [[30, 70], [64, 1]]
+            c.reserve(n.tolist())
+            fill([u for u in range(P * L * H) if u // H // L == 1], n.tolist())
+            c.layer_lens.view(L, P, H)[:, 1] = torch.from_numpy(n.reshape(P, L, H)[1]).int().to(DEV)
+            alive.view(P, H)[1] = 1
+            positions[1] = 100
+            lens, live = n, np.ones(P * L * H, int)
+        lens = lens + live
+        c.reserve(lens.tolist())
+        x = torch.randn(L, P, 1, Hq + 2 * H, d, generator=g).to(torch.bfloat16)
+        qkv.copy_(x)
+        pos = positions.cpu().numpy() + 1
+        before = c.pool.cpu().numpy()
+        table = c.table.cpu().numpy()
+        held = table[table >= 0]
+        assert len(set(held.tolist())) == held.size         # every page is one unit's
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(c.layer_lens.cpu().view(L, P, H), torch.from_numpy(lens).int().view(P, L, H).transpose(0, 1)), t
+        for l in range(L):
+            f = _f64(x[l])
+            turned = op.rotate(f[:, :, :Hq + H], pos, rope.cpu().numpy(), halves)
+            for u in np.flatnonzero(live.reshape(P, L, H)[:, l].reshape(-1)):
+                p, h = divmod(int(u), H)
+                unit = (p * L + l) * H + h
+                row = int(lens[unit]) - 1
+                page = before[table[unit, row // 64]]
+                op.write_row(page, row % 64, True, turned[p, 0, Hq + h], fmt == "fp4", bits)
+                op.write_row(page, row % 64, False, f[p, 0, Hq + H + h], fmt == "fp4", bits)
+            of = table.reshape(P, L, H, -1)[:, l].reshape(P * H, -1)
+            n = lens.reshape(P, L, H)[:, l].reshape(-1)
+            seen = from_bits(torch.bfloat16)(bits(turned[:, :, :Hq]).reshape(-1)).reshape(P, 1, Hq, d)
+            want, want_lse = op.attention(seen, before, of, n, H, scale, d, fmt == "fp4", from_bits(torch.bfloat16))
+            assert np.abs(_f64(out[l]) - want).max() <= TOL * 6, (t, l)
+            assert np.array_equal(np.isneginf(_f64(lse[l])), np.isneginf(want_lse)), (t, l)
+        assert np.array_equal(c.pool.cpu().numpy(), before), t
+
+
+@pytest.mark.parametrize("fmt", ["fp4", "16bit"])
 def test_the_example_runs(fmt, monkeypatch, capsys):
     import importlib.util
     import os

@@ -291,3 +291,48 @@ def test_release_refuses_what_is_no_sequence(seq):
     assert c.free_pages == 3 and torch.equal(c.table, before) and c.lens.tolist() == [1, 1, 70, 70]
     c.release(1)
     assert c.free_pages == 7 and c.lens.tolist() == [1, 1, 0, 0] and c.table[:2].tolist() == before[:2].tolist() and bool((c.table[2:] == -1).all())
+
+
+def test_layers_of_a_paged_cache_follow_what_is_reserved_and_released():
+    """Sequences (prompt, layer): every layer's table and lengths, where they lie, hold what the owner's do after each step."""
+    P, L, H = 3, 2, 2
+    c = nkv.PagedCache(P * L, H, 64, nkv.DTYPE_BF16, nkv.PAGES_FP4, n_pages=40, max_rows=200, device="cpu")
+    start = torch.arange(P * L * H, dtype=torch.int32) * 5
+    c.lens.copy_(start)
+    c.reserve(start.tolist())
+    layers = c.layers(L)
+    where = [(x.table.data_ptr(), x.lens.data_ptr()) for x in layers]
+
+    def in_line():
+        for l, x in enumerate(layers):
+            assert (x.n_seqs, x.H, x.c.table, x.c.lens) == (P, H, *where[l]) and x.c.pool == c.pool.data_ptr()
+            assert torch.equal(x.table, c.table.view(P, L, H, -1)[:, l].reshape(P * H, -1))
+            assert (x.table.data_ptr(), x.lens.data_ptr()) == where[l]
+
+    in_line()
+    assert torch.equal(c.layer_lens, start.view(P, L, H).transpose(0, 1).reshape(L, P * H))
+    c.layer_lens.add_(1)
+    assert [x.lens.tolist() for x in layers] == c.layer_lens.tolist()
+    c.reserve([130] * (P * L * H))
+    in_line()
+    c.release(2 * L + 1)                                                    # the last prompt in layer 1
+    in_line()
+    want = (start.view(P, L, H).transpose(0, 1) + 1).clone()
+    want[1, 2] = 0
+    assert torch.equal(c.layer_lens.view(L, P, H), want) and c.lens.view(P, L, H)[2, 1].tolist() == [0, 0]
+    c.reserve([0] * (P * L - 1) * H + [64] * H)
+    in_line()
+    assert c.layers(L) == layers and torch.equal(c.layer_lens.view(L, P, H), want)   # the same ones
+    for bad in (0, 4, L + 1):
+        with pytest.raises(ValueError):
+            c.layers(bad)
+
+
+def test_layers_of_one_prompt_have_lengths_of_their_own():
+    c = nkv.PagedCache(3, 2, 64, nkv.DTYPE_BF16, nkv.PAGES_FP4, n_pages=12, max_rows=100, device="cpu")
+    c.reserve([60] * 6)
+    layers = c.layers(3)
+    c.layer_lens.add_(1)
+    assert c.lens.tolist() == [0] * 6 and [x.lens.tolist() for x in layers] == [[1, 1]] * 3
+    c.reserve([70] * 6)
+    assert torch.equal(c.layer_table.flatten(0, 1), c.table) and bool((c.table >= 0).all())
