@@ -395,7 +395,7 @@ int nkv_pages_read(void *packed_k, void *packed_v, const int64_t *head_off, int6
  *   out[s][t][h*G+g] = sum_i softmax(scale * <q[s][t][h*G+g], k_i>)_i * v_i        fp32 [n_seqs][n_new][n_q_heads][d]
  *   lse[s][t][h*G+g] = log sum_i exp(scale * <q, k_i>)   (optional, may be NULL)   fp32 [n_seqs][n_new][n_q_heads]
  * q is dense [n_seqs][n_new][n_q_heads][d] in `dtype` (q_out of nkv_pages_append).  A token that sees no row gets out = 0,
- * lse = -inf.  Products are exact and added up in fp32; keys and values of 4-bit pages enter as the values they stand for.
+ * lse = -inf.  scale may be negative, zero or subnormal; NKV_EINVAL where scale * log2(e) is not finite in fp32.  Products are exact and added up in fp32; keys and values of 4-bit pages enter as the values they stand for.
  * Scratch: nkv_pages_workspace_bytes.  A call is deterministic.
  */
 int nkv_pages_workspace_bytes(const nkv_pages *pages, int32_t n_q_heads, int32_t n_new, size_t *bytes);

@@ -601,7 +601,7 @@ int nkv_pages_attention(const void *q, const nkv_pages *pages, int32_t n_q_heads
 {
     int rc = check_attention(pages, n_q_heads, n_new);
     if (rc) return rc;
-    if (!q || !out || !isfinite(scale)) return NKV_EINVAL;
+    if (!q || !out || !isfinite(pages_scale(scale))) return NKV_EINVAL;
     if ((uintptr_t)q % 16 || (uintptr_t)out % 16 || (uintptr_t)lse % 4) return NKV_EINVAL;
     rc = check_ws(ws, ws_bytes, pages_ws_bytes(*pages, n_q_heads, n_new));
     if (rc) return rc;

@@ -171,6 +171,8 @@ inline int64_t page_bytes_of(int d, int format) { return format == NKV_PAGES_FP4
 hipError_t launch_pages_append(const nkv_tokens &t, const nkv_pages &p, hipStream_t st);
 hipError_t launch_pages_rows(bool load, const void *k, const void *v, const int64_t *head_off, int64_t rows, const nkv_pages &p,
                              hipStream_t st);
+// A scale's magnitude as the kernels take it, for powers of two
+inline float pages_scale(double scale) { return (float)(fabs(scale) * 1.4426950408889634); }
 size_t pages_ws_bytes(const nkv_pages &p, int n_q_heads, int n_new);
 hipError_t launch_pages_attention(const void *q, const nkv_pages &p, int n_q_heads, int n_new, double scale, float *out, float *lse,
                                   void *ws, hipStream_t st);

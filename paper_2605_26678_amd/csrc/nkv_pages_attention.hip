@@ -44,8 +44,9 @@ struct AttendArgs {
     const uint8_t *pool;
     const int32_t *table, *lens;
     int32_t n_units, H, G, n_new, n_pages, max_pages;
-    float scale_log2;                    // positive
+    float scale_log2;                    // positive, subnormal or not: rows that are not seen have the product -inf
     uint32_t flip;                       // sign bits of the query that change
+    bool flat;                           // a scale of zero (in 32 bits): the query counts as zeros
     Parts *plan;                         // per unit
     float *part;                         // [part][column][D + 4]: weighted values, maximum, sum
 };
@@ -575,7 +576,7 @@ template <int D, bool F16, bool FP4, int COLS> __global__ __launch_bounds__(kThr
         const int len = clamp_len(a.lens[u], a.max_pages), sq = u / a.H, h = u - sq * a.H;
         const int32_t *table = a.table + (int64_t)u * a.max_pages;
         const uint32_t left = (uint32_t)(len + kRows - 1) / kRows - step, end = i < hi ? step + min(hi - i, left) : step;
-        if (i < hi) load_query<D, F16, FP4>(q, a.q + (((int64_t)sq * a.n_new + token) * a.H * a.G + h * a.G + head) * D, there, a.flip, g);
+        if (i < hi) load_query<D, F16, FP4>(q, a.q + (((int64_t)sq * a.n_new + token) * a.H * a.G + h * a.G + head) * D, there && !a.flat, a.flip, g);
         i += end - step;
         auto id_of = [&](uint32_t at) { return at < end ? table[at] : -1; };
         auto page_of = [&](int id) { return a.pool + (int64_t)(id >= 0 && id < a.n_pages ? id : 0) * kBytes; };
@@ -725,7 +726,9 @@ hipError_t launch_pages_attention(const void *q, const nkv_pages &p, int n_q_hea
     AttendArgs a{};
     a.q = (const uint16_t *)q, a.pool = (const uint8_t *)p.pool, a.table = p.table, a.lens = p.lens;
     a.n_units = p.n_seqs * p.H, a.H = p.H, a.G = n_q_heads / p.H, a.n_new = n_new, a.n_pages = p.n_pages, a.max_pages = p.max_pages;
-    a.scale_log2 = std::max((float)(fabs(scale) * 1.4426950408889634), 0x1p-100f);   // (not 0: rows that are not seen have the product -inf)
+    a.scale_log2 = pages_scale(scale);
+    a.flat = a.scale_log2 == 0.f;
+    if (a.flat) a.scale_log2 = 1.f;
     a.flip = scale < 0 ? 0x80008000u : 0u;
     a.plan = (Parts *)ws;
     a.part = (float *)((char *)ws + plan_bytes(p));

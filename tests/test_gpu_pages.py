@@ -448,6 +448,31 @@ def test_queries_of_very_different_sizes(fmt):
     _check(c, q, o, l, 0.2, fmt, 1)
 
 
+def _times_power_of_two(c, key, e):
+    """The K (or V) rows of all units times 2^e."""
+    k, v, ks, vs = op.places(c.d)
+    for u, n in enumerate(c.lens):
+        for j in range((int(n) + 63) // 64):
+            page, m = c.pool[c.table[u, j]], min(64, int(n) - 64 * j)
+            if c.fp4:
+                page[(ks if key else vs)[:m]] += np.uint8(e)
+            else:
+                w = page.view(np.uint16).reshape(2, 64, c.d)[0 if key else 1]
+                w[:m] = to_bits(c.torch_dtype)(from_bits(c.torch_dtype)(w[:m].reshape(-1)) * 2.0 ** e).reshape(m, c.d)
+
+
+@pytest.mark.parametrize("fmt,dtype", [("fp4", "bf16"), ("fp4", "fp16"), ("16bit", "bf16")])
+@pytest.mark.parametrize("up,scale", [(56, 0.0), (56, 0.09 * 2.0 ** -113), (56, -0.09 * 2.0 ** -113), (59, 0.09 * 2.0 ** -119), (59, 0.09 * 2.0 ** -128), (59, 2.0 ** -160)])
+def test_scales_far_below_one_beside_large_products(fmt, dtype, up, scale):
+    """Logits of ordinary size from products of up to 2^125, also by a scale that is subnormal in fp32, and a scale (zero, or as good as) by which all rows weigh the same."""
+    c = Cache(2, 2, 128, dtype, fmt, [200, 33, 64, 1], rows=1.0, seed=24)
+    up_q = up if dtype == "bf16" else 8
+    _times_power_of_two(c, True, up + 1 + (up - up_q))
+    q = (_queries(c, 1, 8, 15).double() * 2.0 ** up_q).to(c.torch_dtype)
+    o, l = _attend(c, q, scale, 1, 8)
+    _check(c, q, o, l, scale, str((up, scale)), 1)
+
+
 def test_units_may_share_pages():
     c = Cache(4, 1, 64, "bf16", "fp4", [130, 100, 64, 130], rows=1.0, seed=19)
     c.table[1:] = c.table[0]

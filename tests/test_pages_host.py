@@ -336,3 +336,10 @@ def test_layers_of_one_prompt_have_lengths_of_their_own():
     assert c.lens.tolist() == [0] * 6 and [x.lens.tolist() for x in layers] == [[1, 1]] * 3
     c.reserve([70] * 6)
     assert torch.equal(c.layer_table.flatten(0, 1), c.table) and bool((c.table >= 0).all())
+
+
+def test_attention_refuses_a_scale_that_is_infinite_in_32_bits():
+    L, p, n = nkv.lib(), _pages(), C.c_size_t(0)
+    assert L.nkv_pages_workspace_bytes(C.byref(p), 8, 1, C.byref(n)) == 0
+    for scale in (3e38, -3e38, 1e39, -1e300, float("inf")):                # times log2(e)
+        assert L.nkv_pages_attention(FAKE, C.byref(p), 8, 1, scale, FAKE, 0, FAKE, n.value, 0) == nkv.NKV_EINVAL
