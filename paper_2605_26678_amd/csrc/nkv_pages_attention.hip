@@ -33,6 +33,10 @@ constexpr int kThreads = 256, kWaves = kThreads / 64;
 // Workgroups that a compute unit holds at once, by the registers that a head dim takes, and no more than that are launched.
 __host__ __device__ constexpr int groups_at_once(int D) { return D == 64 ? 4 : D <= 128 ? 3 : 2; }
 constexpr float kNone = -3.0e38f;        // running maximum before any row was seen
+// A column's maximum is a rounded product with the scale, and its rows' logits are not rounded before they are taken from it: all of its weights are 2^(half of the
+// maximum's last place) off at most, which their sum takes out again.  From here on that place is 2 or more, and weights could leave their type's range: logits are rounded
+// alike, so that the largest weight is 1.
+constexpr float kFar = 0x1p24f;
 constexpr float kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ int clamp_len(int len, int max_pages) { return max(0, min(len, max_pages * kRows)); }
@@ -286,7 +290,8 @@ __device__ __forceinline__ void accumulate(State<D, F16, FP4, COLS> &st, const R
         top = fmaxf(top, p[i]);
     }
     top *= scale_log2;                                                     // (positive, see load_query)
-    if (__any(top > st.m)) {                                               // seldom after a unit's first steps
+    bool far = false;
+    if (__any(top > st.m || fabsf(st.m) >= kFar)) {                        // seldom after a unit's first steps
         auto larger = [](float a, float b) { return fmaxf(a, b); };
         top = swap_reduce<32>(swap_reduce<16>(top, larger), larger);
         const float m = fmaxf(top, st.m), f0 = __builtin_amdgcn_exp2f(st.m - m);
@@ -298,10 +303,16 @@ __device__ __forceinline__ void accumulate(State<D, F16, FP4, COLS> &st, const R
         for (int t = 0; t < Q::C; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i) st.o[t][i] *= f0;
-    }
-    const float base = Q::kShift - st.m;
+        far = __any(fabsf(m) >= kFar);
+        if (far) {
+#pragma clang fp contract(off)
 #pragma unroll
-    for (int i = 0; i < 4 * Q::kTiles; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(p[i], scale_log2, base));
+            for (int i = 0; i < 4 * Q::kTiles; ++i) p[i] = p[i] * scale_log2 - m;
+        }
+    }
+    const float base = Q::kShift - (far ? 0.f : st.m), factor = far ? 1.f : scale_log2;
+#pragma unroll
+    for (int i = 0; i < 4 * Q::kTiles; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(p[i], factor, base));
     // dims 2 k and 2 k + 1 of row 16 t + 4 g + i, next to each other
     auto values = [&](int t, int i, int k) {
         const int at = i * (Q::C / 2) + k;

@@ -473,6 +473,34 @@ def test_scales_far_below_one_beside_large_products(fmt, dtype, up, scale):
     _check(c, q, o, l, scale, str((up, scale)), 1)
 
 
+@pytest.mark.parametrize("fmt,dtype,e_k,e_q", [("fp4", "bf16", 20, 18), ("fp4", "fp16", 30, 10), ("16bit", "bf16", 20, 18), ("16bit", "fp16", 11, 11)])
+@pytest.mark.parametrize("d,G", [(128, 4), (64, 8), (256, 3)])
+def test_logits_of_millions_give_the_largest_ones_row(fmt, dtype, e_k, e_q, d, G):
+    """Logits between which lie more than 2^20: the weight of all rows but one is 0 in any precision, and where a step of the logits in fp32 is more than a few units, so that
+    the running maximum is off by as much, weights stay finite all the same.  Rows are a_i times one vector of signs, with a_i = 6 in one row and up to 4 in the others."""
+    c = Cache(2, 2, d, dtype, fmt, [70, 300, 33, 129], rows=1.0, seed=25 + d)
+    g = torch.Generator().manual_seed(d)
+    signs = torch.where(torch.randn(d, generator=g) < 0, -1.0, 1.0).double().numpy()
+    best = []
+    for u, n in enumerate(c.lens):
+        a = np.array([1.0, 1.5, 2.0, 3.0, 4.0])[torch.randint(0, 5, (int(n),), generator=g).numpy()]
+        best.append(int(torch.randint(0, int(n), (1,), generator=g)))
+        a[best[u]] = 6.0
+        for i in range(int(n)):
+            op.write_row(c.pool[c.table[u, i // 64]], i % 64, True, a[i] * 2.0 ** e_k / 4 * signs, c.fp4, to_bits(c.torch_dtype))
+    # every query a size of its own, so that the logits' roundings differ
+    size = 1.0 + torch.randint(0, 64, (2, 1, 2 * G, 1), generator=g).double() / 64
+    q = (size * 2.0 ** e_q / 2 * torch.from_numpy(signs)).to(c.torch_dtype)
+    for scale in (d ** -0.5, 1.0):
+        o, l = _attend(c, q, scale, 1, 2 * G)
+        want, want_lse = op.attention(_f64(q), c.pool, c.table, c.lens, 2, scale, d, c.fp4, from_bits(c.torch_dtype))
+        assert want_lse.min() > 2.0 ** 20
+        assert np.isfinite(_f64(o)).all() and np.isfinite(_f64(l)).all()
+        # one row's values: the split of its weight is all that is rounded, and the sum that it is divided by
+        assert (np.abs(_f64(o) - want) <= 2.0 ** -20 * np.abs(want)).all()
+        assert np.abs(_f64(l) / want_lse - 1).max() <= TOL
+
+
 def test_units_may_share_pages():
     c = Cache(4, 1, 64, "bf16", "fp4", [130, 100, 64, 130], rows=1.0, seed=19)
     c.table[1:] = c.table[0]
