@@ -18,6 +18,19 @@ def from_bits(dtype):
     return lambda w: torch.from_numpy(np.ascontiguousarray(w).view(np.int16)).view(dtype).double().numpy()
 
 
+def attention_bar(v_max: float) -> float:
+    """What an attention's output may be off by at logits of a few: sums in fp32 of d products and of some hundred weighted values leave up to a third of it (plain
+    fp32 on the CPU over the tests' caches: 0.02 to 0.17 of it), and weights that lose their last 8 of 24 bits come out at 1.2 to 4 times it."""
+    return 2e-6 * max(1.0, v_max)
+
+
+def values_of(c):
+    """V rows of all units, fp64, one below the other."""
+    rows = [op.read_rows(c.pool[c.table[u, j]], c.d, c.fp4, from_bits(c.torch_dtype))[1][:min(64, int(n) - 64 * j)]
+            for u, n in enumerate(c.lens) for j in range((int(n) + 63) // 64)]
+    return np.concatenate(rows)
+
+
 class Cache:
     """A pool of pages for units of the given lengths (uint8 numpy), every unit's pages anywhere; the rows behind a unit's last
     one, and pages that nobody has, are all ones (NaN in either format).  Unused table entries are -1."""

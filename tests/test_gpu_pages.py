@@ -12,7 +12,7 @@ import torch
 from oracle import pages as op
 import nkv_inputs
 import paper_2605_26678_amd as nkv
-from pages_util import Cache, DTYPES, from_bits, to_bits
+from pages_util import Cache, DTYPES, attention_bar, from_bits, to_bits, values_of
 from parity_util import shape_of
 
 pytestmark = pytest.mark.gpu
@@ -367,6 +367,22 @@ def test_attention_groups_and_tokens(fmt, G, n):
     q = _queries(c, n, 3 * G, 5)
     o, l = _attend(c, q, 128 ** -0.5, n, 3 * G)
     _check(c, q, o, l, 128 ** -0.5, f"G={G} n={n}", n)
+
+
+@pytest.mark.parametrize("d", [64, 96, 128, 192, 256])
+@pytest.mark.parametrize("fmt", ["fp4", "16bit"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("G,n", [(1, 1), (4, 1), (5, 1), (3, 2), (8, 5)])
+def test_attention_keeps_every_bit_of_its_weights(d, fmt, dtype, G, n):
+    """The bar from the values that are there, at which a lost piece of the weights' split shows (tests/test_pages_host.py)."""
+    c = Cache(8, 2, d, dtype, fmt, EDGES, rows=1.0, seed=d + G)
+    q = _queries(c, n, 2 * G, 3)
+    o, l = _attend(c, q, d ** -0.5, n, 2 * G)
+    want, want_lse = op.attention(_f64(q), c.pool, c.table, c.lens, 2, d ** -0.5, d, c.fp4, from_bits(c.torch_dtype))
+    err, bar = np.abs(_f64(o) - want).max(), attention_bar(np.abs(values_of(c)).max())
+    assert err <= bar, f"out off by {err:.3e}, bar {bar:.3e}"
+    seen = np.isfinite(want_lse)
+    assert np.array_equal(np.isfinite(_f64(l)), seen) and np.abs(_f64(l)[seen] - want_lse[seen]).max() <= TOL
 
 
 @pytest.mark.parametrize("fmt,d,dtype", [("fp4", 128, "bf16"), ("16bit", 128, "bf16"), ("fp4", 64, "fp16"), ("16bit", 64, "fp16")])

@@ -343,3 +343,35 @@ def test_attention_refuses_a_scale_that_is_infinite_in_32_bits():
     assert L.nkv_pages_workspace_bytes(C.byref(p), 8, 1, C.byref(n)) == 0
     for scale in (3e38, -3e38, 1e39, -1e300, float("inf")):                # times log2(e)
         assert L.nkv_pages_attention(FAKE, C.byref(p), 8, 1, scale, FAKE, 0, FAKE, n.value, 0) == nkv.NKV_EINVAL
+
+
+@pytest.mark.parametrize("fmt,d,dtype", [("fp4", 64, "bf16"), ("fp4", 128, "fp16"), ("fp4", 256, "bf16"), ("16bit", 64, "fp16"), ("16bit", 128, "bf16"), ("16bit", 256, "bf16")])
+@pytest.mark.parametrize("G,n", [(1, 1), (4, 1), (3, 2)])
+def test_the_bar_of_an_attention_sees_a_lost_piece_of_its_weights(fmt, d, dtype, G, n):
+    """The caches and queries of the GPU's test, in 64 bits: weights cut off behind 16 bits, as if a third piece of 8 were lost, leave the bar; plain
+    fp32 stays well under it."""
+    from pages_util import Cache, attention_bar, from_bits, values_of
+    c = Cache(8, 2, d, dtype, fmt, [0, 1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 700], rows=1.0, seed=d + G)
+    g = torch.Generator().manual_seed(3)
+    q = torch.randn(c.S, n, 2 * G, d, generator=g).to(c.torch_dtype).double().numpy()
+    want, _ = op.attention(q, c.pool, c.table, c.lens, 2, d ** -0.5, d, c.fp4, from_bits(c.torch_dtype))
+    cut, f32 = np.zeros_like(want), np.zeros_like(want)
+    for u in range(16):
+        s, h = divmod(u, 2)
+        rows = [op.read_rows(c.pool[c.table[u, j]], d, c.fp4, from_bits(c.torch_dtype)) for j in range((int(c.lens[u]) + 63) // 64)]
+        for t in range(n):
+            see = int(c.lens[u]) - (n - 1 - t)
+            if see < 1:
+                continue
+            K, V = (np.concatenate([x[i] for x in rows])[:see] for i in range(2))
+            heads = slice(h * G, (h + 1) * G)
+            z = d ** -0.5 * (q[s, t, heads] @ K.T)
+            w = np.exp(z - z.max(-1, keepdims=True))
+            short = (w.astype(np.float32).view(np.uint32) & np.uint32(0xffffff00)).view(np.float32).astype(np.float64)
+            cut[s, t, heads] = (short / w.sum(-1, keepdims=True)) @ V
+            z = np.float32(d ** -0.5) * (q[s, t, heads].astype(np.float32) @ K.astype(np.float32).T)
+            w = np.exp(z - z.max(-1, keepdims=True))
+            f32[s, t, heads] = (w @ V.astype(np.float32)) / w.sum(-1, keepdims=True)
+    bar = attention_bar(np.abs(values_of(c)).max())
+    assert np.abs(cut - want).max() > bar
+    assert np.abs(f32 - want).max() < bar / 3
