@@ -148,6 +148,62 @@ def test_append_leaves_out_padding_foreign_positions_and_pages_that_are_none(fmt
     assert np.array_equal(_f64(q_out), want_q, equal_nan=True)
 
 
+@pytest.mark.parametrize("S,n,H,G,d,rot,halves,dtype,fmt", [
+    (2, 3, 32, 1, 96, 48, False, "fp16", "fp4"),          # 96 rows, 21 at a time: five workgroups a token, the last one partly filled
+    (2, 3, 8, 4, 256, 256, False, "bf16", "16bit"),       # 48 rows, 8 at a time: six workgroups a token
+    (3, 1, 8, 4, 256, 256, True, "bf16", "fp4"),          # 16 at a time: three
+    (1, 700, 8, 4, 256, 128, False, "bf16", "fp4"),       # two workgroups a token, three rounds each
+    (1, 900, 32, 1, 96, 96, True, "bf16", "16bit"),       # two workgroups, 42 rows at a time: the second one's last round is partly filled
+    (3, 701, 8, 4, 128, 128, True, "bf16", "fp4"),        # more than 2048 tokens: one workgroup each, 32 rows and 16 more
+    (3, 701, 8, 4, 128, 32, True, "fp16", "16bit"),
+    (1, 2113, 32, 2, 64, 16, False, "fp16", "fp4"),
+])
+def test_append_with_many_heads_and_tokens(S, n, H, G, d, rot, halves, dtype, fmt):
+    """A token's rows shared out to several workgroups, and more of them than a workgroup takes at a time: sampled tokens' rows of all heads against the oracle, and
+    the rows in front of the new ones as they were."""
+    Hq, held = H * G, 37
+    c = Cache(S, H, d, dtype, fmt, [held + n] * (S * H), rows=1.0, seed=n)
+    x, rope, positions = _append_case(c, n, Hq, rot, halves, 11 * n)
+    before = c.pool.copy()
+    got, q_out = _run_append(c, x, rope, positions, n, Hq, rot, halves)
+    f, q_out = _f64(x), _f64(q_out)
+    bits, back = to_bits(c.torch_dtype), from_bits(c.torch_dtype)
+    spread = sorted({0, 1, n // 3, n // 2, n - 2, n - 1} & set(range(n)))
+    for s in range(S):
+        for t in spread:
+            pos = positions[s:s + 1, t:t + 1].numpy()
+            turned = op.rotate(f[s:s + 1, t:t + 1, :Hq + H], pos, rope.numpy(), halves)[0, 0]
+            assert np.array_equal(q_out[s, t], back(bits(turned[:Hq]).reshape(-1)).reshape(Hq, d)), (s, t)
+            for h in range(H):
+                at, row = c.table[s * H + h, (held + t) // 64], (held + t) % 64
+                want = got[at].copy()
+                op.write_row(want, row, True, turned[Hq + h], c.fp4, bits)
+                op.write_row(want, row, False, f[s, t, Hq + H + h], c.fp4, bits)
+                assert np.array_equal(want, got[at]), (s, t, h)
+        for h in range(H):
+            for key_value in zip(*(op.read_rows(p[c.table[s * H + h, 0]], d, c.fp4, back) for p in (before, got))):
+                assert np.array_equal(key_value[0][:held], key_value[1][:held])
+    # no row was left out: none of the new ones is what was there
+    for u in range(S * H):
+        for j in range((held + n + 63) // 64):
+            old, new = (np.concatenate(op.read_rows(p[c.table[u, j]], d, c.fp4, back), -1) for p in (before, got))
+            lo, hi = max(held - 64 * j, 0), min(held + n - 64 * j, 64)
+            assert (old[lo:hi] != new[lo:hi]).any(-1).all(), (u, j)
+
+
+@pytest.mark.parametrize("d,rot", [(128, 32), (128, 16), (64, 16), (96, 32), (192, 64), (256, 48)])
+@pytest.mark.parametrize("fmt", ["fp4", "16bit"])
+@pytest.mark.parametrize("halves", [True, False])
+def test_append_rotates_a_part_of_a_row(d, rot, fmt, halves):
+    n, Hq = 4, 4
+    c = Cache(2, 2, d, "bf16", fmt, [4, 64, 66, 130], rows=1.0, seed=rot)
+    x, rope, positions = _append_case(c, n, Hq, rot, halves, 3 * d + rot)
+    want, want_q = _append_oracle(c, x, rope, positions, n, Hq, rot, halves)
+    got, q_out = _run_append(c, x, rope, positions, n, Hq, rot, halves)
+    assert np.array_equal(got, want), f"{(got != want).sum()} bytes differ"
+    assert np.array_equal(_f64(q_out), want_q)
+
+
 def test_append_without_queries_and_one_token():
     c = Cache(3, 1, 128, "fp16", "fp4", [1, 64, 65], rows=1.0, seed=6)
     x, rope, positions = _append_case(c, 1, 0, 128, True, 8)
