@@ -783,6 +783,41 @@ def test_a_cache_that_grows_and_gives_back_while_it_decodes_layer_by_layer(fmt):
         assert np.array_equal(c.pool.cpu().numpy(), before), t
 
 
+_FORM = dict(dtype="bf16", fmt="fp4", H=8, G=4, d=128)
+
+
+@pytest.mark.parametrize("case", [
+    dict(_FORM, path="append", S=2, n=40, held=100, rot=128, style="halves"),
+    dict(_FORM, path="append", S=2, n=33, held=0, rot=48, style="pairs", H=32, G=1, d=96, dtype="fp16", fmt="16bit"),
+    dict(_FORM, path="load", S=3, rows=150, uneven=True),
+    dict(_FORM, path="load", S=3, rows=70, uneven=True, d=256, dtype="fp16"),
+    dict(_FORM, path="attend", S=2, rows=300, uneven=True, n=1),
+    dict(_FORM, path="attend", S=2, rows=200, uneven=True, n=4, G=3, d=64, fmt="16bit"),
+    dict(_FORM, path="attend", S=2, rows=200, uneven=True, n=2, G=8, dtype="fp16"),
+    dict(_FORM, path="step", S=3, rows=260, uneven=True, n=1, rot=128, style="halves"),
+], ids=lambda c: "-".join(str(x) for x in c.values()))
+def test_plain_form_definition_and_calls_agree(case, monkeypatch):
+    """The forms that perf/operators.py times, on small cases: rows bit for bit, attention against 64 bits."""
+    from perf import operators
+    monkeypatch.setattr(operators, "own", False)
+    plain = operators.run(operators.prepare(case, 3))
+    plain = {x: t.clone() for x, t in plain.items()}
+    exact = operators.exact(case, 3)
+    monkeypatch.setattr(operators, "own", True)
+    own = operators.run(operators.prepare(case, 3))
+    torch.cuda.synchronize()
+    assert set(own) == set(plain) == set(exact)
+    for x, t in own.items():
+        assert t.shape == plain[x].shape and t.dtype == plain[x].dtype
+        if x in "qkv":
+            assert torch.equal(t, plain[x]), x
+        else:
+            bar = attention_bar(6.0) if x == "attn" else TOL * 16           # V: normal rows; sums of weights up to e^16
+            for y in (t, plain[x]):
+                y, want = y.double(), exact[x]
+                assert torch.equal(y.isneginf(), want.isneginf()) and float((y - want).nan_to_num(0.0).abs().max()) <= bar, x
+
+
 @pytest.mark.parametrize("fmt", ["fp4", "16bit"])
 def test_the_example_runs(fmt, monkeypatch, capsys):
     import importlib.util
