@@ -488,6 +488,25 @@ def test_a_later_tokens_nan_stays_with_it(fmt, d):
         assert np.isnan(_f64(o)[s, 2:]).all()
 
 
+@pytest.mark.parametrize("fmt,dtype", [("fp4", "bf16"), ("fp4", "fp16"), ("16bit", "fp16")])
+@pytest.mark.parametrize("G,n", [(1, 5), (2, 2), (1, 40)])
+def test_a_later_tokens_nan_stays_with_it_in_few_columns_and_over_pages(fmt, dtype, G, n):
+    """The same with five columns at most, whose weights' pieces lie side by side, and with more tokens than a half page has rows: NaN in the value of
+    one token in the middle, in the key of the next."""
+    c = Cache(2, 1, 128, dtype, fmt, [70, 131], rows=1.0, seed=26)
+    q = _queries(c, n, G, 9)
+    want, want_lse = op.attention(_f64(q), c.pool, c.table, c.lens, 1, 0.1, 128, c.fp4, from_bits(c.torch_dtype))
+    t = n // 2
+    for s, key in ((0, False), (1, True)):
+        row = int(c.lens[s]) - n + t + s
+        if row < c.lens[s]:
+            op.write_row(c.pool[c.table[s, row // 64]], row % 64, key, np.full(128, np.nan), c.fp4, to_bits(c.torch_dtype))
+    o, l = _attend(c, q, 0.1, n, G)
+    for s in range(2):
+        assert np.abs(_f64(o)[s, :t + s] - want[s, :t + s]).max() <= TOL * 6 and np.abs(_f64(l)[s, :t + s] - want_lse[s, :t + s]).max() <= TOL * 10
+        assert np.isnan(_f64(o)[s, t + s:]).all()
+
+
 @pytest.mark.parametrize("fmt", ["fp4", "16bit"])
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 def test_peaked_flat_and_negative_logits(fmt, dtype):
