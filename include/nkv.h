@@ -374,7 +374,7 @@ int64_t nkv_page_bytes(int32_t d, int32_t dtype, int32_t format);
  * Appends new tokens: k is rotated by its position's angles, (x, y) -> (x cos - y sin, y cos + x sin) in 64 bits and
  * rounded to 32 (so that the 4-bit code does not depend on how the rotation is computed), and goes with v, rounded to the
  * cache's format, to the pages of rows lens[u] - n_new .. lens[u] - 1; the queries of the same tokens are rotated into
- * q_out.  Pages of different units that overlap race.
+ * q_out, which overlaps nothing that is read.  Pages of different units that overlap race.
  */
 int nkv_pages_append(const nkv_tokens *tokens, const nkv_pages *pages, void *hip_stream);
 
@@ -395,8 +395,17 @@ int nkv_pages_read(void *packed_k, void *packed_v, const int64_t *head_off, int6
  *   out[s][t][h*G+g] = sum_i softmax(scale * <q[s][t][h*G+g], k_i>)_i * v_i        fp32 [n_seqs][n_new][n_q_heads][d]
  *   lse[s][t][h*G+g] = log sum_i exp(scale * <q, k_i>)   (optional, may be NULL)   fp32 [n_seqs][n_new][n_q_heads]
  * q is dense [n_seqs][n_new][n_q_heads][d] in `dtype` (q_out of nkv_pages_append).  A token that sees no row gets out = 0,
- * lse = -inf.  scale may be negative, zero or subnormal; NKV_EINVAL where scale * log2(e) is not finite in fp32.  Products are exact and added up in fp32; keys and values of 4-bit pages enter as the values they stand for.
- * Scratch: nkv_pages_workspace_bytes.  A call is deterministic.
+ * lse = -inf.  scale may be negative, zero or subnormal; NKV_EINVAL where scale * log2(e) is not finite in fp32.  Logits lie
+ * within fp32's range.
+ * Products with keys are exact and added up in fp32.  So are those of values and weights, for which a weight keeps fp32's 24 bits,
+ * and 22 with fp16 rows on 16-bit pages (two pieces of fp16; the sum that it is divided by has them all).  Keys and values of 4-bit
+ * pages enter as the values they stand for; those of 2^128 and more (bf16 rows from 3.5 * 2^126 on, scale bytes 253 and 254) are
+ * beyond fp32, and an attention that sees one gives infinities or NaN.
+ * Scratch: nkv_pages_workspace_bytes, for C = n_q_heads / H * n_new columns of a unit some
+ *   (stretches + units) * C * (d + 4) * 4 bytes, stretches = min(all entries of the table, 8 to 16 a compute unit),
+ * and a unit's pages are read once for every 16 columns.  That suits a token or a few: of one layer of a sequence of 32k rows with 8 KV heads
+ * and 32 query heads of 128 dims, one token takes 6 MiB and four 25 MiB, 64 take 0.4 GiB and 2048 take 12.4 GiB.  A prompt's tokens are appended and
+ * attended some at a time.  A call is deterministic.
  */
 int nkv_pages_workspace_bytes(const nkv_pages *pages, int32_t n_q_heads, int32_t n_new, size_t *bytes);
 int nkv_pages_attention(const void *q, const nkv_pages *pages, int32_t n_q_heads, int32_t n_new, double scale, float *out,

@@ -477,6 +477,7 @@ def pages_read(packed_k, packed_v, head_off, rows: int, pages: Pages, stream=Non
 
 
 def pages_workspace_bytes(pages: Pages, n_q_heads: int, n_new: int = 1) -> int:
+    """Scratch of ``pages_attention``: it grows with n_new times the query heads, see nkv.h; hand over many tokens some at a time."""
     out = C.c_size_t(0)
     rc = lib().nkv_pages_workspace_bytes(pages.ref, int(n_q_heads), int(n_new), C.byref(out))
     if rc:

@@ -71,7 +71,7 @@ __device__ __forceinline__ Slot load_slot(int slot, const uint16_t *kb, const ui
 // A workgroup for a token's heads (K heads, V heads, query heads), or a share of them: kRowsAt rows at a time.  A thread keeps its dims' cosines and sines for
 // all of its rows, and takes eight dims of a row, or, BOTH, two times eight: both dims of eight pairs (or eight and eight that are not rotated), so that each is
 // read and widened once.  In 64 bits the products of a 16-bit value and a 24-bit cosine are exact, so the result is one rounding of the sum, then one to 32 bits,
-// whatever the order of the operations.  3 x 2731 tokens of 8 + 32 heads, head dim 128: eight dims a thread 46.6 us, twice eight 36.9 (4.8 TB/s), with the next
+// whatever the order of the operations.  3 x 2731 tokens of 8 + 32 heads, head dim 128: eight dims a thread 46.6 us, twice eight 36.9 to 37.9 (4.8 TB/s), with the next
 // rows asked for before a row is worked on 41.8: it is wavefronts, and their instructions, half of them in 64 bits, that it takes, not loads in flight.
 template <int D, bool F16, bool FP4, bool BOTH> __global__ __launch_bounds__(256) void append_kernel(const AppendArgs a)
 {
@@ -270,8 +270,10 @@ hipError_t launch_pages_append(const nkv_tokens &t, const nkv_pages &p, hipStrea
     a.H = p.H, a.n_pages = p.n_pages, a.max_pages = p.max_pages;
     a.table = p.table, a.lens = p.lens, a.pool = (uint8_t *)p.pool;
     const int64_t tokens = (int64_t)p.n_seqs * t.n_new;
-    // Both dims of a pair in a thread; in 4 bits where the four threads of a block still lie side by side.  (3 x 2731 tokens of 16 bits, 32 of 128 dims rotated:
-    // 39.8 us, and 42.9 with eight dims a thread.  Neighbouring dims as pairs, or no rotation: eight a thread 37.6 and 34.6 us, sixteen 39.3 and 35.8.)
+    // Both dims of a pair in a thread; in 4 bits where the four threads of a block still lie side by side.  (3 x 2731 tokens of 8 + 32 heads, 16 bits, 32 of 128 dims
+    // rotated: 39.9 us, and 42.9 with eight dims a thread.  Neighbouring dims as pairs, or no rotation: eight a thread 37.6 and 34.6 us, sixteen 39.3 and
+    // 35.8.  Neighbours at head dim 96, 5 x 389 tokens of 32 + 32 heads, fp16 in 4 bits: eight 17.2, sixteen 16.0.  Eight for all neighbours, one kernel less: what
+    // sixteen gain there is less than what they lose at 128.)
     const bool both = t.rot > 0 && a.halves && (p.format != NKV_PAGES_FP4 || (t.rot % 64 == 0 && p.d % 64 == 0));
     // Tokens enough to fill the chip: a workgroup takes all of a token's heads, and loads its angles once; fewer: a share of them.
     const int at_once = 256 / (p.d / (both ? 16 : 8)), most = (2 * p.H + t.n_q_heads + at_once - 1) / at_once;

@@ -2,11 +2,12 @@
 //
 // For unit u and its columns (token, query head): s_i = scale <q, k_i>, out = sum_i softmax(s)_i v_i over the rows that the column sees.
 // Every row is read once for up to 16 columns and used for 4 d multiply-adds a column: bound by memory, if the rest keeps up.
-// Both products go through the matrix cores, exactly:
+// Both products go through the matrix cores, exactly but for fp16 weights:
 //   S = K Q^T     4-bit values become bf16, which holds them exactly (an fp16 query then in two bf16 pieces); 16 x 16 x 32 products
 //                 over a lane's dims in turn.  (The scaled product of 4-bit rows as they lie in the page and 8-bit pieces of a query
 //                 loses bits of small terms beside large ones: up to 6e-6 of the terms' sum, 2e-7 in the mean.)
-//   O^T = V^T P   a weight is split into three bf16 pieces (two of fp16 for rows of those), which hold its 24 (22) bits.
+//   O^T = V^T P   a weight is split into three bf16 pieces, which hold its 24 bits; for 16-bit rows of fp16 into two of fp16, which hold 22: off by 2^-22 of
+//                 the weight at most, 1.4e-8 of an output over some thousand rows, where the sums in fp32 leave 2e-7.
 // A column's running maximum, sum and weighted values stay in registers; with rows as the operands' other axis no lane
 // exchange is needed between the products: the rows that a lane holds of S are those it holds of P, and V's rows are taken in that order.
 //
@@ -16,7 +17,7 @@
 // while the next ones are on their way.
 //
 // Whole calls, us, and what reading the same bytes alone takes (6.8 TB/s): 36 x 8 units of about 8192 rows, head dim 128, 4 query heads a KV head, bf16, 4
-// bits 65 (kernel 59.5), 49; one layer of them 10.3, 1.4: the launches, and three trips to memory one after the other (lengths, page, rows).  A call that
+// bits 65 (kernel 60.1), 49; one layer of them 10.1, 1.4: the launches, and three trips to memory one after the other (lengths, page, rows).  A call that
 // fills the device takes some 10 us beside 4.1 a page and wavefront (6.5 TB/s); the vector and matrix instructions of that page take 2.8.
 #include "nkv_pages.h"
 
