@@ -304,7 +304,7 @@ __device__ __forceinline__ void accumulate(State<D, F16, FP4, COLS> &st, const R
         for (int t = 0; t < Q::C; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i) st.o[t][i] *= f0;
-        far = __any(fabsf(m) >= kFar);
+        far = __any(fabsf(m) >= kFar && m > kNone);                        // (not where a column has seen no row yet)
         if (far) {
 #pragma clang fp contract(off)
 #pragma unroll

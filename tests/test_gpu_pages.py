@@ -593,6 +593,30 @@ def test_logits_of_millions_give_the_largest_ones_row(fmt, dtype, e_k, e_q, d, G
         assert np.abs(_f64(l) / want_lse - 1).max() <= TOL
 
 
+@pytest.mark.parametrize("fmt", ["fp4", "16bit"])
+@pytest.mark.parametrize("n", [5, 16])
+def test_tokens_without_rows_leave_the_others_weights_as_they_are(fmt, n):
+    """Logits of some hundreds, a few apart: in a call whose first tokens see no row, a token's weights are those of a call of its own (whose products are the
+    same sums in fp32), to a few roundings; logits rounded before the maximum is taken from them would be 1.5e-5 off."""
+    d, rows = 64, 4
+    c = Cache(1, 1, d, "bf16", fmt, [rows], rows=1.0, seed=27)
+    g = torch.Generator().manual_seed(4)
+    mean = torch.randn(d, generator=g).sign().double().numpy() * 3.0
+    K = mean + 0.25 * torch.randn(rows, d, generator=g).double().numpy()
+    for i in range(rows):
+        op.write_row(c.pool[c.table[0, 0]], i, True, K[i], c.fp4, to_bits(c.torch_dtype))
+    q = torch.from_numpy(mean * (1 + 0.1 * torch.rand(1, n, 1, d, generator=g).double().numpy())).to(c.torch_dtype)
+    scale = 0.5
+    o, l = _attend(c, q, scale, n, 1)
+    for t in range(n - rows, n):
+        alone = Cache(1, 1, d, "bf16", fmt, [rows], seed=27)
+        alone.pool, alone.table, alone.lens = c.pool, c.table, np.array([rows - (n - 1 - t)], np.int32)
+        o1, l1 = _attend(alone, q[:, t:t + 1].contiguous(), scale, 1, 1)
+        assert float(l1) > 200
+        assert np.abs(_f64(o)[0, t] - _f64(o1)[0, 0]).max() <= 2e-6, t
+    assert bool((o[0, :n - rows] == 0).all()) and bool(l[0, :n - rows].isneginf().all())
+
+
 def test_units_may_share_pages():
     c = Cache(4, 1, 64, "bf16", "fp4", [130, 100, 64, 130], rows=1.0, seed=19)
     c.table[1:] = c.table[0]
