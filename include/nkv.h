@@ -400,7 +400,7 @@ int nkv_pages_read(void *packed_k, void *packed_v, const int64_t *head_off, int6
  * Products with keys are exact and added up in fp32.  So are those of values and weights, for which a weight keeps fp32's 24 bits,
  * and 22 with fp16 rows on 16-bit pages (two pieces of fp16; the sum that it is divided by has them all).  Keys and values of 4-bit
  * pages enter as the values they stand for; those of 2^128 and more (bf16 rows from 3.5 * 2^126 on, scale bytes 253 and 254) are
- * beyond fp32, and an attention that sees one gives infinities or NaN.
+ * beyond fp32, and a token that sees such a block gets infinities or NaN.
  * Scratch: nkv_pages_workspace_bytes, for C = n_q_heads / H * n_new columns of a unit some
  *   (stretches + units) * C * (d + 4) * 4 bytes, stretches = min(all entries of the table, 8 to 16 a compute unit),
  * and a unit's pages are read once for every 16 columns.  That suits a token or a few: of one layer of a sequence of 32k rows with 8 KV heads

@@ -247,7 +247,8 @@ template <int D, bool F16, bool FP4, int COLS> struct State {
 
 // The end of a unit's rows.  rel: rows from the half's first one on, lim: those that the lane's column sees, least: those that all columns see.
 // Rows that a column does not see get the product -inf, so weight 0; V of rows that are not there becomes 0 or 1, since 0 times NaN is NaN.  So it does
-// where a row that only later tokens see holds a NaN or infinity, whose columns get a NaN for a product instead.
+// where a row that only later tokens see holds a NaN or infinity (in 4 bits: a block of a scale from 2^126 on, whose larger codes are beyond bf16), whose
+// columns get a NaN for a product instead.
 template <int D, bool F16, bool FP4>
 __device__ __forceinline__ void mask_rows(Rows<D, F16, FP4> &f, f32x4 (&s)[Geo<D, F16, FP4>::kTiles], int g, int rel, int lim, int least)
 {
@@ -260,7 +261,7 @@ __device__ __forceinline__ void mask_rows(Rows<D, F16, FP4> &f, f32x4 (&s)[Geo<D
             bool clear = row >= rel, poison = false;
             if (least < rel) {                                             // several tokens
                 bool odd = false;
-                if constexpr (FP4) odd = (f.vs[t] >> (8 * i) & 255u) == 255u;
+                if constexpr (FP4) odd = (f.vs[t] >> (8 * i) & 255u) >= 253u;
                 else
 #pragma unroll
                     for (int k = 0; k < Q::C / 2; ++k) {

@@ -509,6 +509,25 @@ def test_a_later_tokens_nan_stays_with_it_in_few_columns_and_over_pages(fmt, dty
 
 
 @pytest.mark.parametrize("fmt", ["fp4", "16bit"])
+@pytest.mark.parametrize("d,G,n", [(128, 3, 4), (64, 1, 4), (256, 1, 20)])
+def test_a_later_tokens_largest_value_stays_with_it(fmt, d, G, n):
+    """The value of a token in the middle holds bf16's largest number, which in 4 bits is 2^128: tokens in front of it do not see it."""
+    c = Cache(2, 1, d, "bf16", fmt, [70, 131], rows=1.0, seed=28)
+    q = _queries(c, n, G, 9)
+    want, want_lse = op.attention(_f64(q), c.pool, c.table, c.lens, 1, 0.1, d, c.fp4, from_bits(c.torch_dtype))
+    t = n // 2
+    for s in range(2):
+        row = int(c.lens[s]) - n + t
+        x = np.linspace(-1, 1, d)
+        x[5], x[d - 1] = torch.finfo(torch.bfloat16).max, -torch.finfo(torch.bfloat16).max
+        op.write_row(c.pool[c.table[s, row // 64]], row % 64, False, x, c.fp4, to_bits(c.torch_dtype))
+    o, l = _attend(c, q, 0.1, n, G)
+    assert np.abs(_f64(o)[:, :t] - want[:, :t]).max() <= TOL * 6 and np.abs(_f64(l)[:, :t] - want_lse[:, :t]).max() <= TOL * 10
+    for s in range(2):
+        assert (~(np.abs(_f64(o)[s, t:, :, 5]) < 1e30)).all()             # large, infinite or NaN
+
+
+@pytest.mark.parametrize("fmt", ["fp4", "16bit"])
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 def test_peaked_flat_and_negative_logits(fmt, dtype):
     """One row that takes nearly all weight, all rows alike (scale 0: the mean of the values, lse = log n), a negative scale, large logits."""
