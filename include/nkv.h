@@ -412,6 +412,53 @@ int nkv_pages_attention(const void *q, const nkv_pages *pages, int32_t n_q_heads
                         float *lse, void *ws, size_t ws_bytes, void *hip_stream);
 
 /*
+ * Copies whole pages inside the pool, page src[i] to page dst[i] (device, i < n): a sequence that continues another one shares
+ * the other's full pages and gets copies of those that it will write.  Pairs of which one is outside [0, n_pages) are left out.  No page is
+ * in dst twice or in both dst and src, but where src[i] = dst[i]: such pages' contents are undefined afterwards.  table and lens are not read.
+ */
+int nkv_pages_copy(const int32_t *src, const int32_t *dst, int64_t n, const nkv_pages *pages, void *hip_stream);
+
+/*
+ * Thins out a cache: rows kept_idx[head_off[u] .. head_off[u + 1] - 1] of unit u of `from` (numbers within the unit, in any order, twice if that
+ * is wanted) become rows 0, 1, .. of unit u of `to`, bit by bit, 4-bit rows as the codes and scales that they are.  head_off (int64 [units + 1]) is
+ * clamped to `rows`, how many numbers kept_idx (int32) holds.  A number that is no row of the unit, or whose page is none, gives a row of zeros; rows whose
+ * page in `to` is none are not written, and neither are those behind a unit's last one on its last page.  The two have the same sequences, heads, rows and
+ * format (NKV_ESHAPE) and may share a pool, but no page of `to` is one that `from` reads.  lens of `to` is not read: the caller sets it to the counts.
+ */
+int nkv_pages_compact(const int32_t *kept_idx, const int64_t *head_off, int64_t rows, const nkv_pages *from, const nkv_pages *to,
+                      void *hip_stream);
+
+/*
+ * ---- Beam search: the next beams of every prompt ----
+ *
+ * Of prompt p's candidates (beam b, token t) the n_out with the largest scores[p][b] + logits[p][b][t] - log sum_i exp(logits[p][b][i]), largest first,
+ * of equal ones the lower beam, then the lower token:
+ *   out_scores [n_prompts][n_out] fp32, out_beams, out_tokens [n_prompts][n_out] int32
+ * Values are formed and compared in 64 bits; the sums of exponentials are in 32 bits up to 8192 logits and in 64 from there on, off by some 1e-7 of
+ * themselves.  Tokens of a beam are in the order of their logits.
+ * A token whose logit is -inf is no candidate, and a beam has none whose score is infinite or NaN (a beam that is not there yet: -inf) or whose log sum is (one of
+ * its logits is NaN or +inf, or all are -inf).  Where there are fewer than n_out the rest is score -inf, beam -1, token -1.
+ * NKV_ESHAPE: n_beams * vocab of 2^32 and more, vocab over 2^30, or 2^24 and more stretches of 2048 logits (8192 where there are 1024 and more of these).
+ * Deterministic; scratch: nkv_beam_workspace_bytes, n_out * 8 + 8 bytes a stretch.
+ */
+#define NKV_MAX_BEAMS_OUT 64
+typedef struct nkv_beams {
+    uint32_t struct_size;     /* sizeof(nkv_beams)                                                    */
+    int32_t  n_prompts;
+    int32_t  n_beams;         /* beams of a prompt                                                    */
+    int32_t  vocab;           /* logits of a beam                                                     */
+    int32_t  n_out;           /* 1 .. NKV_MAX_BEAMS_OUT                                               */
+    int32_t  dtype;           /* of the logits: NKV_DTYPE_F32, _BF16 or _F16                          */
+    int64_t  strides[2];      /* {prompt, beam} in elements: any; a beam's logits lie next to each other */
+    const void *logits;       /* DEVICE, aligned as its elements are                                  */
+    const float *scores;      /* DEVICE, dense [n_prompts][n_beams]                                   */
+} nkv_beams;
+
+int nkv_beam_workspace_bytes(const nkv_beams *beams, size_t *bytes);
+int nkv_beam_select(const nkv_beams *beams, float *out_scores, int32_t *out_beams, int32_t *out_tokens, void *ws, size_t ws_bytes,
+                    void *hip_stream);
+
+/*
  * Plain device-to-device copy of `bytes` bytes (a multiple of 16, both pointers 16-byte aligned): contiguous
  * 16 KB pieces per workgroup, non-temporal 16-byte loads and stores -- the access pattern of the K/V gather
  * without its indirection.  dst == NULL: the loads only (what a pure reader can reach).  Not part of the pass:

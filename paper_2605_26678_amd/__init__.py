@@ -32,11 +32,13 @@ PIN = 3.0e38
 PAGE_ROWS = 64
 PAGES_16BIT, PAGES_FP4 = 0, 1
 ROPE_HALVES, ROPE_PAIRS = 0, 1
+MAX_BEAMS_OUT = 64
 
 EXPORTS = ("nkv_params_default", "nkv_block_size", "nkv_k0", "nkv_m_safe", "nkv_m_p", "nkv_packed_rows",
            "nkv_workspace_bytes", "nkv_score", "nkv_score_raw", "nkv_budget", "nkv_budget_noalloc", "nkv_select_compact",
            "nkv_decode_workspace_bytes", "nkv_decode_attention", "nkv_page_bytes", "nkv_pages_append", "nkv_pages_load",
-           "nkv_pages_read", "nkv_pages_workspace_bytes", "nkv_pages_attention", "nkv_copy_probe", "nkv_strerror", "nkv_version")
+           "nkv_pages_read", "nkv_pages_workspace_bytes", "nkv_pages_attention", "nkv_pages_copy", "nkv_pages_compact",
+           "nkv_beam_workspace_bytes", "nkv_beam_select", "nkv_copy_probe", "nkv_strerror", "nkv_version")
 KERNELS = ("scan", "finalize", "budget", "select", "gather", "decode")
 PASS_KERNELS = KERNELS[:5]          # the kernels of the compression pass itself
 
@@ -70,6 +72,11 @@ class nkv_tokens(C.Structure):
                 ("q", C.c_void_p), ("q_out", C.c_void_p), ("k_strides", C.c_int64 * 3),
                 ("v_strides", C.c_int64 * 3), ("q_strides", C.c_int64 * 3), ("positions", C.c_void_p),
                 ("rope", C.c_void_p)]
+
+
+class nkv_beams(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("n_prompts", C.c_int32), ("n_beams", C.c_int32), ("vocab", C.c_int32), ("n_out", C.c_int32),
+                ("dtype", C.c_int32), ("strides", C.c_int64 * 2), ("logits", C.c_void_p), ("scores", C.c_void_p)]
 
 
 _TOKENS_SIZE = C.sizeof(nkv_tokens)
@@ -124,6 +131,10 @@ def lib() -> C.CDLL:
         L.nkv_pages_workspace_bytes.argtypes = [C.POINTER(nkv_pages), C.c_int32, C.c_int32, C.POINTER(C.c_size_t)]
         L.nkv_pages_attention.argtypes = [vp, C.POINTER(nkv_pages), C.c_int32, C.c_int32, f64, vp, vp, vp,
                                           C.c_size_t, vp]
+        L.nkv_pages_copy.argtypes = [vp, vp, i64, C.POINTER(nkv_pages), vp]
+        L.nkv_pages_compact.argtypes = [vp, vp, i64, C.POINTER(nkv_pages), C.POINTER(nkv_pages), vp]
+        L.nkv_beam_workspace_bytes.argtypes = [C.POINTER(nkv_beams), C.POINTER(C.c_size_t)]
+        L.nkv_beam_select.argtypes = [C.POINTER(nkv_beams), vp, vp, vp, vp, C.c_size_t, vp]
         L.nkv_copy_probe.argtypes = [vp, vp, C.c_size_t, vp]
         L.nkv_strerror.argtypes = [C.c_int]
         L.nkv_strerror.restype = C.c_char_p
@@ -506,6 +517,81 @@ def pages_attention(q, pages: Pages, n_q_heads: int, n_new: int, scale: float, o
                                    0 if lse is None else lse.data_ptr(), ws_at, ws_bytes, _stream(stream))
     if rc:
         raise NkvError(rc, "nkv_pages_attention")
+
+
+def pages_copy(src, dst, pages: Pages, stream=None) -> None:
+    """Page src[i] to page dst[i] of the pool, src and dst int32 of the same length; see ``nkv_pages_copy`` in nkv.h."""
+    n = src.numel()
+    if dst.numel() != n:
+        raise ValueError(f"src has {n} pages and dst {dst.numel()}")
+    _check_dense(src, "src", pages, pages.torch_i32, n)
+    _check_dense(dst, "dst", pages, pages.torch_i32, n)
+    _check_gpu(pages)
+    rc = lib().nkv_pages_copy(src.data_ptr(), dst.data_ptr(), n, pages.ref, _stream(stream))
+    if rc:
+        raise NkvError(rc, "nkv_pages_copy")
+
+
+def pages_compact(kept_idx, head_off, rows: int, old: Pages, pages: Pages, stream=None) -> None:
+    """Rows kept_idx[head_off[u] .. head_off[u + 1] - 1] (int32, numbers within the unit) of every unit of ``old`` to the front of the unit
+    in ``pages``, which has pages of its own; see ``nkv_pages_compact`` in nkv.h."""
+    rows = int(rows)
+    if old.index != pages.index:
+        raise _elsewhere(old.pool, "old", pages)
+    _check_dense(kept_idx, "kept_idx", pages, pages.torch_i32, rows)
+    _check_dense(head_off, "head_off", pages, pages.torch_i64, pages.units + 1)
+    _check_gpu(pages)
+    rc = lib().nkv_pages_compact(kept_idx.data_ptr(), head_off.data_ptr(), rows, old.ref, pages.ref, _stream(stream))
+    if rc:
+        raise NkvError(rc, "nkv_pages_compact")
+
+
+def _beams(n_prompts: int, n_beams: int, vocab: int, n_out: int, dtype: int, strides, logits: int, scores: int) -> nkv_beams:
+    return nkv_beams(C.sizeof(nkv_beams), n_prompts, n_beams, vocab, n_out, dtype, (C.c_int64 * 2)(*strides), logits, scores)
+
+
+def beam_workspace_bytes(n_prompts: int, n_beams: int, vocab: int, n_out: int) -> int:
+    """Scratch of ``beam_select``."""
+    out = C.c_size_t(0)
+    some = 256                                           # (an address that is not used)
+    rc = lib().nkv_beam_workspace_bytes(C.byref(_beams(n_prompts, n_beams, vocab, n_out, DTYPE_F32, (0, 0), some, some)), C.byref(out))
+    if rc:
+        raise NkvError(rc, "nkv_beam_workspace_bytes")
+    return int(out.value)
+
+
+_logit_types = None
+
+
+def beam_select(logits, scores, out_scores, out_beams, out_tokens, ws, stream=None) -> None:
+    """The best candidates of every prompt: logits [P, B, V] of fp32, bf16 or fp16 (any strides but the last dim's), scores fp32 [P, B] ->
+    out_scores fp32, out_beams, out_tokens int32 [P, n_out], largest first; see ``nkv_beam_select`` in nkv.h."""
+    global _logit_types
+    import torch
+    if _logit_types is None:
+        _logit_types = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16}
+    dtype = _logit_types.get(logits.dtype)
+    if dtype is None or logits.dim() != 3 or logits.stride(2) != 1 and logits.shape[2] > 1:
+        raise ValueError("logits is fp32, bf16 or fp16 [prompts, beams, vocabulary], a beam's logits next to each other")
+    P, B, V = logits.shape
+    at = logits.get_device()
+    if out_scores.dim() != 2 or out_scores.shape[0] != P:
+        raise ValueError(f"out_scores is [{P}, n_out]")
+    n_out = out_scores.shape[1]
+    for t, what, kind, shape in ((scores, "scores", torch.float32, (P, B)), (out_scores, "out_scores", torch.float32, (P, n_out)),
+                                 (out_beams, "out_beams", torch.int32, (P, n_out)), (out_tokens, "out_tokens", torch.int32, (P, n_out))):
+        if t.dtype is not kind or t.shape != shape or not t.is_contiguous():
+            raise ValueError(f"{what} is dense {kind} {list(shape)}, not {t.dtype} {list(t.shape)}")
+        if t.get_device() != at:
+            raise ValueError(f"{what} is on device {t.device}, and the logits are on {logits.device}")
+    if not ws.is_contiguous() or ws.get_device() != at:
+        raise ValueError("ws is contiguous and on the logits' device")
+    if at < 0:
+        raise ValueError("the logits are not on a GPU")
+    rc = lib().nkv_beam_select(C.byref(_beams(P, B, V, n_out, dtype, (logits.stride(0), logits.stride(1)), logits.data_ptr(), scores.data_ptr())),
+                               out_scores.data_ptr(), out_beams.data_ptr(), out_tokens.data_ptr(), ws.data_ptr(), ws.nbytes, _stream(stream))
+    if rc:
+        raise NkvError(rc, "nkv_beam_select")
 
 
 def copy_probe(dst, src, stream=None) -> None:

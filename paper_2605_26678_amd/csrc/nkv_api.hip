@@ -291,6 +291,19 @@ int check_attention(const nkv_pages *pages, int32_t n_q_heads, int32_t n_new)
     return NKV_OK;
 }
 
+int check_beams(const nkv_beams *s)
+{
+    if (!s || s->struct_size != sizeof(nkv_beams)) return NKV_EINVAL;
+    if (s->n_prompts < 1 || s->n_beams < 1 || s->vocab < 1) return NKV_ESHAPE;
+    if (s->n_out < 1 || s->n_out > NKV_MAX_BEAMS_OUT) return NKV_EINVAL;
+    if (s->dtype == NKV_DTYPE_F8_E4M3) return NKV_EUNSUPPORTED;
+    if (s->dtype < NKV_DTYPE_F32 || s->dtype > NKV_DTYPE_F8_E4M3) return NKV_EINVAL;
+    if (!s->logits || !s->scores || (uintptr_t)s->logits % esize_of(s->dtype) || (uintptr_t)s->scores % 4) return NKV_EINVAL;
+    // a candidate's number within a prompt is 32 bits
+    if (s->vocab > (1 << 30) || (int64_t)s->n_beams * s->vocab >= (1ll << 32) || !beam_one_launch(*s)) return NKV_ESHAPE;
+    return NKV_OK;
+}
+
 }  // namespace
 }  // namespace nkv
 
@@ -606,6 +619,46 @@ int nkv_pages_attention(const void *q, const nkv_pages *pages, int32_t n_q_heads
     rc = check_ws(ws, ws_bytes, pages_ws_bytes(*pages, n_q_heads, n_new));
     if (rc) return rc;
     return launch_pages_attention(q, *pages, n_q_heads, n_new, scale, out, lse, ws, (hipStream_t)hip_stream) == hipSuccess ? NKV_OK : NKV_EHIP;
+}
+
+int nkv_pages_copy(const int32_t *src, const int32_t *dst, int64_t n, const nkv_pages *pages, void *hip_stream)
+{
+    const int rc = check_pages(pages);
+    if (rc) return rc;
+    if (n < 0 || (n > 0 && (!src || !dst)) || (uintptr_t)src % 4 || (uintptr_t)dst % 4) return NKV_EINVAL;
+    if (n >= (1 << 22)) return NKV_ESHAPE;                           // up to four workgroups a page
+    return launch_pages_copy(src, dst, n, *pages, (hipStream_t)hip_stream) == hipSuccess ? NKV_OK : NKV_EHIP;
+}
+
+int nkv_pages_compact(const int32_t *kept_idx, const int64_t *head_off, int64_t rows, const nkv_pages *from, const nkv_pages *to, void *hip_stream)
+{
+    int rc = check_pages(from);
+    if (rc) return rc;
+    rc = check_pages(to);
+    if (rc) return rc;
+    if (from->n_seqs != to->n_seqs || from->H != to->H || from->d != to->d || from->dtype != to->dtype || from->format != to->format) return NKV_ESHAPE;
+    if (!head_off || rows < 0 || (rows > 0 && !kept_idx) || (uintptr_t)kept_idx % 4 || (uintptr_t)head_off % 8) return NKV_EINVAL;
+    if (!one_launch(rows / NKV_PAGE_ROWS + 2 * (int64_t)to->n_seqs * to->H, 2 * to->d)) return NKV_ESHAPE;   // a workgroup for a page
+    return launch_pages_compact(kept_idx, head_off, rows, *from, *to, (hipStream_t)hip_stream) == hipSuccess ? NKV_OK : NKV_EHIP;
+}
+
+int nkv_beam_workspace_bytes(const nkv_beams *beams, size_t *bytes)
+{
+    if (!bytes) return NKV_EINVAL;
+    const int rc = check_beams(beams);
+    if (rc) return rc;
+    *bytes = beam_ws_bytes(*beams);
+    return NKV_OK;
+}
+
+int nkv_beam_select(const nkv_beams *beams, float *out_scores, int32_t *out_beams, int32_t *out_tokens, void *ws, size_t ws_bytes, void *hip_stream)
+{
+    int rc = check_beams(beams);
+    if (rc) return rc;
+    if (!out_scores || !out_beams || !out_tokens || (uintptr_t)out_scores % 4 || (uintptr_t)out_beams % 4 || (uintptr_t)out_tokens % 4) return NKV_EINVAL;
+    rc = check_ws(ws, ws_bytes, beam_ws_bytes(*beams));
+    if (rc) return rc;
+    return launch_beam_select(*beams, out_scores, out_beams, out_tokens, ws, (hipStream_t)hip_stream) == hipSuccess ? NKV_OK : NKV_EHIP;
 }
 
 int nkv_copy_probe(void *dst, const void *src, size_t bytes, void *hip_stream)

@@ -1,0 +1,348 @@
+// Selection of a beam search's next beams (nkv_beam_select): of every prompt's B * V candidates scores[b] + x - log sum exp x the n_out largest.
+//
+// Every logit is read once, for one exponential and one comparison: bound by memory.  A workgroup keeps a stretch of one beam's row in registers
+// (beam_scan_kernel) and leaves its maximum, its sum of exponentials and its n_out largest logits; a workgroup for a prompt joins them
+// (beam_join_kernel): the sums in 64 bits, the candidates by their value in 64 bits.
+//
+// Within a beam the order of the candidates is that of the logits, so no sum is needed to drop nearly all of them: the n_out-th largest of a
+// wavefront's 64 lane maxima is a bound that at least n_out of its logits reach, and few more.  Lists are 64 keys, one a lane, sorted and joined by
+// bitonic steps between lanes (21 steps to sort, 7 to join two).  A key holds the logit and, of equal ones, the lower token as the larger key, so that
+// no two are alike and the answer does not depend on the order of anything.
+#include "nkv_device.h"
+
+#include <algorithm>
+#include <type_traits>
+
+namespace nkv {
+namespace {
+
+constexpr int kThreads = 256, kWaves = kThreads / kWave, kJoin = 1024, kJoinWaves = kJoin / kWave;
+constexpr float kLog2e = 1.4426950408889634f;
+
+// Partial result of a stretch, in front of its n_out keys.
+struct Head {
+    float top, sum;                      // sum of exp(x - top), or of exp(x) where all of them are -inf
+};
+
+// the word of the lane whose number differs in the bits M, a power of two
+template <int M> __device__ __forceinline__ uint32_t lane_xor(uint32_t v)
+{
+    if constexpr (M == 1) return dpp_word<0xB1>(v);                        // quad_perm [1,0,3,2]
+    else if constexpr (M == 2) return dpp_word<0x4E>(v);                   // quad_perm [2,3,0,1]
+    else if constexpr (M == 4) return dpp_word<0x1B>(dpp_word<0x141>(v));  // 7 by row_half_mirror, and 3 by quad_perm [3,2,1,0]
+    else if constexpr (M == 8) return dpp_word<0x128>(v);                  // row_ror:8
+    else if constexpr (M == 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        return (threadIdx.x & 16) ? r[0] : r[1];
+    } else {
+        const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        return (threadIdx.x & 32) ? r[0] : r[1];
+    }
+}
+// lane 63 - i's
+__device__ __forceinline__ uint32_t lane_mirror(uint32_t v) { return lane_xor<32>(lane_xor<16>(dpp_word<0x140>(v))); }
+
+// A logit of a beam: its order and, inverted, its token.  Zero: none.
+struct Key {
+    uint32_t value, token;
+    __device__ __forceinline__ bool operator>(const Key &o) const { return ((uint64_t)value << 32 | token) > ((uint64_t)o.value << 32 | o.token); }
+    template <typename F> __device__ __forceinline__ Key moved(F f) const { return {f(value), f(token)}; }
+    __device__ static Key none() { return {0u, 0u}; }
+};
+// A candidate of a prompt: the order of its value in 64 bits and, inverted, beam * V + token.
+struct Candidate {
+    uint32_t hi, lo, at;
+    __device__ __forceinline__ uint64_t value() const { return (uint64_t)hi << 32 | lo; }
+    __device__ __forceinline__ bool operator>(const Candidate &o) const { return value() > o.value() || (value() == o.value() && at > o.at); }
+    template <typename F> __device__ __forceinline__ Candidate moved(F f) const { return {f(hi), f(lo), f(at)}; }
+    __device__ static Candidate none() { return {0u, 0u, 0u}; }
+};
+
+template <int J, typename K> __device__ __forceinline__ K step(const K &a, bool larger)
+{
+    const K b = a.moved([](uint32_t v) { return lane_xor<J>(v); });
+    return (b > a) == larger ? b : a;                                      // (equal ones are the same)
+}
+// the 64 lanes' keys, largest first, where every stretch of 2 J is bitonic
+template <int J, typename K> __device__ __forceinline__ K ordered(K a, bool descending)
+{
+    const int lane = threadIdx.x & (kWave - 1);
+    a = step<J>(a, ((lane & J) == 0) == descending);
+    if constexpr (J > 1) return ordered<J / 2>(a, descending);
+    else return a;
+}
+template <typename K> __device__ __forceinline__ K sorted(K a)
+{
+    const int lane = threadIdx.x & (kWave - 1);
+    a = ordered<1>(a, (lane & 2) == 0);
+    a = ordered<2>(a, (lane & 4) == 0);
+    a = ordered<4>(a, (lane & 8) == 0);
+    a = ordered<8>(a, (lane & 16) == 0);
+    a = ordered<16>(a, (lane & 32) == 0);
+    return ordered<32>(a, true);
+}
+// the 64 largest of two lists that are largest first
+template <typename K> __device__ __forceinline__ K joined(const K &a, const K &b)
+{
+    const K c = b.moved([](uint32_t v) { return lane_mirror(v); });
+    return ordered<32>(c > a ? c : a, true);
+}
+template <typename K> __device__ __forceinline__ K of_lane(const K &a, int lane)
+{
+    return a.moved([lane](uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); });
+}
+
+template <typename T> struct Logits;
+template <> struct Logits<float> { static constexpr int kWords = 8; static constexpr int kBits = 32; };
+template <> struct Logits<f16_t> { static constexpr int kWords = 4; static constexpr int kBits = 16; };
+template <> struct Logits<uint16_t> { static constexpr int kWords = 4; static constexpr int kBits = 16; };   // bf16
+
+template <typename T> __device__ __forceinline__ float logit(const uint32_t *w, int i)
+{
+    if constexpr (std::is_same_v<T, float>) return __uint_as_float(w[i]);
+    else if constexpr (std::is_same_v<T, f16_t>) return (float)__builtin_bit_cast(_Float16, (uint16_t)(i % 2 ? w[i / 2] >> 16 : w[i / 2]));
+    else return __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+}
+
+// logit e of a lane's, chosen among its registers
+template <typename T, int VECS> __device__ __forceinline__ float logit_at(const uint32_t (&w)[VECS][Logits<T>::kWords], int e)
+{
+    constexpr int N = VECS * Logits<T>::kWords;
+    constexpr bool kHalf = !std::is_same_v<T, float>;
+    uint32_t x[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = w[i / Logits<T>::kWords][i % Logits<T>::kWords];
+    int at = kHalf ? e / 2 : e;
+#pragma unroll
+    for (int n = N / 2; n > 0; n /= 2) {
+        const uint32_t upper = 0u - (uint32_t)(at & 1);                    // (a choice by bits: one by condition becomes an address in memory)
+#pragma unroll
+        for (int i = 0; i < n; ++i) x[i] = (x[2 * i + 1] & upper) | (x[2 * i] & ~upper);
+        at >>= 1;
+    }
+    if constexpr (kHalf) x[0] = e % 2 ? x[0] >> 16 : x[0] & 0xffffu;
+    return logit<T>(x, 0);
+}
+
+struct ScanArgs {
+    const void *logits;
+    int64_t prompt, beam;                // strides
+    int32_t B, V, n_out, stretches;
+    Head *heads;                         // [row][stretch]
+    Key *keys;                           // [row][stretch][n_out]
+};
+
+// grid: rows * stretches.  E logits a thread, eight at a time: of which thread does not depend on where a row begins, so that equal rows have
+// equal sums.
+template <typename T, int E> __global__ __launch_bounds__(kThreads) void beam_scan_kernel(const ScanArgs a)
+{
+    using L = Logits<T>;
+    using Words = unsigned int __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+    constexpr int kVecs = E / 8;
+    __shared__ Key buffer[kWaves][2 * kWave];
+    __shared__ Head heads[kWaves];
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), w = __builtin_amdgcn_readfirstlane(tid / kWave), n_out = a.n_out;
+    const int row = blockIdx.x / a.stretches, stretch = blockIdx.x - row * a.stretches;
+    const int p = row / a.B, b = row - p * a.B;
+    const T *x = (const T *)a.logits + p * a.prompt + b * a.beam;
+    const int first = stretch * (kThreads * E);                         // (V is under 2^31 - kThreads * 32)
+    uint32_t raw[kVecs][L::kWords];
+#pragma unroll
+    for (int j = 0; j < kVecs; ++j) {
+        const int at = first + (j * kThreads + tid) * 8;
+        if (at + 8 <= a.V) {
+#pragma unroll
+            for (int i = 0; i < L::kWords; i += 4) {
+                const Words v = __builtin_nontemporal_load(reinterpret_cast<const Words *>(x + at) + i / 4);
+                raw[j][i] = v.x, raw[j][i + 1] = v.y, raw[j][i + 2] = v.z, raw[j][i + 3] = v.w;
+            }
+        } else {                                                           // the row's end: what is behind it counts as -inf
+#pragma unroll
+            for (int i = 0; i < L::kWords; ++i) {
+                if constexpr (std::is_same_v<T, float>) raw[j][i] = at + i < a.V ? reinterpret_cast<const uint32_t *>(x)[at + i] : 0xff800000u;
+                else {
+                    constexpr uint32_t none = std::is_same_v<T, f16_t> ? 0xfc00u : 0xff80u;
+                    const uint16_t *h = reinterpret_cast<const uint16_t *>(x);
+                    const uint32_t lo = at + 2 * i < a.V ? h[at + 2 * i] : none, hi = at + 2 * i + 1 < a.V ? h[at + 2 * i + 1] : none;
+                    raw[j][i] = lo | hi << 16;
+                }
+            }
+        }
+    }
+    float mine = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < kVecs; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) mine = fmaxf(mine, logit<T>(raw[j], i));
+    const float top = wave_max(mine), base = top == -INFINITY ? 0.f : top;
+    float sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < kVecs; ++j) {
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s += __builtin_amdgcn_exp2f((logit<T>(raw[j], i) - base) * kLog2e);
+        sum += s;
+    }
+    sum = wave_sum(sum);
+    // The largest bound, bit by bit, that n_out lane maxima reach (all of 64 lanes count: those of -inf too, which are none in the end).
+    const uint32_t key = ord_key(mine);
+    uint32_t bound = 0u;
+    for (int bit = 31; bit >= 32 - L::kBits; --bit) {
+        const uint32_t trial = bound | 1u << bit;
+        const int reach = __popcll(__ballot(key >= trial));
+        if (reach >= n_out) bound = trial;
+        if (reach == n_out) break;
+    }
+    const float from = key_value(max(bound, ord_key(-3.402823466e38f)));   // -inf and NaN are no candidates
+    uint32_t takes = 0u;                                                   // bit 8 j + i: the lane's logit i of vector j
+#pragma unroll
+    for (int j = 0; j < kVecs; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) takes |= logit<T>(raw[j], i) >= from ? 1u << (8 * j + i) : 0u;
+    Key list = Key::none(), least = Key::none();
+    int held = 0;
+    Key *mine_b = buffer[w];
+    auto flush = [&](int count) {                                          // the first `count` of the buffer
+        __builtin_amdgcn_wave_barrier();
+        const Key k = lane < count ? mine_b[lane] : Key::none();
+        list = joined(list, sorted(k));
+        least = of_lane(list, n_out - 1);
+    };
+    do {                                                                   // one of every lane's at a time; fewer than 64 are held
+        const bool left = takes != 0u;
+        const int e = left ? __builtin_ctz(takes) : 0;
+        takes &= takes - 1u;
+        const Key k{ord_key(logit_at<T, kVecs>(raw, e)), ~(uint32_t)(first + (e / 8 * kThreads + tid) * 8 + e % 8)};
+        const bool counts = left && k > least;
+        const unsigned long long mask = __ballot(counts);
+        if (counts) mine_b[held + __popcll(mask & ((1ull << lane) - 1ull))] = k;
+        held += __popcll(mask);
+        if (held >= kWave) {
+            flush(kWave);
+            held -= kWave;
+            const Key rest = mine_b[kWave + lane];
+            __builtin_amdgcn_wave_barrier();
+            mine_b[lane] = rest;
+        }
+        __builtin_amdgcn_wave_barrier();
+    } while (__any(takes != 0u));
+    if (held > 0) flush(held);
+    __builtin_amdgcn_wave_barrier();
+    mine_b[lane] = list;
+    if (lane == 0) heads[w] = Head{top, sum};
+    __syncthreads();
+    if (w > 0) return;
+    static_assert(kWaves == 4, "two steps");
+    list = joined(joined(list, buffer[1][lane]), joined(buffer[2][lane], buffer[3][lane]));
+    const int64_t part = blockIdx.x;
+    if (lane < n_out) a.keys[part * n_out + lane] = list;
+    if (lane == 0) {
+        float m = -INFINITY, s = 0.f;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) m = fmaxf(m, heads[i].top);
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) s += heads[i].top == -INFINITY ? heads[i].sum : heads[i].sum * __builtin_amdgcn_exp2f((heads[i].top - m) * kLog2e);
+        a.heads[part] = Head{m, s};
+    }
+}
+
+__device__ __forceinline__ uint64_t ord64(double x)
+{
+    const uint64_t u = __builtin_bit_cast(uint64_t, x == 0.0 ? 0.0 : x);
+    return u >> 63 ? ~u : u | 1ull << 63;
+}
+__device__ __forceinline__ double value64(uint64_t k) { return __builtin_bit_cast(double, k >> 63 ? k & ~(1ull << 63) : ~k); }
+
+// grid: a workgroup a prompt
+__global__ __launch_bounds__(kJoin) void beam_join_kernel(const Head *__restrict__ heads, const Key *__restrict__ keys, const float *__restrict__ scores, int B,
+                                                         int V, int n_out, int stretches, double *__restrict__ lses, float *__restrict__ out_scores,
+                                                         int32_t *__restrict__ out_beams, int32_t *__restrict__ out_tokens)
+{
+    __shared__ Candidate lists[kJoinWaves][kWave];
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), w = __builtin_amdgcn_readfirstlane(tid / kWave), p = blockIdx.x;
+    // log sum exp of every beam, NaN for a beam without candidates: where it is not finite, or the beam's score is not
+    for (int b = w; b < B; b += kJoinWaves) {
+        const Head *h = heads + ((int64_t)p * B + b) * stretches;
+        float m = -INFINITY;
+        for (int i = lane; i < stretches; i += kWave) m = fmaxf(m, h[i].top);
+        m = wave_max(m);
+        double s = 0.0;
+        for (int i = lane; i < stretches; i += kWave) s += h[i].top == -INFINITY ? (double)h[i].sum : (double)h[i].sum * exp((double)h[i].top - (double)m);
+        s = wave_sum(s);
+        const double lse = (double)m + log(s);
+        if (lane == 0) lses[(int64_t)p * B + b] = isfinite(lse) && isfinite(scores[(int64_t)p * B + b]) ? lse : (double)NAN;
+    }
+    __syncthreads();
+    Candidate list = Candidate::none();
+    const int parts = B * stretches;
+    for (int i = w; i < parts; i += kJoinWaves) {
+        const int b = i / stretches;
+        const Key k = lane < n_out ? keys[((int64_t)p * parts + i) * n_out + lane] : Key::none();
+        const double lse = lses[(int64_t)p * B + b];
+        if (lse != lse) continue;
+        Candidate c = Candidate::none();
+        if (k.value) {
+            const uint64_t v = ord64((double)scores[(int64_t)p * B + b] + ((double)key_value(k.value) - lse));
+            c = {(uint32_t)(v >> 32), (uint32_t)v, ~((uint32_t)b * (uint32_t)V + ~k.token)};
+        }
+        if (of_lane(c, 0) > of_lane(list, n_out - 1)) list = joined(list, c);
+    }
+    lists[w][lane] = list;
+    for (int half = kJoinWaves / 2; half > 0; half /= 2) {
+        __syncthreads();
+        if (w < half) {
+            list = joined(list, lists[w + half][lane]);
+            lists[w][lane] = list;
+        }
+    }
+    if (tid < n_out) {
+        const bool none = list.value() == 0ull;
+        const uint32_t at = ~list.at;
+        out_scores[(int64_t)p * n_out + tid] = none ? -INFINITY : (float)value64(list.value());
+        out_beams[(int64_t)p * n_out + tid] = none ? -1 : (int32_t)(at / (uint32_t)V);
+        out_tokens[(int64_t)p * n_out + tid] = none ? -1 : (int32_t)(at % (uint32_t)V);
+    }
+}
+
+// Long stretches where there are enough of them to fill the chip: fewer lists to join.
+int logits_of_thread(const nkv_beams &s) { return (int64_t)s.n_prompts * s.n_beams * ((s.vocab + kThreads * 32 - 1) / (kThreads * 32)) >= 1024 ? 32 : 8; }
+int stretches_of(const nkv_beams &s)
+{
+    const int at_once = kThreads * logits_of_thread(s);
+    return (int)(((int64_t)s.vocab + at_once - 1) / at_once);
+}
+size_t up(size_t x) { return (x + 255) / 256 * 256; }
+
+}  // namespace
+
+bool beam_one_launch(const nkv_beams &s) { return (int64_t)s.n_prompts * s.n_beams < (1 << 24) && (int64_t)s.n_prompts * s.n_beams * stretches_of(s) < (1 << 24); }
+
+size_t beam_ws_bytes(const nkv_beams &s)
+{
+    const size_t rows = (size_t)s.n_prompts * s.n_beams, parts = rows * stretches_of(s);
+    return up(rows * sizeof(double)) + up(parts * sizeof(Head)) + parts * s.n_out * sizeof(Key);
+}
+
+hipError_t launch_beam_select(const nkv_beams &s, float *out_scores, int32_t *out_beams, int32_t *out_tokens, void *ws, hipStream_t st)
+{
+    const size_t rows = (size_t)s.n_prompts * s.n_beams;
+    const int stretches = stretches_of(s);
+    double *lses = (double *)ws;
+    Head *heads = (Head *)((char *)ws + up(rows * sizeof(double)));
+    Key *keys = (Key *)((char *)heads + up(rows * stretches * sizeof(Head)));
+    const ScanArgs a{s.logits, s.strides[0], s.strides[1], s.n_beams, s.vocab, s.n_out, stretches, heads, keys};
+    const unsigned grid = (unsigned)(rows * stretches);
+    auto go = [&](auto type) {
+        using T = decltype(type);
+        if (logits_of_thread(s) == 32) beam_scan_kernel<T, 32><<<grid, kThreads, 0, st>>>(a);
+        else beam_scan_kernel<T, 8><<<grid, kThreads, 0, st>>>(a);
+    };
+    if (s.dtype == NKV_DTYPE_F32) go(float{});
+    else if (s.dtype == NKV_DTYPE_F16) go(f16_t{});
+    else go(uint16_t{});
+    beam_join_kernel<<<(unsigned)s.n_prompts, kJoin, 0, st>>>(heads, keys, s.scores, s.n_beams, s.vocab, s.n_out, stretches, lses, out_scores, out_beams,
+                                                              out_tokens);
+    return hipGetLastError();
+}
+
+}  // namespace nkv

@@ -177,6 +177,15 @@ size_t pages_ws_bytes(const nkv_pages &p, int n_q_heads, int n_new);
 hipError_t launch_pages_attention(const void *q, const nkv_pages &p, int n_q_heads, int n_new, double scale, float *out, float *lse,
                                   void *ws, hipStream_t st);
 
+hipError_t launch_pages_copy(const int32_t *src, const int32_t *dst, int64_t n, const nkv_pages &p, hipStream_t st);
+hipError_t launch_pages_compact(const int32_t *kept_idx, const int64_t *head_off, int64_t rows, const nkv_pages &from, const nkv_pages &to,
+                                hipStream_t st);
+
+// ---- beam search ----
+size_t beam_ws_bytes(const nkv_beams &s);
+bool beam_one_launch(const nkv_beams &s);
+hipError_t launch_beam_select(const nkv_beams &s, float *out_scores, int32_t *out_beams, int32_t *out_tokens, void *ws, hipStream_t st);
+
 // ---- plain copy, the bandwidth yardstick ----
 hipError_t launch_copy_probe(void *dst, const void *src, size_t bytes, hipStream_t st);
 

@@ -1,7 +1,7 @@
 // Rows into and out of the paged cache: new tokens, rotated on the way (nkv_pages_append), and the packed rows that the
-// compression operator leaves (nkv_pages_load, nkv_pages_read).
+// compression operator leaves (nkv_pages_load, nkv_pages_read); from page to page: whole ones (nkv_pages_copy), and the rows that stay (nkv_pages_compact).
 //
-// All three move each byte once and compute little: 16-byte loads, one thread for eight dims of a row.  A block of the 4-bit format is
+// All of them move each byte once and compute little: 16-byte loads, one thread for eight dims of a row.  A block of the 4-bit format is
 // 32 dims, so four neighbouring lanes find its scale among themselves.
 #include "nkv_pages.h"
 
@@ -253,6 +253,94 @@ __global__ __launch_bounds__(2 * D) void rows_kernel(uint16_t *__restrict__ pk, 
     }
 }
 
+// Rows of one table's pages to the front of another's, bit by bit.  A workgroup takes one page of the new ones, numbered as in rows_kernel: 16 rows at a
+// time, D / 8 threads a row, everything that four rows a thread need asked for at once.  Bound by memory: a row's bytes are read and written once; what
+// a row of 4 bits shares with its neighbours (V's codes, the scales) is there for those that are kept too.
+template <int D, bool FP4>
+__global__ __launch_bounds__(2 * D) void compact_kernel(const int32_t *__restrict__ kept_idx, const int64_t *__restrict__ head_off, int64_t rows, int n_units,
+                                                        const uint8_t *from_pool, const int32_t *__restrict__ from_table, const int32_t *__restrict__ from_lens,
+                                                        int from_pages, int from_max, uint8_t *pool, const int32_t *__restrict__ table, int n_pages, int max_pages)
+{
+    constexpr int CPR = D / 8;
+    constexpr int64_t kBytes = FP4 ? Fp4Page<D>::kBytes : WidePage<D>::kBytes;
+    const Span sp = span_of(head_off, from_lens, n_units, rows, from_max, blockIdx.x);
+    const int64_t j = blockIdx.x - sp.number;
+    if (j * kRows >= sp.n || j >= max_pages) return;
+    const int id = table[(int64_t)sp.unit * max_pages + j];
+    if (id < 0 || id >= n_pages) return;
+    uint8_t *page = pool + id * kBytes;
+    const int c = threadIdx.x % CPR, r = threadIdx.x / CPR, count = (int)min(sp.n - j * kRows, (int64_t)kRows);
+    const uint8_t *src[4];
+    int at[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) at[t] = kept_idx[sp.off + j * kRows + min(16 * t + r, count - 1)];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        const bool row = at[t] >= 0 && at[t] < sp.len;
+        const int p = row ? from_table[(int64_t)sp.unit * from_max + at[t] / kRows] : -1;
+        src[t] = p >= 0 && p < from_pages ? from_pool + p * kBytes : nullptr;
+        at[t] &= kRows - 1;
+    }
+    if constexpr (FP4) {
+        using P = Fp4Page<D>;
+        uint32_t k[4], v[4];
+        uint8_t ks[4], vs[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            k[t] = v[t] = 0u, ks[t] = vs[t] = 1;                           // (zeros as they are appended)
+            if (!src[t]) continue;
+            k[t] = *reinterpret_cast<const uint32_t *>(src[t] + P::k_code(at[t], 8 * c));
+            v[t] = load_v_codes<D>(src[t], at[t], c);
+            ks[t] = src[t][P::k_scale(at[t], c / 4)], vs[t] = src[t][P::v_scale(at[t], c / 4)];
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int row = 16 * t + r;
+            if (row >= count) break;
+            *reinterpret_cast<uint32_t *>(page + P::k_code(row, 8 * c)) = k[t];
+            store_v_codes<D>(page, row, c, v[t]);
+            if (c % 4 == 0) page[P::k_scale(row, c / 4)] = ks[t], page[P::v_scale(row, c / 4)] = vs[t];
+        }
+    } else {
+        using P = WidePage<D>;
+        u32x4 k[4], v[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            k[t] = v[t] = u32x4{0u, 0u, 0u, 0u};
+            if (!src[t]) continue;
+            k[t] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(src[t] + P::k(at[t], 8 * c)));
+            v[t] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(src[t] + P::v(at[t], 8 * c)));
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int row = 16 * t + r;
+            if (row >= count) break;
+            *reinterpret_cast<u32x4 *>(page + P::k(row, 8 * c)) = k[t];
+            *reinterpret_cast<u32x4 *>(page + P::v(row, 8 * c)) = v[t];
+        }
+    }
+}
+
+// grid: `pieces` workgroups a page, a thread U loads at once.
+constexpr int kCopyAtOnce = 4;
+__global__ __launch_bounds__(256) void copy_pages_kernel(const int32_t *__restrict__ src, const int32_t *__restrict__ dst, int pieces, int words, int n_pages,
+                                                         u32x4 *pool)
+{
+    const int i = blockIdx.x / pieces, piece = blockIdx.x - i * pieces, from = src[i], to = dst[i];
+    if (from < 0 || from >= n_pages || to < 0 || to >= n_pages || from == to) return;
+    const u32x4 *a = pool + (int64_t)from * words;
+    u32x4 *b = pool + (int64_t)to * words;
+    u32x4 x[kCopyAtOnce];
+    for (int at = piece * (256 * kCopyAtOnce) + threadIdx.x; at < words; at += pieces * (256 * kCopyAtOnce)) {
+#pragma unroll
+        for (int k = 0; k < kCopyAtOnce; ++k)
+            if (at + 256 * k < words) x[k] = a[at + 256 * k];
+#pragma unroll
+        for (int k = 0; k < kCopyAtOnce; ++k)
+            if (at + 256 * k < words) b[at + 256 * k] = x[k];
+    }
+}
+
 }  // namespace
 
 bool pages_row_supported(int dtype, int d)
@@ -315,6 +403,28 @@ hipError_t launch_pages_rows(bool load, const void *k, const void *v, const int6
         if (p.format != NKV_PAGES_FP4) go(No{}, No{});                      // 16-bit rows are copied as they are
         else if (p.dtype == NKV_DTYPE_F16) go(Yes{}, Yes{});
         else go(No{}, Yes{});
+    });
+    return hipGetLastError();
+}
+
+hipError_t launch_pages_copy(const int32_t *src, const int32_t *dst, int64_t n, const nkv_pages &p, hipStream_t st)
+{
+    if (n == 0) return hipSuccess;
+    const int words = (int)(page_bytes_of(p.d, p.format) / 16), pieces = std::min(4, (words + 256 * kCopyAtOnce - 1) / (256 * kCopyAtOnce));
+    copy_pages_kernel<<<(unsigned)(n * pieces), 256, 0, st>>>(src, dst, pieces, words, p.n_pages, (u32x4 *)p.pool);
+    return hipGetLastError();
+}
+
+hipError_t launch_pages_compact(const int32_t *kept_idx, const int64_t *head_off, int64_t rows, const nkv_pages &from, const nkv_pages &to, hipStream_t st)
+{
+    if (rows == 0) return hipSuccess;
+    const int n_units = to.n_seqs * to.H;
+    const unsigned groups = (unsigned)(rows / kRows + 2 * (int64_t)n_units);
+    for_head_dim(to.d, [&](auto dim) {
+        constexpr int D = decltype(dim)::value;
+        (to.format == NKV_PAGES_FP4 ? compact_kernel<D, true> : compact_kernel<D, false>)<<<groups, 2 * D, 0, st>>>(
+            kept_idx, head_off, rows, n_units, (const uint8_t *)from.pool, from.table, from.lens, from.n_pages, from.max_pages, (uint8_t *)to.pool, to.table,
+            to.n_pages, to.max_pages);
     });
     return hipGetLastError();
 }
