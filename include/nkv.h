@@ -412,6 +412,34 @@ int nkv_pages_attention(const void *q, const nkv_pages *pages, int32_t n_q_heads
                         float *lse, void *ws, size_t ws_bytes, void *hip_stream);
 
 /*
+ * The same attention for as many tokens as there are, a prompt's chunk or one, with rules for the logits and the output in the rows' type.  Token t stands on
+ * row r = lens[u] - n_new + t of its unit and sees the rows i <= r, of those with a window w > 0 the ones with i > r - w, and whatever r and the window the
+ * rows i < prefix[s] (of lens[u]); a token with r < 0 sees nothing.
+ *   z_i = scale * <q, k_i>, capped to cap * tanh(z_i / cap) where cap > 0, less slopes[h * G + g] * |r - i|
+ *   out[s][t][h*G+g] = sum_i softmax(z)_i * v_i      in `dtype`, dense [n_seqs][n_new][n_q_heads][d]
+ *   lse[s][t][h*G+g] = log sum_i exp(z_i)            (optional, may be NULL)   fp32 [n_seqs][n_new][n_q_heads]
+ * rules may be NULL: every row i <= r, logits as they are.  A token that sees no row gets out = 0, lse = -inf.  A row that a token does not see has no effect on it,
+ * whatever it holds; one whose value holds an infinity or NaN gives NaN (infinity where all tokens of some columns see it) to those that do.
+ * Keys' products are exact and added up in fp32, as is the sum of the weights.  A weight is rounded to 16 bits for its product with the values: bf16's 8 bits for bf16
+ * rows, fp16's 11 for fp16 rows (two pieces of bf16 on 4-bit pages), so an output is off by that much of its largest terms at most, as its own rounding is.
+ * scale as for nkv_pages_attention; NKV_EINVAL for a negative or NaN cap, and one that, or whose quotient with the scale, is not within 1e-30 and fp32's range;
+ * slopes are finite.
+ * Scratch: nkv_pages_prompt_workspace_bytes, 0 where the columns fill the chip (ws may be NULL then), some 35 MiB at most for heads of 128 dims where the rows are shared out.
+ * NKV_ESHAPE from 2^30 columns (n_new * G) of a unit, and 2^23 pieces of 128 columns of all units, on.  Deterministic.
+ */
+typedef struct nkv_logit_rules {
+    uint32_t struct_size;     /* sizeof(nkv_logit_rules)                              */
+    int32_t  window;          /* rows that a token sees, its own among them; 0: all   */
+    double   cap;             /* 0: none                                              */
+    const float   *slopes;    /* DEVICE, [n_q_heads]; NULL: none                      */
+    const int32_t *prefix;    /* DEVICE, [n_seqs], clamped to [0, lens]; NULL: none   */
+} nkv_logit_rules;
+
+int nkv_pages_prompt_workspace_bytes(const nkv_pages *pages, int32_t n_q_heads, int32_t n_new, size_t *bytes);
+int nkv_pages_prompt_attention(const void *q, const nkv_pages *pages, const nkv_logit_rules *rules, int32_t n_q_heads, int32_t n_new, double scale,
+                               void *out, float *lse, void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
  * Copies whole pages inside the pool, page src[i] to page dst[i] (device, i < n): a sequence that continues another one shares
  * the other's full pages and gets copies of those that it will write.  Pairs of which one is outside [0, n_pages) are left out.  No page is
  * in dst twice or in both dst and src, but where src[i] = dst[i]: such pages' contents are undefined afterwards.  table and lens are not read.

@@ -37,7 +37,7 @@ MAX_BEAMS_OUT = 64
 EXPORTS = ("nkv_params_default", "nkv_block_size", "nkv_k0", "nkv_m_safe", "nkv_m_p", "nkv_packed_rows",
            "nkv_workspace_bytes", "nkv_score", "nkv_score_raw", "nkv_budget", "nkv_budget_noalloc", "nkv_select_compact",
            "nkv_decode_workspace_bytes", "nkv_decode_attention", "nkv_page_bytes", "nkv_pages_append", "nkv_pages_load",
-           "nkv_pages_read", "nkv_pages_workspace_bytes", "nkv_pages_attention", "nkv_pages_copy", "nkv_pages_compact",
+           "nkv_pages_read", "nkv_pages_workspace_bytes", "nkv_pages_attention", "nkv_pages_prompt_workspace_bytes", "nkv_pages_prompt_attention", "nkv_pages_copy", "nkv_pages_compact",
            "nkv_beam_workspace_bytes", "nkv_beam_select", "nkv_copy_probe", "nkv_strerror", "nkv_version")
 KERNELS = ("scan", "finalize", "budget", "select", "gather", "decode")
 PASS_KERNELS = KERNELS[:5]          # the kernels of the compression pass itself
@@ -72,6 +72,10 @@ class nkv_tokens(C.Structure):
                 ("q", C.c_void_p), ("q_out", C.c_void_p), ("k_strides", C.c_int64 * 3),
                 ("v_strides", C.c_int64 * 3), ("q_strides", C.c_int64 * 3), ("positions", C.c_void_p),
                 ("rope", C.c_void_p)]
+
+
+class nkv_logit_rules(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("window", C.c_int32), ("cap", C.c_double), ("slopes", C.c_void_p), ("prefix", C.c_void_p)]
 
 
 class nkv_beams(C.Structure):
@@ -131,6 +135,9 @@ def lib() -> C.CDLL:
         L.nkv_pages_workspace_bytes.argtypes = [C.POINTER(nkv_pages), C.c_int32, C.c_int32, C.POINTER(C.c_size_t)]
         L.nkv_pages_attention.argtypes = [vp, C.POINTER(nkv_pages), C.c_int32, C.c_int32, f64, vp, vp, vp,
                                           C.c_size_t, vp]
+        L.nkv_pages_prompt_workspace_bytes.argtypes = [C.POINTER(nkv_pages), C.c_int32, C.c_int32, C.POINTER(C.c_size_t)]
+        L.nkv_pages_prompt_attention.argtypes = [vp, C.POINTER(nkv_pages), C.POINTER(nkv_logit_rules), C.c_int32, C.c_int32, f64, vp, vp, vp,
+                                                 C.c_size_t, vp]
         L.nkv_pages_copy.argtypes = [vp, vp, i64, C.POINTER(nkv_pages), vp]
         L.nkv_pages_compact.argtypes = [vp, vp, i64, C.POINTER(nkv_pages), C.POINTER(nkv_pages), vp]
         L.nkv_beam_workspace_bytes.argtypes = [C.POINTER(nkv_beams), C.POINTER(C.c_size_t)]
@@ -517,6 +524,61 @@ def pages_attention(q, pages: Pages, n_q_heads: int, n_new: int, scale: float, o
                                    0 if lse is None else lse.data_ptr(), ws_at, ws_bytes, _stream(stream))
     if rc:
         raise NkvError(rc, "nkv_pages_attention")
+
+
+class LogitRules:
+    """Rules for the logits of ``pages_prompt_attention``, as ``nkv_logit_rules`` in nkv.h describes them: ``cap`` (0: none), ``window`` (0: none), ``slopes``
+    fp32 [n_q_heads] and ``prefix`` int32 [n_seqs] on the device, or None."""
+
+    def __init__(self, cap: float = 0.0, window: int = 0, slopes=None, prefix=None):
+        import torch
+        for t, what, dtype in ((slopes, "slopes", torch.float32), (prefix, "prefix", torch.int32)):
+            if t is not None and (t.dtype is not dtype or t.dim() != 1 or not t.is_contiguous()):
+                raise ValueError(f"{what} is contiguous {dtype} of one dim")
+        if not cap >= 0.0 or window < 0:
+            raise ValueError("cap and window are not negative")
+        self.cap, self.window, self.slopes, self.prefix = float(cap), int(window), slopes, prefix
+        self.c = nkv_logit_rules(C.sizeof(nkv_logit_rules), self.window, self.cap, _ptr(slopes), _ptr(prefix))
+        self.ref = C.byref(self.c)
+
+
+def pages_prompt_workspace_bytes(pages: Pages, n_q_heads: int, n_new: int) -> int:
+    """Scratch of ``pages_prompt_attention``; 0 where it needs none."""
+    out = C.c_size_t(0)
+    rc = lib().nkv_pages_prompt_workspace_bytes(pages.ref, int(n_q_heads), int(n_new), C.byref(out))
+    if rc:
+        raise NkvError(rc, "nkv_pages_prompt_workspace_bytes")
+    return int(out.value)
+
+
+def pages_prompt_attention(q, pages: Pages, n_q_heads: int, n_new: int, scale: float, out, lse=None, ws=None, rules: Optional[LogitRules] = None,
+                           stream=None) -> None:
+    """The last n_new tokens' attention over the pages, a prompt's chunk or single tokens, by ``rules``: q [n_seqs, n_new, Hq, d] -> out of that shape and type
+    (and lse fp32 [n_seqs, n_new, Hq]); see ``nkv_pages_prompt_attention`` in nkv.h."""
+    shape = (pages.n_seqs, n_new, n_q_heads, pages.d)
+    _check_rows(q, "q", pages, shape)
+    _check_rows(out, "out", pages, shape)
+    if lse is not None:
+        _check_dense(lse, "lse", pages, pages.torch_f32, pages.n_seqs * n_new * n_q_heads)
+    rules_at = None
+    if rules is not None:
+        rules_at = rules.ref
+        if rules.slopes is not None:
+            _check_dense(rules.slopes, "slopes", pages, pages.torch_f32, n_q_heads)
+        if rules.prefix is not None:
+            _check_dense(rules.prefix, "prefix", pages, pages.torch_i32, pages.n_seqs)
+    ws_at = ws_bytes = 0
+    if ws is not None:
+        if not ws.is_contiguous():
+            raise ValueError("ws is contiguous")
+        if ws.get_device() != pages.index:
+            raise _elsewhere(ws, "ws", pages)
+        ws_at, ws_bytes = ws.data_ptr(), ws.nbytes
+    _check_gpu(pages)
+    rc = lib().nkv_pages_prompt_attention(q.data_ptr(), pages.ref, rules_at, int(n_q_heads), int(n_new), float(scale), out.data_ptr(),
+                                          0 if lse is None else lse.data_ptr(), ws_at, ws_bytes, _stream(stream))
+    if rc:
+        raise NkvError(rc, "nkv_pages_prompt_attention")
 
 
 def pages_copy(src, dst, pages: Pages, stream=None) -> None:

@@ -291,6 +291,27 @@ int check_attention(const nkv_pages *pages, int32_t n_q_heads, int32_t n_new)
     return NKV_OK;
 }
 
+int check_prompt(const nkv_pages *pages, int32_t n_q_heads, int32_t n_new)
+{
+    const int rc = check_pages(pages);
+    if (rc) return rc;
+    if (n_new < 1 || n_q_heads < pages->H || n_q_heads % pages->H) return NKV_EINVAL;
+    return pages_prompt_one_launch(*pages, n_q_heads, n_new) ? NKV_OK : NKV_ESHAPE;
+}
+
+// A cap's quotient with the scale, and what it stands for in powers of two, are finite and not zero in 32 bits (a scale of zero aside).
+int check_rules(const nkv_logit_rules *r, double scale)
+{
+    if (!isfinite(pages_scale(scale))) return NKV_EINVAL;
+    if (!r) return NKV_OK;
+    if (r->struct_size != sizeof(nkv_logit_rules) || r->window < 0 || !(r->cap >= 0) || (uintptr_t)r->slopes % 4 || (uintptr_t)r->prefix % 4) return NKV_EINVAL;
+    if (r->cap > 0) {
+        const float c = pages_scale(r->cap), x = (float)(fabs(scale) / r->cap);
+        if (!isfinite(c) || !isfinite(x) || c < 1e-30f || (pages_scale(scale) != 0.f && x < 1e-30f)) return NKV_EINVAL;
+    }
+    return NKV_OK;
+}
+
 int check_beams(const nkv_beams *s)
 {
     if (!s || s->struct_size != sizeof(nkv_beams)) return NKV_EINVAL;
@@ -619,6 +640,28 @@ int nkv_pages_attention(const void *q, const nkv_pages *pages, int32_t n_q_heads
     rc = check_ws(ws, ws_bytes, pages_ws_bytes(*pages, n_q_heads, n_new));
     if (rc) return rc;
     return launch_pages_attention(q, *pages, n_q_heads, n_new, scale, out, lse, ws, (hipStream_t)hip_stream) == hipSuccess ? NKV_OK : NKV_EHIP;
+}
+
+int nkv_pages_prompt_workspace_bytes(const nkv_pages *pages, int32_t n_q_heads, int32_t n_new, size_t *bytes)
+{
+    if (!bytes) return NKV_EINVAL;
+    const int rc = check_prompt(pages, n_q_heads, n_new);
+    if (rc) return rc;
+    *bytes = pages_prompt_ws_bytes(*pages, n_q_heads, n_new);
+    return NKV_OK;
+}
+
+int nkv_pages_prompt_attention(const void *q, const nkv_pages *pages, const nkv_logit_rules *rules, int32_t n_q_heads, int32_t n_new, double scale,
+                               void *out, float *lse, void *ws, size_t ws_bytes, void *hip_stream)
+{
+    int rc = check_prompt(pages, n_q_heads, n_new);
+    if (rc) return rc;
+    rc = check_rules(rules, scale);
+    if (rc) return rc;
+    if (!q || !out || (uintptr_t)q % 16 || (uintptr_t)out % 16 || (uintptr_t)lse % 4) return NKV_EINVAL;
+    rc = check_ws(ws, ws_bytes, pages_prompt_ws_bytes(*pages, n_q_heads, n_new));
+    if (rc) return rc;
+    return launch_pages_prompt(q, *pages, rules, n_q_heads, n_new, scale, out, lse, ws, (hipStream_t)hip_stream) == hipSuccess ? NKV_OK : NKV_EHIP;
 }
 
 int nkv_pages_copy(const int32_t *src, const int32_t *dst, int64_t n, const nkv_pages *pages, void *hip_stream)

@@ -177,6 +177,10 @@ size_t pages_ws_bytes(const nkv_pages &p, int n_q_heads, int n_new);
 hipError_t launch_pages_attention(const void *q, const nkv_pages &p, int n_q_heads, int n_new, double scale, float *out, float *lse,
                                   void *ws, hipStream_t st);
 
+bool pages_prompt_one_launch(const nkv_pages &p, int n_q_heads, int n_new);
+size_t pages_prompt_ws_bytes(const nkv_pages &p, int n_q_heads, int n_new);
+hipError_t launch_pages_prompt(const void *q, const nkv_pages &p, const nkv_logit_rules *rules, int n_q_heads, int n_new, double scale, void *out, float *lse,
+                               void *ws, hipStream_t st);
 hipError_t launch_pages_copy(const int32_t *src, const int32_t *dst, int64_t n, const nkv_pages &p, hipStream_t st);
 hipError_t launch_pages_compact(const int32_t *kept_idx, const int64_t *head_off, int64_t rows, const nkv_pages &from, const nkv_pages &to,
                                 hipStream_t st);

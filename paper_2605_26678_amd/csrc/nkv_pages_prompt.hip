@@ -1,0 +1,63 @@
+// nkv_pages_prompt_attention: which kernel takes a call.
+#include "nkv_pages_prompt.h"
+
+#include <algorithm>
+
+namespace nkv {
+namespace {
+
+struct Grid {
+    int tiles, splits;                   // workgroups of a unit: tiles of columns, and shares of the rows that one sees
+};
+// A compute unit holds one workgroup.  Where the tiles are few, the rows are shared out too, until there is one for (nearly) every compute unit.
+Grid grid_of(const nkv_pages &p, int n_q_heads, int n_new)
+{
+    const int64_t cols = (int64_t)(n_q_heads / p.H) * n_new, at_once = 32 * prompt_waves(p.d, p.dtype == NKV_DTYPE_F16 && p.format == NKV_PAGES_FP4);
+    const int64_t tiles = (cols + at_once - 1) / at_once, groups = (int64_t)p.n_seqs * p.H * tiles;
+    return {(int)tiles, (int)std::max<int64_t>(1, std::min<int64_t>(256 / groups, p.max_pages / 2))};
+}
+
+}  // namespace
+
+bool pages_prompt_one_launch(const nkv_pages &p, int n_q_heads, int n_new)
+{
+    // fewer than 2^32 threads: 512 a workgroup of the products, and a thread for four dims of a column where parts are joined
+    const int64_t units = (int64_t)p.n_seqs * p.H, cols = (int64_t)(n_q_heads / p.H) * n_new;
+    if (cols >= (1 << 30) || units * ((cols + 127) / 128) >= (1 << 23)) return false;
+    return true;
+}
+
+size_t pages_prompt_ws_bytes(const nkv_pages &p, int n_q_heads, int n_new)
+{
+    const Grid g = grid_of(p, n_q_heads, n_new);
+    return g.splits == 1 ? 0 : (size_t)g.splits * p.n_seqs * (n_q_heads * (size_t)n_new) * (p.d + 4) * sizeof(float);
+}
+
+hipError_t launch_pages_prompt(const void *q, const nkv_pages &p, const nkv_logit_rules *rules, int n_q_heads, int n_new, double scale, void *out, float *lse,
+                               void *ws, hipStream_t st)
+{
+    PromptArgs a{};
+    a.q = (const uint16_t *)q, a.pool = (const uint8_t *)p.pool, a.table = p.table, a.lens = p.lens;
+    a.n_units = p.n_seqs * p.H, a.H = p.H, a.G = n_q_heads / p.H, a.n_new = n_new, a.n_pages = p.n_pages, a.max_pages = p.max_pages;
+    a.scale_log2 = pages_scale(scale);
+    a.flat = a.scale_log2 == 0.f;
+    if (a.flat) a.scale_log2 = 1.f;
+    a.flip = scale < 0 ? 0x80008000u : 0u;
+    if (rules) {
+        a.window = rules->window, a.slopes = rules->slopes, a.prefix = rules->prefix;
+        if (rules->cap > 0) a.cap_log2 = pages_scale(rules->cap), a.over_cap = a.flat ? 1.f : (float)(fabs(scale) / rules->cap);
+        a.bent = rules->cap > 0 || rules->slopes;
+    }
+    a.out = (uint16_t *)out, a.lse = lse, a.part = (float *)ws;
+    const Grid g = grid_of(p, n_q_heads, n_new);
+    a.tiles = g.tiles, a.splits = g.splits;
+    switch (p.d) {
+    case 64: return launch_prompt_tiles<64>(a, p, st);
+    case 96: return launch_prompt_tiles<96>(a, p, st);
+    case 128: return launch_prompt_tiles<128>(a, p, st);
+    case 192: return launch_prompt_tiles<192>(a, p, st);
+    default: return launch_prompt_tiles<256>(a, p, st);
+    }
+}
+
+}  // namespace nkv

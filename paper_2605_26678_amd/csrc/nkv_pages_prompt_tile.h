@@ -1,0 +1,416 @@
+// The kernel of nkv_pages_prompt_attention for a prompt's chunk, instantiated a head dim at a time.
+//
+// With many columns the two products of 4 d operations a row and column are what it takes: they go through the matrix cores, 32 rows or dims x 32
+// columns x 16 at a time, with
+//   S = K Q^T     rows x columns, so that a lane holds 32 rows' logits of one column: maximum and sum in the lane, and one exchange with lane ^ 32
+//   O^T = V^T P   dims x columns: the rows that a lane holds of S are those that the product takes from it as P, in that order; V's columns come from LDS
+//                 transposed by the load (ds_read_b64_tr_b16)
+// A workgroup takes kWaves x 32 columns of a unit, and walks over the pages that they see: a page is a tile of 64 rows, held twice in LDS, the next one on its way
+// in registers (4-bit rows become 16-bit ones there, once for all columns).  K's products are exact; a weight is rounded to the rows' 16 bits, off by half
+// a step of the type that the output is rounded to, and the sum that divides is that of the unrounded ones in fp32.  fp16 rows of 4-bit pages are outside of fp16's range
+// where their scales are: they become bf16, exactly, and queries and weights are two pieces of bf16 then.
+#pragma once
+
+#include "nkv_pages_prompt.h"
+
+#include <algorithm>
+
+namespace nkv {
+namespace {
+
+using f32x16 = float __attribute__((ext_vector_type(16)));
+using f32x4 = float __attribute__((ext_vector_type(4)));
+using bf16x8 = __bf16 __attribute__((ext_vector_type(8)));
+using f16x8 = _Float16 __attribute__((ext_vector_type(8)));
+using i16x4 = short __attribute__((ext_vector_type(4)));
+
+template <int D, bool F16, bool FP4> struct Tile {
+    static constexpr int kWaves = prompt_waves(D, F16 && FP4), kThreads = kWaves * 64, kCols = kWaves * 32;
+    static constexpr bool kTwo = F16 && FP4;                              // two pieces
+    static constexpr bool kHalf = F16 && !FP4;                            // the products' type is fp16
+    static constexpr int kCpr = D / 8;                                    // 16-byte chunks of a row
+    static constexpr int kStride = (D == 96 ? 128 : D) * 2;               // bytes of a row in LDS
+    static constexpr int kMatrix = kRows * kStride;
+    static constexpr int kItems = (kRows * kCpr + kThreads - 1) / kThreads;   // chunks a thread moves of K, and of V
+    static constexpr bool kEven = kRows * kCpr % kThreads == 0;
+    // fp16 weights of up to 2^(6 + 8), see kRoom: those of 2^-30 of the largest one still have all of their bits
+    static constexpr float kShift = kHalf ? 6.f : 0.f;
+};
+// A column's maximum is only moved when a logit is more than this above it (in powers of two): weights of up to 2^8 have the bits that those of up to 1 have, and
+// the weighted values in their registers are seldom multiplied.
+constexpr float kRoom = 8.f;
+
+// Chunk c of a row lies at c ^ that: eight rows' same chunk of K, and the four rows by two chunks of V that 16 lanes transpose, are in different banks.
+__device__ __forceinline__ int k_swizzle(int row) { return row & 7; }
+template <int STRIDE> __device__ __forceinline__ int v_swizzle(int row)
+{
+    const int a = row & 3;
+    return STRIDE % 256 == 0 ? 4 * a ^ (a & 2) : 4 * (a & 1) ^ (a & 2);
+}
+
+template <bool HALF> __device__ __forceinline__ f32x16 product32(const u32x4 &a, const u32x4 &b, const f32x16 &c)
+{
+    if constexpr (HALF) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// A page on its way to LDS.
+template <int D, bool F16, bool FP4> struct Stage {
+    using T = Tile<D, F16, FP4>;
+    uint32_t k[T::kItems][FP4 ? 1 : 4], v[T::kItems][FP4 ? 1 : 4];
+    uint8_t ks[T::kItems], vs[T::kItems];
+
+    __device__ __forceinline__ void load(const uint8_t *__restrict__ page, int tid)
+    {
+#pragma unroll
+        for (int i = 0; i < T::kItems; ++i) {
+            const int idx = i * T::kThreads + tid;
+            if (!T::kEven && idx >= kRows * T::kCpr) break;
+            const int row = idx / T::kCpr, c = idx - row * T::kCpr;
+            if constexpr (FP4) {
+                using P = Fp4Page<D>;
+                k[i][0] = *reinterpret_cast<const uint32_t *>(page + P::k_code(row, 8 * c));
+                v[i][0] = load_v_codes<D>(page, row, c);
+                ks[i] = page[P::k_scale(row, c / 4)], vs[i] = page[P::v_scale(row, c / 4)];
+            } else {
+                using P = WidePage<D>;
+                const u32x4 x = *reinterpret_cast<const u32x4 *>(page + P::k(row, 8 * c)), y = *reinterpret_cast<const u32x4 *>(page + P::v(row, 8 * c));
+#pragma unroll
+                for (int w = 0; w < 4; ++w) k[i][w] = x[w], v[i][w] = y[w];
+            }
+        }
+    }
+    // valid: rows that are there; V's others become zeros, since 0 times NaN is NaN.  ODD: some columns do not see all of the rows, so infinities and NaN among V
+    // become zeros as well, and their rows' bits are set in `odd`: the columns that do see them get a NaN for a logit.
+    template <bool ODD> __device__ __forceinline__ void store(uint8_t *lds_k, uint8_t *lds_v, int tid, int valid, uint32_t *odd) const
+    {
+#pragma unroll
+        for (int i = 0; i < T::kItems; ++i) {
+            const int idx = i * T::kThreads + tid;
+            if (!T::kEven && idx >= kRows * T::kCpr) break;
+            const int row = idx / T::kCpr, c = idx - row * T::kCpr;
+            u32x4 x, y;
+            if constexpr (FP4) {
+                x = codes(k[i][0], ks[i]);
+                y = codes(v[i][0], vs[i]);
+            } else {
+#pragma unroll
+                for (int w = 0; w < 4; ++w) x[w] = k[i][w], y[w] = v[i][w];
+            }
+            if constexpr (ODD) {
+                constexpr uint32_t e = T::kHalf ? 0x7c00u : 0x7f80u;
+                bool found = false;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const bool lo = (y[w] & e) == e, hi = (y[w] >> 16 & e) == e;
+                    found |= lo || hi;
+                    y[w] = (lo ? 0u : y[w] & 0xffffu) | (hi ? 0u : y[w] & 0xffff0000u);
+                }
+                if (row >= valid) y = u32x4{0u, 0u, 0u, 0u};
+                else if (found) atomicOr(odd + row / 32, 1u << row % 32);
+            }
+            *reinterpret_cast<u32x4 *>(lds_k + row * T::kStride + (c ^ k_swizzle(row)) * 16) = x;
+            *reinterpret_cast<u32x4 *>(lds_v + row * T::kStride + (c ^ v_swizzle<T::kStride>(row)) * 16) = y;
+        }
+    }
+    __device__ __forceinline__ static u32x4 codes(uint32_t w, uint8_t scale)
+    {
+        const float s = __uint_as_float((uint32_t)scale << 23);
+        return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3))};
+    }
+};
+
+__device__ __forceinline__ float other_half(float x)                      // of lane ^ 32
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
+}
+
+// grid: units * tiles * splits.  The unit changes first: a GPU's eight dies take workgroups in turn, so that a die works on few units at a time and finds their pages in its L2.  The
+// last columns, which see the most rows, go first.
+template <int D, bool F16, bool FP4, bool BENT>
+__global__ __launch_bounds__((Tile<D, F16, FP4>::kThreads), (Tile<D, F16, FP4>::kWaves / 4)) void prompt_kernel(const PromptArgs a)
+{
+    using T = Tile<D, F16, FP4>;
+    constexpr int kSteps = D / 16, kDims = D / 32;                        // of a row's products; of V's dims
+    __shared__ __align__(16) uint8_t lds[2][2][T::kMatrix];
+    __shared__ uint32_t odd[3][2];
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 31, g = lane >> 5;
+    int id = blockIdx.x;
+    const int u = id % a.n_units;
+    id /= a.n_units;
+    const int split = id % a.splits, tile = a.tiles - 1 - id / a.splits;
+    const int sq = u / a.H, h = u - sq * a.H, cols = a.n_new * a.G;
+    const int len = rows_of(a.lens[u], a.max_pages), prefix = prefix_of(a, sq, len);
+    const int32_t *table = a.table + (int64_t)u * a.max_pages;
+    // rows that the workgroup's tokens, the wavefront's and the lane's stand on
+    const int col_first = tile * T::kCols, col_last = min(cols, col_first + T::kCols) - 1;
+    const int r_first = len - a.n_new + col_first / a.G, r_last = len - a.n_new + col_last / a.G;
+    const int wcol = col_first + w * 32, wcol_last = min(cols - 1, wcol + 31);
+    const bool works = wcol < cols;
+    const int w_first = len - a.n_new + wcol / a.G, w_last = len - a.n_new + wcol_last / a.G;
+    const int col = wcol + n;
+    const bool there = col < cols;
+    const int token = (there ? col : cols - 1) / a.G, head = (there ? col : cols - 1) - token * a.G, at = len - a.n_new + token;
+    const int since = a.window > 0 ? at - a.window + 1 : 0;               // the first row of the lane's window
+    const int64_t row_out = ((int64_t)sq * a.n_new + token) * a.H * a.G + h * a.G + head;
+
+    const Seen seen = seen_pages(r_first, r_last, a.window, prefix);
+    const int begin = (int)((int64_t)seen.count * split / a.splits), end = (int)((int64_t)seen.count * (split + 1) / a.splits);
+
+    u32x4 q[T::kTwo ? 2 : 1][kSteps];
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+        u32x4 x = there && !a.flat ? *reinterpret_cast<const u32x4 *>(a.q + row_out * D + 16 * s + 8 * g) : u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] ^= a.flip;
+        if constexpr (T::kTwo) {                                          // 11 bits: eight, and the three that are left
+            float v[8], rest[8];
+            unpack8<true>(x, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float cut = __uint_as_float(__float_as_uint(v[i]) & 0xffff0000u);
+                rest[i] = v[i] - cut;
+                v[i] = cut;
+            }
+            q[0][s] = pack8<false>(v);
+            q[1][s] = pack8<false>(rest);
+        } else {
+            q[0][s] = x;
+        }
+    }
+    float m = kNoMax, l = 0.f;
+    f32x16 o[kDims];
+#pragma unroll
+    for (int t = 0; t < kDims; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
+    const float slope = BENT && a.slopes ? a.slopes[h * a.G + head] * kToLog2 : 0.f;
+
+    auto id_of = [&](int step) { return step < end ? table[seen.page(step)] : -1; };
+    auto page_of = [&](int p) { return a.pool + (int64_t)(p >= 0 && p < a.n_pages ? p : 0) * (FP4 ? Fp4Page<D>::kBytes : WidePage<D>::kBytes); };
+    // all rows of a page are seen by all tokens on rows r0 .. r1
+    auto all_seen = [&](int first, int r0, int r1) { return r0 >= 0 && first + kRows <= len && (first + kRows <= prefix || (first + kRows - 1 <= r0 && (a.window <= 0 || first > r1 - a.window))); };
+    auto none_seen = [&](int first, int r0, int r1) { return first >= prefix && (first > r1 || (a.window > 0 && first + kRows - 1 <= r0 - a.window)); };
+
+    Stage<D, F16, FP4> stage;
+    int this_id = id_of(begin), next_id = id_of(begin + 1);
+    auto put = [&](int step) {                                            // the staged page, of that step
+        const int first = seen.page(step) * kRows, half = (step - begin) & 1;
+        uint8_t *const lk = lds[half][0], *const lv = lds[half][1];
+        if (all_seen(first, r_first, r_last)) stage.template store<false>(lk, lv, tid, kRows, nullptr);
+        else stage.template store<true>(lk, lv, tid, len - first, odd[(step - begin) % 3]);
+    };
+    if (tid < 6) odd[tid / 2][tid % 2] = 0u;
+    __syncthreads();
+    if (begin < end) {
+        stage.load(page_of(this_id), tid);
+        put(begin);
+    }
+    __syncthreads();
+    for (int step = begin; step < end; ++step) {
+        const int first = seen.page(step) * kRows, half = (step - begin) & 1;
+        const bool counts = this_id >= 0 && this_id < a.n_pages;
+        this_id = next_id;
+        next_id = id_of(step + 2);
+        if (step + 1 < end) stage.load(page_of(this_id), tid);
+        if (tid < 2) odd[(step - begin + 2) % 3][tid] = 0u;
+        if (counts && works && !none_seen(first, w_first, w_last)) {
+            const uint8_t *const lk = lds[half][0], *const lv = lds[half][1];
+            // ---- S ----
+            f32x16 s[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[t][i] = 0.f;
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k)
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const u32x4 x = *reinterpret_cast<const u32x4 *>(lk + (32 * t + n) * T::kStride + ((2 * k + g) ^ k_swizzle(n)) * 16);
+                    if constexpr (T::kTwo) s[t] = product32<false>(x, q[1][k], s[t]);
+                    s[t] = product32<T::kHalf>(x, q[0][k], s[t]);
+                }
+            float p[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) p[i] = s[i / 16][i % 16];
+            const int base = first + 4 * g;                               // p[i] is of row base + row_at(i)
+            auto row_at = [](int i) { return 32 * (i / 16) + 8 * (i % 16 / 4) + i % 4; };
+            if constexpr (BENT) {
+                bend(p, a.scale_log2, a.cap_log2, a.over_cap);
+                if (a.slopes) {
+                    const float from = (float)(at - base);
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) p[i] = fmaf(-slope, fabsf(from - (float)row_at(i)), p[i]);
+                }
+            }
+            if (!all_seen(first, r_first, r_last)) {
+                const uint32_t odd_lo = odd[(step - begin) % 3][0], odd_hi = odd[(step - begin) % 3][1];
+                if (odd_lo | odd_hi) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        const uint32_t bits = i < 16 ? odd_lo : odd_hi;
+                        if (bits >> (row_at(i) % 32 + 4 * g) & 1u) p[i] = __uint_as_float(0x7fc00000u);
+                    }
+                }
+                if (!all_seen(first, w_first, w_last)) {
+                    const int upto = at + 1 - base, from = since - base, front = prefix - base;
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        const int r = row_at(i);
+                        const bool sees = at >= 0 && ((r < upto && r >= from) || r < front);   // (a token in front of the unit's first row sees nothing)
+                        p[i] = sees ? p[i] : -INFINITY;
+                    }
+                }
+            }
+            // ---- weights ----
+            const float scale = BENT ? 1.f : a.scale_log2;
+            float top = p[0];
+#pragma unroll
+            for (int i = 1; i < 32; ++i) top = fmaxf(top, p[i]);
+            top = fmaxf(top, other_half(top)) * scale;
+            if (__any(top > m + kRoom || fabsf(m) >= kFarMax)) {
+                const float to = top > m + kRoom ? top : m, f = __builtin_amdgcn_exp2f(m - to);
+                m = to;
+                l *= f;
+#pragma unroll
+                for (int t = 0; t < kDims; ++t)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[t][i] *= f;
+            }
+            if (__any(fabsf(m) >= kFarMax && m > kNoMax)) {
+#pragma clang fp contract(off)
+#pragma unroll
+                for (int i = 0; i < 32; ++i) p[i] = __builtin_amdgcn_exp2f((p[i] * scale - m) + T::kShift);
+            } else {
+                const float less = T::kShift - m;
+#pragma unroll
+                for (int i = 0; i < 32; ++i) p[i] = __builtin_amdgcn_exp2f(BENT ? p[i] + less : fmaf(p[i], scale, less));
+            }
+            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < 32; ++i) sum[i % 4] += p[i];
+            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            u32x4 wt[T::kTwo ? 2 : 1][4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                float x[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = p[8 * k + i];
+                if constexpr (T::kTwo) {
+                    float rest[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float cut = __uint_as_float(__float_as_uint(x[i]) & 0xffff0000u);
+                        rest[i] = x[i] - cut;
+                        x[i] = cut;
+                    }
+                    wt[1][k] = pack8<false>(rest);
+                }
+                wt[0][k] = pack8<T::kHalf>(x);
+            }
+            // ---- O ----
+            const int vr = (lane & 15) / 4, vc = 2 * (lane >> 4 & 1) + (lane & 3) / 2, vb = 8 * (lane & 1);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int t = 0; t < kDims; ++t) {
+                    u32x4 x;
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const uint8_t *from = lv + (16 * k + 8 * j + 4 * g + vr) * T::kStride + ((4 * t + vc) ^ v_swizzle<T::kStride>(vr)) * 16 + vb;
+                        const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)from));
+                        x[2 * j] = y.x, x[2 * j + 1] = y.y;
+                    }
+                    if constexpr (T::kTwo) o[t] = product32<false>(x, wt[1][k], o[t]);
+                    o[t] = product32<T::kHalf>(x, wt[0][k], o[t]);
+                }
+        }
+        if (step + 1 < end) put(step + 1);
+        __syncthreads();
+    }
+    if (!there) return;
+    l += other_half(l);
+    if (a.splits > 1) {
+        float *dst = a.part + (((int64_t)split * a.n_units + u) * cols + col) * (D + 4);
+#pragma unroll
+        for (int t = 0; t < kDims; ++t)
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+                *reinterpret_cast<f32x4 *>(dst + 32 * t + 8 * b + 4 * g) = f32x4{o[t][4 * b], o[t][4 * b + 1], o[t][4 * b + 2], o[t][4 * b + 3]};
+        if (g == 0) dst[D] = m - T::kShift, dst[D + 1] = l;
+        return;
+    }
+    const bool none = l == 0.f;                                           // (NaN is handed on)
+    const float inv = none ? 0.f : 1.f / l;
+#pragma unroll
+    for (int t = 0; t < kDims; ++t)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            u32x2 y;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float x0 = none ? 0.f : o[t][4 * b + 2 * i] * inv, x1 = none ? 0.f : o[t][4 * b + 2 * i + 1] * inv;
+                if constexpr (F16) y[i] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)x0, (_Float16)x1});
+                else y[i] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)x0, (__bf16)x1});
+            }
+            *reinterpret_cast<u32x2 *>(a.out + row_out * D + 32 * t + 8 * b + 4 * g) = y;
+        }
+    if (a.lse && g == 0) a.lse[row_out] = none ? -INFINITY : (m - T::kShift + log2f(l)) * kToLn;
+}
+
+// The splits' parts of a column: D / 4 threads, several columns a workgroup.
+template <int D, bool F16> __global__ __launch_bounds__(256) void prompt_join_kernel(const PromptArgs a)
+{
+    constexpr int kLanes = D / 4, kAtOnce = 256 / kLanes;
+    const int cols = a.n_new * a.G, e = threadIdx.x % kLanes * 4;
+    const int64_t i = (int64_t)blockIdx.x * kAtOnce + threadIdx.x / kLanes, total = (int64_t)a.n_units * cols;
+    if (threadIdx.x >= kLanes * kAtOnce || i >= total) return;
+    float m = kNoMax, l = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.part[(s * total + i) * (D + 4) + D]);
+    for (int s = 0; s < a.splits; ++s) {
+        const float *p = a.part + (s * total + i) * (D + 4);
+        const float f = __builtin_amdgcn_exp2f(p[D] - m);
+        const f32x4 x = *reinterpret_cast<const f32x4 *>(p + e);
+        l = fmaf(f, p[D + 1], l);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[r] = fmaf(f, x[r], o[r]);
+    }
+    const int u = (int)(i / cols), col = (int)(i - (int64_t)u * cols), sq = u / a.H, h = u - sq * a.H, token = col / a.G, head = col - token * a.G;
+    const int64_t row = ((int64_t)sq * a.n_new + token) * a.H * a.G + h * a.G + head;
+    const bool none = l == 0.f;
+    u32x2 y;
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const float x0 = none ? 0.f : o[2 * r] / l, x1 = none ? 0.f : o[2 * r + 1] / l;
+        if constexpr (F16) y[r] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)x0, (_Float16)x1});
+        else y[r] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)x0, (__bf16)x1});
+    }
+    *reinterpret_cast<u32x2 *>(a.out + row * D + e) = y;
+    if (a.lse && e == 0) a.lse[row] = none ? -INFINITY : (m + log2f(l)) * kToLn;
+}
+
+}  // namespace
+
+template <int D> hipError_t launch_prompt_tiles(const PromptArgs &a, const nkv_pages &p, hipStream_t st)
+{
+    auto go = [&](auto f16, auto fp4) {
+        constexpr bool F16 = decltype(f16)::value, FP4 = decltype(fp4)::value;
+        const unsigned groups = (unsigned)((int64_t)a.n_units * a.tiles * a.splits);
+        (a.bent ? prompt_kernel<D, F16, FP4, true> : prompt_kernel<D, F16, FP4, false>)<<<groups, Tile<D, F16, FP4>::kThreads, 0, st>>>(a);
+        constexpr int kAtOnce = 256 / (D / 4);
+        if (a.splits > 1) prompt_join_kernel<D, F16><<<(unsigned)(((int64_t)a.n_units * a.n_new * a.G + kAtOnce - 1) / kAtOnce), 256, 0, st>>>(a);
+    };
+    using Yes = std::true_type;
+    using No = std::false_type;
+    const bool f16 = p.dtype == NKV_DTYPE_F16, fp4 = p.format == NKV_PAGES_FP4;
+    if (f16 && fp4) go(Yes{}, Yes{});
+    else if (f16) go(Yes{}, No{});
+    else if (fp4) go(No{}, Yes{});
+    else go(No{}, No{});
+    return hipGetLastError();
+}
+
+}  // namespace nkv
