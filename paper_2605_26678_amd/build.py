@@ -14,7 +14,7 @@ LIB = os.path.join(HERE, "libnkv.so")
 
 SOURCES = ["nkv_api.hip", "nkv_score_generic.hip", "nkv_score_fast.hip", "nkv_score_tile.hip", "nkv_finalize.hip", "nkv_finalize_wide.hip", "nkv_budget.hip",
            "nkv_budget_wide.hip", "nkv_budget_heads.hip", "nkv_select.hip", "nkv_select_wide.hip", "nkv_decode.hip",
-           "nkv_pages.hip", "nkv_pages_attention.hip", "nkv_pages_prompt.hip", "nkv_pages_prompt_64.hip", "nkv_pages_prompt_96.hip",
+           "nkv_pages.hip", "nkv_pages_attention.hip", "nkv_pages_prompt.hip", "nkv_pages_prompt_tokens.hip", "nkv_pages_prompt_64.hip", "nkv_pages_prompt_96.hip",
            "nkv_pages_prompt_128.hip", "nkv_pages_prompt_192.hip", "nkv_pages_prompt_256.hip", "nkv_beam.hip"]
 
 # -packed-fp32-ops is switched off on purpose: packed fp32 instructions are not to be generated.

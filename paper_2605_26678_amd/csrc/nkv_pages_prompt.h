@@ -41,7 +41,6 @@ __device__ __forceinline__ Seen seen_pages(int r0, int r1, int window, int prefi
     return {front, lo - front, front + max(r1 / kRows + 1, all) - lo};
 }
 __device__ __forceinline__ int rows_of(int len, int max_pages) { return max(0, min(len, max_pages * kRows)); }
-__device__ __forceinline__ int prefix_of(const PromptArgs &a, int seq, int len) { return a.prefix ? max(0, min(a.prefix[seq], len)) : 0; }
 
 // A logit in powers of two from a product: capped, less its distance's share.  |x| <= 5/8: x (1 - 0.33 x^2 + ..), a minimax polynomial whose relative error is 2^-27.9;
 // beyond: (1 - e^-2x) / (1 + e^-2x), where nothing cancels.
@@ -75,6 +74,9 @@ template <int N> __device__ __forceinline__ void bend(float (&s)[N], float scale
         s[i] = p * cap_log2;
     }
 }
+
+size_t prompt_token_ws_bytes(const nkv_pages &p, int n_q_heads, int n_new);
+hipError_t launch_prompt_tokens(const PromptArgs &a, const nkv_pages &p, void *ws, hipStream_t st);
 
 // Wavefronts of a workgroup, of 32 columns each: eight, or four where a lane's queries and weighted values take more than half of its registers.
 constexpr int prompt_waves(int d, bool two_pieces) { return d > 128 || (d == 128 && two_pieces) ? 4 : 8; }

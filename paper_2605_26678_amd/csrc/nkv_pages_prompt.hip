@@ -17,18 +17,21 @@ Grid grid_of(const nkv_pages &p, int n_q_heads, int n_new)
     return {(int)tiles, (int)std::max<int64_t>(1, std::min<int64_t>(256 / groups, p.max_pages / 2))};
 }
 
+// Columns that go with the single tokens: those that one product of theirs holds, so that a page is read once.
+bool few_columns(const nkv_pages &p, int n_q_heads, int n_new) { return (int64_t)(n_q_heads / p.H) * n_new <= 16; }
+
 }  // namespace
 
 bool pages_prompt_one_launch(const nkv_pages &p, int n_q_heads, int n_new)
 {
     // fewer than 2^32 threads: 512 a workgroup of the products, and a thread for four dims of a column where parts are joined
     const int64_t units = (int64_t)p.n_seqs * p.H, cols = (int64_t)(n_q_heads / p.H) * n_new;
-    if (cols >= (1 << 30) || units * ((cols + 127) / 128) >= (1 << 23)) return false;
-    return true;
+    return cols < (1 << 30) && units * ((cols + 127) / 128) < (1 << 23) && (!few_columns(p, n_q_heads, n_new) || units * cols < (1 << 24));
 }
 
 size_t pages_prompt_ws_bytes(const nkv_pages &p, int n_q_heads, int n_new)
 {
+    if (few_columns(p, n_q_heads, n_new)) return prompt_token_ws_bytes(p, n_q_heads, n_new);
     const Grid g = grid_of(p, n_q_heads, n_new);
     return g.splits == 1 ? 0 : (size_t)g.splits * p.n_seqs * (n_q_heads * (size_t)n_new) * (p.d + 4) * sizeof(float);
 }
@@ -49,6 +52,7 @@ hipError_t launch_pages_prompt(const void *q, const nkv_pages &p, const nkv_logi
         a.bent = rules->cap > 0 || rules->slopes;
     }
     a.out = (uint16_t *)out, a.lse = lse, a.part = (float *)ws;
+    if (few_columns(p, n_q_heads, n_new)) return launch_prompt_tokens(a, p, ws, st);
     const Grid g = grid_of(p, n_q_heads, n_new);
     a.tiles = g.tiles, a.splits = g.splits;
     switch (p.d) {

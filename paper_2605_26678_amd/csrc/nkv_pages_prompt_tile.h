@@ -142,7 +142,7 @@ __global__ __launch_bounds__((Tile<D, F16, FP4>::kThreads), (Tile<D, F16, FP4>::
     id /= a.n_units;
     const int split = id % a.splits, tile = a.tiles - 1 - id / a.splits;
     const int sq = u / a.H, h = u - sq * a.H, cols = a.n_new * a.G;
-    const int len = rows_of(a.lens[u], a.max_pages), prefix = prefix_of(a, sq, len);
+    const int len = rows_of(a.lens[u], a.max_pages), prefix = a.prefix ? max(0, min(a.prefix[sq], len)) : 0;
     const int32_t *table = a.table + (int64_t)u * a.max_pages;
     // rows that the workgroup's tokens, the wavefront's and the lane's stand on
     const int col_first = tile * T::kCols, col_last = min(cols, col_first + T::kCols) - 1;
