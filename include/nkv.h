@@ -466,14 +466,15 @@ int nkv_pages_compact(const int32_t *kept_idx, const int64_t *head_off, int64_t 
  * themselves.  Tokens of a beam are in the order of their logits.
  * A token whose logit is -inf is no candidate, and a beam has none whose score is infinite or NaN (a beam that is not there yet: -inf) or whose log sum is (one of
  * its logits is NaN or +inf, or all are -inf).  Where there are fewer than n_out the rest is score -inf, beam -1, token -1.
- * NKV_ESHAPE: n_beams * vocab of 2^32 and more, vocab over 2^30, or 2^24 and more stretches of 2048 logits (8192 where there are 1024 and more of these).
+ * NKV_ESHAPE: n_beams over NKV_MAX_BEAMS, n_beams * vocab of 2^32 and more, vocab over 2^30, or 2^24 and more stretches of 2048 logits (8192 where there are 1024 and more of these).
  * Deterministic; scratch: nkv_beam_workspace_bytes, n_out * 8 + 8 bytes a stretch.
  */
+#define NKV_MAX_BEAMS 1024
 #define NKV_MAX_BEAMS_OUT 64
 typedef struct nkv_beams {
     uint32_t struct_size;     /* sizeof(nkv_beams)                                                    */
     int32_t  n_prompts;
-    int32_t  n_beams;         /* beams of a prompt                                                    */
+    int32_t  n_beams;         /* beams of a prompt, up to NKV_MAX_BEAMS                               */
     int32_t  vocab;           /* logits of a beam                                                     */
     int32_t  n_out;           /* 1 .. NKV_MAX_BEAMS_OUT                                               */
     int32_t  dtype;           /* of the logits: NKV_DTYPE_F32, _BF16 or _F16                          */

@@ -315,7 +315,7 @@ int check_rules(const nkv_logit_rules *r, double scale)
 int check_beams(const nkv_beams *s)
 {
     if (!s || s->struct_size != sizeof(nkv_beams)) return NKV_EINVAL;
-    if (s->n_prompts < 1 || s->n_beams < 1 || s->vocab < 1) return NKV_ESHAPE;
+    if (s->n_prompts < 1 || s->n_beams < 1 || s->n_beams > NKV_MAX_BEAMS || s->vocab < 1) return NKV_ESHAPE;
     if (s->n_out < 1 || s->n_out > NKV_MAX_BEAMS_OUT) return NKV_EINVAL;
     if (s->dtype == NKV_DTYPE_F8_E4M3) return NKV_EUNSUPPORTED;
     if (s->dtype < NKV_DTYPE_F32 || s->dtype > NKV_DTYPE_F8_E4M3) return NKV_EINVAL;

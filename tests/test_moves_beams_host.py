@@ -37,7 +37,7 @@ def _beams(**kw):
 
 
 @pytest.mark.parametrize("kw,status", [
-    (dict(struct_size=1), nkv.NKV_EINVAL), (dict(n_prompts=0), nkv.NKV_ESHAPE), (dict(n_beams=0), nkv.NKV_ESHAPE), (dict(vocab=0), nkv.NKV_ESHAPE),
+    (dict(struct_size=1), nkv.NKV_EINVAL), (dict(n_prompts=0), nkv.NKV_ESHAPE), (dict(n_beams=0), nkv.NKV_ESHAPE), (dict(vocab=0), nkv.NKV_ESHAPE), (dict(n_beams=1025), nkv.NKV_ESHAPE),
     (dict(n_out=0), nkv.NKV_EINVAL), (dict(n_out=65), nkv.NKV_EINVAL), (dict(dtype=nkv.DTYPE_F8_E4M3), nkv.NKV_EUNSUPPORTED), (dict(dtype=9), nkv.NKV_EINVAL),
     (dict(dtype=-1), nkv.NKV_EINVAL), (dict(logits=0), nkv.NKV_EINVAL), (dict(scores=0), nkv.NKV_EINVAL), (dict(logits=FAKE + 1), nkv.NKV_EINVAL),
     (dict(logits=FAKE + 2, dtype=nkv.DTYPE_F32), nkv.NKV_EINVAL), (dict(scores=FAKE + 2), nkv.NKV_EINVAL), (dict(vocab=(1 << 30) + 1), nkv.NKV_ESHAPE),
