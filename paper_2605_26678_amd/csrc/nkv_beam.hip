@@ -17,6 +17,7 @@ namespace nkv {
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / kWave, kJoin = 1024, kJoinWaves = kJoin / kWave;
+constexpr int kGather = 512;            // candidates that are counted one against the other
 constexpr float kLog2e = 1.4426950408889634f;
 
 // Partial result of a stretch, in front of its n_out keys.
@@ -92,6 +93,13 @@ template <typename K> __device__ __forceinline__ K of_lane(const K &a, int lane)
     return a.moved([lane](uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); });
 }
 
+__device__ __forceinline__ int sum_of_8(int x)                            // over lanes 8 i .. 8 i + 7, all of them active
+{
+    x += dpp_partner<0xB1>(x);                                             // quad_perm [1,0,3,2]
+    x += dpp_partner<0x4E>(x);                                             // quad_perm [2,3,0,1]
+    return x + dpp_partner<0x141>(x);                                      // row_half_mirror: the other quad
+}
+
 // A number that n of the 64 lanes' reach, and few more of them: bit by bit from the first in which they differ.
 __device__ __forceinline__ uint32_t reached(uint32_t x, int n)
 {
@@ -158,7 +166,10 @@ template <typename T, int E> __global__ __launch_bounds__(kThreads) void beam_sc
     using Words = unsigned int __attribute__((ext_vector_type(4), aligned(sizeof(T))));
     constexpr int kVecs = E / 8;
     __shared__ Key buffer[kWaves][2 * kWave];
+    __shared__ uint64_t gathered[kGather];
     __shared__ Head heads[kWaves];
+    __shared__ uint32_t bounds[kWaves];
+    __shared__ int count;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), w = __builtin_amdgcn_readfirstlane(tid / kWave), n_out = a.n_out;
     const int row = blockIdx.x / a.stretches, stretch = blockIdx.x - row * a.stretches;
     const int p = row / a.B, b = row - p * a.B;
@@ -222,12 +233,49 @@ template <typename T, int E> __global__ __launch_bounds__(kThreads) void beam_sc
         if (reach >= n_out) bound = trial;
         if (reach == n_out) break;
     }
+    if (lane == 0) bounds[w] = bound, heads[w] = Head{top, sum};
+    if (tid == 0) count = 0;
+    __syncthreads();
+    const int64_t part = blockIdx.x;
+    if (tid == 0) {
+        float m = -INFINITY, s = 0.f;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) m = fmaxf(m, heads[i].top);
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) s += heads[i].top == -INFINITY ? heads[i].sum : heads[i].sum * __builtin_amdgcn_exp2f((heads[i].top - m) * kLog2e);
+        a.heads[part] = Head{m, s};
+    }
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) bound = max(bound, bounds[i]);
     const float from = key_value(max(bound, ord_key(-3.402823466e38f)));   // -inf and NaN are no candidates
     uint32_t takes = 0u;                                                   // bit 8 j + i: the lane's logit i of vector j
+    if (__any(mine >= from)) {
 #pragma unroll
-    for (int j = 0; j < kVecs; ++j)
+        for (int j = 0; j < kVecs; ++j)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) takes |= logit<T>(raw[j], i) >= from ? 1u << (8 * j + i) : 0u;
+            for (int i = 0; i < 8; ++i) takes |= logit<T>(raw[j], i) >= from ? 1u << (8 * j + i) : 0u;
+    }
+    auto key_of = [&](int e) { return Key{ord_key(logit_at<T, kVecs>(raw, e)), ~(uint32_t)(first + (e / 8 * kThreads + tid) * 8 + e % 8)}; };
+    for (uint32_t left = takes; left != 0u; left &= left - 1u) {
+        const Key k = key_of(__builtin_ctz(left));
+        const int at = atomicAdd(&count, 1);
+        if (at < kGather) gathered[at] = (uint64_t)k.value << 32 | k.token;
+    }
+    __syncthreads();
+    const int found = __builtin_amdgcn_readfirstlane(count);
+    if (found <= kGather) {
+        for (int i = tid / 8; i < found; i += kThreads / 8) {              // eight threads a candidate
+            const uint64_t key = gathered[i];
+            int before = 0;
+#pragma unroll 4
+            for (int k = tid % 8; k < found; k += 8) before += gathered[k] > key ? 1 : 0;
+            before = sum_of_8(before);
+            if (tid % 8 == 0 && before < n_out) a.keys[part * n_out + before] = Key{(uint32_t)(key >> 32), (uint32_t)key};
+        }
+        if (tid >= found && tid < n_out) a.keys[part * n_out + tid] = Key::none();
+        return;
+    }
+    // Too many that are equal, or side by side in few lanes: the lanes' one after the other, 64 at a time.
     Key list = Key::none(), least = Key::none();
     int held = 0;
     Key *mine_b = buffer[w];
@@ -241,7 +289,7 @@ template <typename T, int E> __global__ __launch_bounds__(kThreads) void beam_sc
         const bool left = takes != 0u;
         const int e = left ? __builtin_ctz(takes) : 0;
         takes &= takes - 1u;
-        const Key k{ord_key(logit_at<T, kVecs>(raw, e)), ~(uint32_t)(first + (e / 8 * kThreads + tid) * 8 + e % 8)};
+        const Key k = key_of(e);
         const bool counts = left && k > least;
         const unsigned long long mask = __ballot(counts);
         if (counts) mine_b[held + __popcll(mask & ((1ull << lane) - 1ull))] = k;
@@ -258,21 +306,11 @@ template <typename T, int E> __global__ __launch_bounds__(kThreads) void beam_sc
     if (held > 0) flush(held);
     __builtin_amdgcn_wave_barrier();
     mine_b[lane] = list;
-    if (lane == 0) heads[w] = Head{top, sum};
     __syncthreads();
     if (w > 0) return;
     static_assert(kWaves == 4, "two steps");
     list = joined(joined(list, buffer[1][lane]), joined(buffer[2][lane], buffer[3][lane]));
-    const int64_t part = blockIdx.x;
     if (lane < n_out) a.keys[part * n_out + lane] = list;
-    if (lane == 0) {
-        float m = -INFINITY, s = 0.f;
-#pragma unroll
-        for (int i = 0; i < kWaves; ++i) m = fmaxf(m, heads[i].top);
-#pragma unroll
-        for (int i = 0; i < kWaves; ++i) s += heads[i].top == -INFINITY ? heads[i].sum : heads[i].sum * __builtin_amdgcn_exp2f((heads[i].top - m) * kLog2e);
-        a.heads[part] = Head{m, s};
-    }
 }
 
 __device__ __forceinline__ uint64_t ord64(double x)
@@ -285,7 +323,7 @@ __device__ __forceinline__ double value64(uint64_t k) { return __builtin_bit_cas
 // grid: a workgroup a prompt.  Nearly all of its time is waiting, so it does little in a row: a wavefront finds the n_out-th largest of its lanes' best candidates, which
 // bounds the prompt's n_out-th from below; those that reach the largest such bound, a few times n_out, are gathered, and each counts those before it.  (Joining the
 // lists in the wavefronts and then in a tree took 8, 12 and 12 us of the three measured cases.)  Where too many are equal the lists are joined after all.
-constexpr int kHold = 8, kGather = 512;
+constexpr int kHold = 8;
 __global__ __launch_bounds__(kJoin) void beam_join_kernel(const Head *__restrict__ heads, const Key *__restrict__ keys, const float *__restrict__ scores, int B,
                                                          int V, int n_out, int stretches, float *__restrict__ out_scores, int32_t *__restrict__ out_beams,
                                                          int32_t *__restrict__ out_tokens)
@@ -374,9 +412,7 @@ __global__ __launch_bounds__(kJoin) void beam_join_kernel(const Head *__restrict
                 const uint64_t other = lds.gathered.value[k];
                 before += other > value || (other == value && lds.gathered.at[k] > at) ? 1 : 0;
             }
-            before += dpp_partner<0xB1>(before);                           // quad_perm [1,0,3,2]
-            before += dpp_partner<0x4E>(before);                           // quad_perm [2,3,0,1]
-            before += dpp_partner<0x141>(before);                          // row_half_mirror: the other quad
+            before = sum_of_8(before);
             if (tid % 8 == 0 && before < n_out) put(before, Candidate{(uint32_t)(value >> 32), (uint32_t)value, at});
         }
         if (tid >= found && tid < n_out) put(tid, Candidate::none());
