@@ -86,6 +86,9 @@ class nkv_beams(C.Structure):
 _TOKENS_SIZE = C.sizeof(nkv_tokens)
 _TOKENS = struct.Struct("Iiiiii4P9q2P")        # nkv_tokens' fields in their order, packed in half the time of a ctypes structure
 assert _TOKENS.size == _TOKENS_SIZE
+_BEAMS_SIZE = C.sizeof(nkv_beams)
+_BEAMS = struct.Struct("I5i2q2P")              # nkv_beams' fields likewise
+assert _BEAMS.size == _BEAMS_SIZE
 
 
 class NkvError(RuntimeError):
@@ -140,8 +143,8 @@ def lib() -> C.CDLL:
                                                  C.c_size_t, vp]
         L.nkv_pages_copy.argtypes = [vp, vp, i64, C.POINTER(nkv_pages), vp]
         L.nkv_pages_compact.argtypes = [vp, vp, i64, C.POINTER(nkv_pages), C.POINTER(nkv_pages), vp]
-        L.nkv_beam_workspace_bytes.argtypes = [C.POINTER(nkv_beams), C.POINTER(C.c_size_t)]
-        L.nkv_beam_select.argtypes = [C.POINTER(nkv_beams), vp, vp, vp, vp, C.c_size_t, vp]
+        L.nkv_beam_workspace_bytes.argtypes = [vp, C.POINTER(C.c_size_t)]      # nkv_beams *, likewise
+        L.nkv_beam_select.argtypes = [vp, vp, vp, vp, vp, C.c_size_t, vp]
         L.nkv_copy_probe.argtypes = [vp, vp, C.c_size_t, vp]
         L.nkv_strerror.argtypes = [C.c_int]
         L.nkv_strerror.restype = C.c_char_p
@@ -586,9 +589,11 @@ def pages_copy(src, dst, pages: Pages, stream=None) -> None:
     n = src.numel()
     if dst.numel() != n:
         raise ValueError(f"src has {n} pages and dst {dst.numel()}")
-    _check_dense(src, "src", pages, pages.torch_i32, n)
-    _check_dense(dst, "dst", pages, pages.torch_i32, n)
-    _check_gpu(pages)
+    at, i32 = pages.index, pages.torch_i32
+    if not (src.dtype is i32 and src.is_contiguous() and src.get_device() == at and dst.dtype is i32 and dst.is_contiguous() and dst.get_device() == at >= 0):
+        _check_dense(src, "src", pages, i32, n)
+        _check_dense(dst, "dst", pages, i32, n)
+        _check_gpu(pages)
     rc = lib().nkv_pages_copy(src.data_ptr(), dst.data_ptr(), n, pages.ref, _stream(stream))
     if rc:
         raise NkvError(rc, "nkv_pages_copy")
@@ -608,49 +613,54 @@ def pages_compact(kept_idx, head_off, rows: int, old: Pages, pages: Pages, strea
         raise NkvError(rc, "nkv_pages_compact")
 
 
-def _beams(n_prompts: int, n_beams: int, vocab: int, n_out: int, dtype: int, strides, logits: int, scores: int) -> nkv_beams:
-    return nkv_beams(C.sizeof(nkv_beams), n_prompts, n_beams, vocab, n_out, dtype, (C.c_int64 * 2)(*strides), logits, scores)
-
-
 def beam_workspace_bytes(n_prompts: int, n_beams: int, vocab: int, n_out: int) -> int:
     """Scratch of ``beam_select``."""
     out = C.c_size_t(0)
     some = 256                                           # (an address that is not used)
-    rc = lib().nkv_beam_workspace_bytes(C.byref(_beams(n_prompts, n_beams, vocab, n_out, DTYPE_F32, (0, 0), some, some)), C.byref(out))
+    rc = lib().nkv_beam_workspace_bytes(_BEAMS.pack(_BEAMS_SIZE, n_prompts, n_beams, vocab, n_out, DTYPE_F32, 0, 0, some, some), C.byref(out))
     if rc:
         raise NkvError(rc, "nkv_beam_workspace_bytes")
     return int(out.value)
 
 
-_logit_types = None
+_beam_types = None
+
+
+def _find_beam_types():
+    import torch
+    return {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16}, torch.float32, torch.int32
+
+
+def _check_beam(t, what: str, kind, shape, logits) -> None:
+    if t.dtype is not kind or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{what} is dense {kind} {list(shape)}, not {t.dtype} {list(t.shape)}")
+    if t.get_device() != logits.get_device():
+        raise ValueError(f"{what} is on device {t.device}, and the logits are on {logits.device}")
 
 
 def beam_select(logits, scores, out_scores, out_beams, out_tokens, ws, stream=None) -> None:
     """The best candidates of every prompt: logits [P, B, V] of fp32, bf16 or fp16 (any strides but the last dim's), scores fp32 [P, B] ->
     out_scores fp32, out_beams, out_tokens int32 [P, n_out], largest first; see ``nkv_beam_select`` in nkv.h."""
-    global _logit_types
-    import torch
-    if _logit_types is None:
-        _logit_types = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16}
-    dtype = _logit_types.get(logits.dtype)
-    if dtype is None or logits.dim() != 3 or logits.stride(2) != 1 and logits.shape[2] > 1:
+    global _beam_types
+    if _beam_types is None:
+        _beam_types = _find_beam_types()
+    codes, f32, i32 = _beam_types
+    dtype, given, strides = codes.get(logits.dtype), logits.shape, logits.stride()
+    if dtype is None or len(given) != 3 or strides[2] != 1 and given[2] > 1:
         raise ValueError("logits is fp32, bf16 or fp16 [prompts, beams, vocabulary], a beam's logits next to each other")
-    P, B, V = logits.shape
-    at = logits.get_device()
-    if out_scores.dim() != 2 or out_scores.shape[0] != P:
+    P, B, V = given
+    shape, at = out_scores.shape, logits.get_device()
+    if len(shape) != 2 or shape[0] != P:
         raise ValueError(f"out_scores is [{P}, n_out]")
-    n_out = out_scores.shape[1]
-    for t, what, kind, shape in ((scores, "scores", torch.float32, (P, B)), (out_scores, "out_scores", torch.float32, (P, n_out)),
-                                 (out_beams, "out_beams", torch.int32, (P, n_out)), (out_tokens, "out_tokens", torch.int32, (P, n_out))):
-        if t.dtype is not kind or t.shape != shape or not t.is_contiguous():
-            raise ValueError(f"{what} is dense {kind} {list(shape)}, not {t.dtype} {list(t.shape)}")
-        if t.get_device() != at:
-            raise ValueError(f"{what} is on device {t.device}, and the logits are on {logits.device}")
+    _check_beam(scores, "scores", f32, (P, B), logits)
+    _check_beam(out_scores, "out_scores", f32, shape, logits)
+    _check_beam(out_beams, "out_beams", i32, shape, logits)
+    _check_beam(out_tokens, "out_tokens", i32, shape, logits)
     if not ws.is_contiguous() or ws.get_device() != at:
         raise ValueError("ws is contiguous and on the logits' device")
     if at < 0:
         raise ValueError("the logits are not on a GPU")
-    rc = lib().nkv_beam_select(C.byref(_beams(P, B, V, n_out, dtype, (logits.stride(0), logits.stride(1)), logits.data_ptr(), scores.data_ptr())),
+    rc = lib().nkv_beam_select(_BEAMS.pack(_BEAMS_SIZE, P, B, V, shape[1], dtype, strides[0], strides[1], logits.data_ptr(), scores.data_ptr()),
                                out_scores.data_ptr(), out_beams.data_ptr(), out_tokens.data_ptr(), ws.data_ptr(), ws.nbytes, _stream(stream))
     if rc:
         raise NkvError(rc, "nkv_beam_select")

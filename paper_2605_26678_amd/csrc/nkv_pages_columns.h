@@ -333,7 +333,9 @@ __device__ __forceinline__ void bend_products(const AttendArgs &a, f32x4 (&s)[Ge
     for (int i = 0; i < N; ++i) s[i / 4][i % 4] = a.slopes ? fmaf(-slope, fabsf(from - (float)(16 * (i / 4) + i % 4)), z[i]) : z[i];
 }
 
-template <int D, bool F16, bool FP4, int COLS>
+// WHOLE: weights in all the pieces that hold their 24 bits (fp16 rows of 16-bit pages: 22); otherwise rounded to the 16 bits that the output has (fp16 rows of 4-bit
+// pages: to two pieces of bf16), a third of the products with V.
+template <int D, bool F16, bool FP4, int COLS, bool WHOLE>
 __device__ __forceinline__ void accumulate(State<D, F16, FP4, COLS> &st, const Rows<D, F16, FP4> &f, const f32x4 (&products)[Geo<D, F16, FP4>::kTiles],
                                            float scale_log2, int slot)
 {
@@ -381,6 +383,7 @@ __device__ __forceinline__ void accumulate(State<D, F16, FP4, COLS> &st, const R
         return __float_as_uint(__uint_as_float(__float_as_uint(x) & upto) - __uint_as_float(__float_as_uint(x) & above));
     };
     if constexpr (COLS == 5) {
+        static_assert(WHOLE, "three pieces side by side");
         // A row's two dims stay side by side, as a product's two rows: beside (piece, 0) for the first dim, (0, piece) for the second.  Twice the
         // products, of which there are few, and no exchange of halves between rows' words.  The sum of the weights is one more product, with ones.
         constexpr uint32_t one = 0x3f803f80u;
@@ -408,11 +411,18 @@ __device__ __forceinline__ void accumulate(State<D, F16, FP4, COLS> &st, const R
         for (int i = 0; i < 4 * Q::kTiles; ++i) l += p[i];
         st.l += l;
         // the 32 rows of two tiles: words of two rows' weights, a piece at a time
-        u32x4 w[Q::kSets];
+        constexpr int kSets = WHOLE ? Q::kSets : F16 && FP4 ? 2 : 1;
+        u32x4 w[kSets];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const float a = p[2 * j], b = p[2 * j + 1];
-            if constexpr (Q::kHalfP) {
+            if constexpr (!WHOLE && kSets == 1) {
+                if constexpr (F16) w[0][j] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)a, (_Float16)b});
+                else w[0][j] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
+            } else if constexpr (!WHOLE) {
+                w[0][j] = high_halves(__float_as_uint(a), __float_as_uint(b));
+                w[1][j] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)__uint_as_float(between(a, ~0u, kTop)), (__bf16)__uint_as_float(between(b, ~0u, kTop))});
+            } else if constexpr (Q::kHalfP) {
                 const f16x2 hi = {(_Float16)a, (_Float16)b}, lo = {(_Float16)(a - (float)hi.x), (_Float16)(b - (float)hi.y)};
                 w[0][j] = __builtin_bit_cast(uint32_t, hi), w[1][j] = __builtin_bit_cast(uint32_t, lo);
             } else {
@@ -429,7 +439,7 @@ __device__ __forceinline__ void accumulate(State<D, F16, FP4, COLS> &st, const R
             const u32x4 lo = {low_halves(x[0], x[1]), low_halves(x[2], x[3]), low_halves(x[4], x[5]), low_halves(x[6], x[7])};
             const u32x4 hi = {high_halves(x[0], x[1]), high_halves(x[2], x[3]), high_halves(x[4], x[5]), high_halves(x[6], x[7])};
 #pragma unroll
-            for (int c = Q::kSets - 1; c >= 0; --c) {
+            for (int c = kSets - 1; c >= 0; --c) {
                 st.o[2 * k] = product<Q::kHalfP>(lo, w[c], st.o[2 * k]);
                 st.o[2 * k + 1] = product<Q::kHalfP>(hi, w[c], st.o[2 * k + 1]);
             }
@@ -640,7 +650,6 @@ template <int D, bool F16, bool FP4, int COLS, bool RULES> __global__ __launch_b
             }
         }
     };
-    auto slope_of = [&](int h) { return a.slopes ? a.slopes[h * a.G + head] * kToLog2 : 0.f; };
     // ---- the stretch, unit by unit ----
     uint32_t i = lo;
     do {
@@ -651,7 +660,9 @@ template <int D, bool F16, bool FP4, int COLS, bool RULES> __global__ __launch_b
         const int32_t *table = a.table + (int64_t)u * a.max_pages;
         Seen seen{};
         int prefix = 0;
+        float slope = 0.f;
         if constexpr (RULES) {
+            if (a.slopes) slope = a.slopes[h * a.G + head] * kToLog2;
             prefix = prefix_of(a, u, len);
             seen = seen_pages(len - a.n_new, len - 1, a.window, prefix);
         }
@@ -672,20 +683,22 @@ template <int D, bool F16, bool FP4, int COLS, bool RULES> __global__ __launch_b
             f32x4 s[Q::kTiles];
             if (works) key_products<D, F16, FP4>(f, q, half, s);
             keys_on();
-            if (works && RULES) {
-                if (a.bent) bend_products<D, F16, FP4>(a, s, (float)(len - a.n_new + token - row0 - 4 * g), slope_of(h));
-                // all of the half's rows are seen by all tokens
-                const int r0 = len - a.n_new, r1 = len - 1;
-                if (!(r0 >= 0 && rel >= Q::kStep && (row0 + Q::kStep <= prefix || (least >= Q::kStep && (a.window <= 0 || row0 > r1 - a.window))))) {
-                    const int at = r0 + token, since = a.window > 0 ? at - a.window + 1 : 0;
-                    const bool some = at >= 0, all = r0 >= 0;              // (a token in front of the unit's first row sees nothing)
-                    mask_rows_by_rules<D, F16, FP4>(f, s, g, rel, some ? at + 1 - row0 : 0, some ? since - row0 : 0, some ? prefix - row0 : 0, all ? least : 0,
-                                                    all && a.window > 0 ? r1 - a.window + 1 - row0 : 0, all ? prefix - row0 : 0);
+            if constexpr (RULES) {
+                if (works) {
+                    if (a.bent) bend_products<D, F16, FP4>(a, s, (float)(len - a.n_new + token - row0 - 4 * g), slope);
+                    // all of the half's rows are seen by all tokens
+                    const int r0 = len - a.n_new, r1 = len - 1;
+                    if (!(r0 >= 0 && rel >= Q::kStep && (row0 + Q::kStep <= prefix || (least >= Q::kStep && (a.window <= 0 || row0 > r1 - a.window))))) {
+                        const int at = r0 + token, since = a.window > 0 ? at - a.window + 1 : 0;
+                        const bool some = at >= 0, all = r0 >= 0;          // (a token in front of the unit's first row sees nothing)
+                        mask_rows_by_rules<D, F16, FP4>(f, s, g, rel, some ? at + 1 - row0 : 0, some ? since - row0 : 0, some ? prefix - row0 : 0, all ? least : 0,
+                                                        all && a.window > 0 ? r1 - a.window + 1 - row0 : 0, all ? prefix - row0 : 0);
+                    }
+                    accumulate<D, F16, FP4, COLS, false>(st, f, s, a.bent ? 1.f : a.scale_log2, slot);
                 }
-                accumulate<D, F16, FP4, COLS>(st, f, s, a.bent ? 1.f : a.scale_log2, slot);
             } else if (works) {
                 if (least < Q::kStep) mask_rows<D, F16, FP4>(f, s, g, rel, least + token, least);
-                accumulate<D, F16, FP4, COLS>(st, f, s, a.scale_log2, slot);
+                accumulate<D, F16, FP4, COLS, true>(st, f, s, a.scale_log2, slot);
             }
             values_on();
         };
@@ -827,7 +840,7 @@ template <bool RULES, typename Out> hipError_t launch_columns(AttendArgs a, cons
                     constexpr int COLS = decltype(columns)::value;
                     pages_attend_kernel<D, F16, FP4, COLS, RULES><<<dim3(groups_of(p), (unsigned)((cols + COLS - 1) / COLS)), kThreads, 0, st>>>(a);
                 };
-                if constexpr (FP4) {                                       // (16-bit rows are bound by memory with 16 columns too)
+                if constexpr (FP4 && !RULES) {                             // (16-bit rows are bound by memory with 16 columns too)
                     if (cols <= 5) return launch(std::integral_constant<int, 5>{});
                 }
                 launch(std::integral_constant<int, 16>{});
