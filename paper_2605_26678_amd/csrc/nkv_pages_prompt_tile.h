@@ -40,13 +40,10 @@ template <int D, bool F16, bool FP4> struct Tile {
 // the weighted values in their registers are seldom multiplied.
 constexpr float kRoom = 8.f;
 
-// Chunk c of a row lies at c ^ that: eight rows' same chunk of K, and the four rows by two chunks of V that 16 lanes transpose, are in different banks.
-__device__ __forceinline__ int k_swizzle(int row) { return row & 7; }
-template <int STRIDE> __device__ __forceinline__ int v_swizzle(int row)
-{
-    const int a = row & 3;
-    return STRIDE % 256 == 0 ? 4 * a ^ (a & 2) : 4 * (a & 1) ^ (a & 2);
-}
+// Chunk c of a row lies at c ^ that.  LDS has 64 banks, 16 chunks: of K, any 16 rows that differ in their last four bits are in different banks; of V, the four rows by
+// four chunks that 32 lanes transpose, and the eight rows by two chunks that lanes 0 .. 15 and 32 .. 47 do.
+template <int STRIDE> __device__ __forceinline__ int k_swizzle(int row) { return STRIDE % 256 == 0 ? row & 15 : row >> 1 & 7; }
+template <int STRIDE> __device__ __forceinline__ int v_swizzle(int row) { return STRIDE % 256 == 0 ? 4 * (row & 3) + (row >> 1 & 2) : 2 * (row & 2) + (row >> 1 & 2); }
 
 template <bool HALF> __device__ __forceinline__ f32x16 product32(const u32x4 &a, const u32x4 &b, const f32x16 &c)
 {
@@ -109,7 +106,7 @@ template <int D, bool F16, bool FP4> struct Stage {
                 if (row >= valid) y = u32x4{0u, 0u, 0u, 0u};
                 else if (found) atomicOr(odd + row / 32, 1u << row % 32);
             }
-            *reinterpret_cast<u32x4 *>(lds_k + row * T::kStride + (c ^ k_swizzle(row)) * 16) = x;
+            *reinterpret_cast<u32x4 *>(lds_k + row * T::kStride + (c ^ k_swizzle<T::kStride>(row)) * 16) = x;
             *reinterpret_cast<u32x4 *>(lds_v + row * T::kStride + (c ^ v_swizzle<T::kStride>(row)) * 16) = y;
         }
     }
@@ -228,7 +225,7 @@ __global__ __launch_bounds__((Tile<D, F16, FP4>::kThreads), (Tile<D, F16, FP4>::
             for (int k = 0; k < kSteps; ++k)
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
-                    const u32x4 x = *reinterpret_cast<const u32x4 *>(lk + (32 * t + n) * T::kStride + ((2 * k + g) ^ k_swizzle(n)) * 16);
+                    const u32x4 x = *reinterpret_cast<const u32x4 *>(lk + (32 * t + n) * T::kStride + ((2 * k + g) ^ k_swizzle<T::kStride>(n)) * 16);
                     if constexpr (T::kTwo) s[t] = product32<false>(x, q[1][k], s[t]);
                     s[t] = product32<T::kHalf>(x, q[0][k], s[t]);
                 }
@@ -319,7 +316,7 @@ __global__ __launch_bounds__((Tile<D, F16, FP4>::kThreads), (Tile<D, F16, FP4>::
                     u32x4 x;
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        const uint8_t *from = lv + (16 * k + 8 * j + 4 * g + vr) * T::kStride + ((4 * t + vc) ^ v_swizzle<T::kStride>(vr)) * 16 + vb;
+                        const uint8_t *from = lv + (16 * k + 8 * j + 4 * g + vr) * T::kStride + ((4 * t + vc) ^ v_swizzle<T::kStride>(4 * g + vr)) * 16 + vb;
                         const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)from));
                         x[2 * j] = y.x, x[2 * j + 1] = y.y;
                     }
