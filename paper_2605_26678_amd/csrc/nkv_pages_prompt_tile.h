@@ -36,6 +36,7 @@ template <int D, bool F16, bool FP4> struct Tile {
     // fp16 weights of up to 2^(6 + 8), see kRoom: those of 2^-30 of the largest one still have all of their bits
     static constexpr float kShift = kHalf ? 6.f : 0.f;
 };
+constexpr int kProducts = 0x8, kReads = 0x100;   // groups of instructions, as sched_group_barrier numbers them
 // A column's maximum is only moved when a logit is more than this above it (in powers of two): weights of up to 2^8 have the bits that those of up to 1 have, and
 // the weighted values in their registers are seldom multiplied.
 constexpr float kRoom = 8.f;
@@ -185,14 +186,19 @@ __global__ __launch_bounds__((Tile<D, F16, FP4>::kThreads), (Tile<D, F16, FP4>::
         for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
     const float slope = BENT && a.slopes ? a.slopes[h * a.G + head] * kToLog2 : 0.f;
 
-    auto id_of = [&](int step) { return step < end ? table[seen.page(step)] : -1; };
+    // the pages' numbers, 64 steps' at a time, one a lane: a load for every step would be waited for at every step
+    int ids = -1;
+    auto id_of = [&](int step) {
+        if ((step - begin) % kWave == 0) ids = step + lane < end ? table[seen.page(step + lane)] : -1;
+        return __builtin_amdgcn_readlane(ids, (step - begin) % kWave);
+    };
     auto page_of = [&](int p) { return a.pool + (int64_t)(p >= 0 && p < a.n_pages ? p : 0) * (FP4 ? Fp4Page<D>::kBytes : WidePage<D>::kBytes); };
     // all rows of a page are seen by all tokens on rows r0 .. r1
     auto all_seen = [&](int first, int r0, int r1) { return r0 >= 0 && first + kRows <= len && (first + kRows <= prefix || (first + kRows - 1 <= r0 && (a.window <= 0 || first > r1 - a.window))); };
     auto none_seen = [&](int first, int r0, int r1) { return first >= prefix && (first > r1 || (a.window > 0 && first + kRows - 1 <= r0 - a.window)); };
 
     Stage<D, F16, FP4> stage;
-    int this_id = id_of(begin), next_id = id_of(begin + 1);
+    int this_id = id_of(begin);
     auto put = [&](int step) {                                            // the staged page, of that step
         const int first = seen.page(step) * kRows, half = (step - begin) & 1;
         uint8_t *const lk = lds[half][0], *const lv = lds[half][1];
@@ -209,26 +215,42 @@ __global__ __launch_bounds__((Tile<D, F16, FP4>::kThreads), (Tile<D, F16, FP4>::
     for (int step = begin; step < end; ++step) {
         const int first = seen.page(step) * kRows, half = (step - begin) & 1;
         const bool counts = this_id >= 0 && this_id < a.n_pages;
-        this_id = next_id;
-        next_id = id_of(step + 2);
+        this_id = id_of(step + 1);
         if (step + 1 < end) stage.load(page_of(this_id), tid);
         if (tid < 2) odd[(step - begin + 2) % 3][tid] = 0u;
         if (counts && works && !none_seen(first, w_first, w_last)) {
             const uint8_t *const lk = lds[half][0], *const lv = lds[half][1];
             // ---- S ----
+            // Four steps' rows are asked for ahead of the products: a read from LDS takes as long as four of them.
             f32x16 s[2];
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[t][i] = 0.f;
+            constexpr int kAhead = kSteps < 4 ? kSteps : 4;
+            u32x4 rows[kAhead][2];
+            auto read_keys = [&](int k) {
 #pragma unroll
-            for (int k = 0; k < kSteps; ++k)
+                for (int t = 0; t < 2; ++t)
+                    rows[k % kAhead][t] = *reinterpret_cast<const u32x4 *>(lk + (32 * t + n) * T::kStride + ((2 * k + g) ^ k_swizzle<T::kStride>(n)) * 16);
+            };
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) read_keys(k);
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k) {
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
-                    const u32x4 x = *reinterpret_cast<const u32x4 *>(lk + (32 * t + n) * T::kStride + ((2 * k + g) ^ k_swizzle<T::kStride>(n)) * 16);
-                    if constexpr (T::kTwo) s[t] = product32<false>(x, q[1][k], s[t]);
-                    s[t] = product32<T::kHalf>(x, q[0][k], s[t]);
+                    if constexpr (T::kTwo) s[t] = product32<false>(rows[k % kAhead][t], q[1][k], s[t]);
+                    s[t] = product32<T::kHalf>(rows[k % kAhead][t], q[0][k], s[t]);
                 }
+                if (k + kAhead < kSteps) read_keys(k + kAhead);
+            }
+            __builtin_amdgcn_sched_group_barrier(kReads, 2 * kAhead, 0);
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k) {
+                __builtin_amdgcn_sched_group_barrier(kProducts, T::kTwo ? 4 : 2, 0);
+                if (k + kAhead < kSteps) __builtin_amdgcn_sched_group_barrier(kReads, 2, 0);
+            }
             float p[32];
 #pragma unroll
             for (int i = 0; i < 32; ++i) p[i] = s[i / 16][i % 16];
@@ -243,22 +265,20 @@ __global__ __launch_bounds__((Tile<D, F16, FP4>::kThreads), (Tile<D, F16, FP4>::
                 }
             }
             if (!all_seen(first, r_first, r_last)) {
-                const uint32_t odd_lo = odd[(step - begin) % 3][0], odd_hi = odd[(step - begin) % 3][1];
-                if (odd_lo | odd_hi) {
+                // the page's rows that the lane's token sees, a bit each (in front of the unit's first row it sees nothing)
+                const int lo = max(since - first, 0), hi = at < 0 ? 0 : min(at + 1 - first, kRows), fr = at < 0 ? 0 : min(prefix - first, kRows);
+                uint64_t bits = hi > lo ? ~0ull >> (kRows - (hi - lo)) << lo : 0ull;
+                bits |= fr > 0 ? ~0ull >> (kRows - fr) : 0ull;
+                const uint64_t bad = (uint64_t)odd[(step - begin) % 3][1] << 32 | odd[(step - begin) % 3][0];
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        const uint32_t bits = i < 16 ? odd_lo : odd_hi;
-                        if (bits >> (row_at(i) % 32 + 4 * g) & 1u) p[i] = __uint_as_float(0x7fc00000u);
-                    }
-                }
-                if (!all_seen(first, w_first, w_last)) {
-                    const int upto = at + 1 - base, from = since - base, front = prefix - base;
+                for (int t = 0; t < 2; ++t) {
+                    const uint32_t sees = (uint32_t)(bits >> 32 * t) >> 4 * g, poison = (uint32_t)(bad >> 32 * t) >> 4 * g;
+                    if (__any(poison != 0u)) {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        const int r = row_at(i);
-                        const bool sees = at >= 0 && ((r < upto && r >= from) || r < front);   // (a token in front of the unit's first row sees nothing)
-                        p[i] = sees ? p[i] : -INFINITY;
+                        for (int i = 0; i < 16; ++i) p[16 * t + i] = poison & 1u << row_at(i) ? __uint_as_float(0x7fc00000u) : p[16 * t + i];
                     }
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) p[16 * t + i] = sees & 1u << row_at(i) ? p[16 * t + i] : -INFINITY;
                 }
             }
             // ---- weights ----
@@ -308,21 +328,32 @@ __global__ __launch_bounds__((Tile<D, F16, FP4>::kThreads), (Tile<D, F16, FP4>::
                 wt[0][k] = pack8<T::kHalf>(x);
             }
             // ---- O ----
-            const int vr = (lane & 15) / 4, vc = 2 * (lane >> 4 & 1) + (lane & 3) / 2, vb = 8 * (lane & 1);
+            constexpr int kMoves = 4 * kDims, kHeld = 4;
+            u32x4 dims[kHeld];
+            auto read_values = [&](int i) {
+                const int k = i / kDims, t = i % kDims;
+                const int vr = (lane & 15) / 4, vc = 2 * (lane >> 4 & 1) + (lane & 3) / 2, vb = 8 * (lane & 1);
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-#pragma unroll
-                for (int t = 0; t < kDims; ++t) {
-                    u32x4 x;
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const uint8_t *from = lv + (16 * k + 8 * j + 4 * g + vr) * T::kStride + ((4 * t + vc) ^ v_swizzle<T::kStride>(4 * g + vr)) * 16 + vb;
-                        const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)from));
-                        x[2 * j] = y.x, x[2 * j + 1] = y.y;
-                    }
-                    if constexpr (T::kTwo) o[t] = product32<false>(x, wt[1][k], o[t]);
-                    o[t] = product32<T::kHalf>(x, wt[0][k], o[t]);
+                for (int j = 0; j < 2; ++j) {
+                    const uint8_t *from = lv + (16 * k + 8 * j + 4 * g + vr) * T::kStride + ((4 * t + vc) ^ v_swizzle<T::kStride>(4 * g + vr)) * 16 + vb;
+                    const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4 *)from));
+                    dims[i % kHeld][2 * j] = y.x, dims[i % kHeld][2 * j + 1] = y.y;
                 }
+            };
+#pragma unroll
+            for (int i = 0; i < kHeld; ++i) read_values(i);
+#pragma unroll
+            for (int i = 0; i < kMoves; ++i) {
+                if constexpr (T::kTwo) o[i % kDims] = product32<false>(dims[i % kHeld], wt[1][i / kDims], o[i % kDims]);
+                o[i % kDims] = product32<T::kHalf>(dims[i % kHeld], wt[0][i / kDims], o[i % kDims]);
+                if (i + kHeld < kMoves) read_values(i + kHeld);
+            }
+            __builtin_amdgcn_sched_group_barrier(kReads, 2 * kHeld, 1);
+#pragma unroll
+            for (int i = 0; i < kMoves; ++i) {
+                __builtin_amdgcn_sched_group_barrier(kProducts, T::kTwo ? 2 : 1, 1);
+                if (i + kHeld < kMoves) __builtin_amdgcn_sched_group_barrier(kReads, 2, 1);
+            }
         }
         if (step + 1 < end) put(step + 1);
         __syncthreads();
