@@ -58,7 +58,7 @@ struct AttendArgs {
     float *part;                         // [part][column][D + 4]: weighted values, maximum, sum
     // RULES
     bool bent;                           // cap or slopes
-    float cap_log2, over_cap;
+    Cap cap;
     int32_t window;
     const float *slopes;
     const int32_t *prefix;
@@ -328,7 +328,7 @@ __device__ __forceinline__ void bend_products(const AttendArgs &a, f32x4 (&s)[Ge
     float z[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) z[i] = s[i / 4][i % 4];
-    bend(z, a.scale_log2, a.cap_log2, a.over_cap);
+    bend(z, a.scale_log2, a.cap);
 #pragma unroll
     for (int i = 0; i < N; ++i) s[i / 4][i % 4] = a.slopes ? fmaf(-slope, fabsf(from - (float)(16 * (i / 4) + i % 4)), z[i]) : z[i];
 }

@@ -6,6 +6,12 @@
 
 namespace nkv {
 
+// A logit's cap: cap * log2(e) tanh(x), x = product * over_cap; none where cap_log2 is 0.  Products of up to `near` take near_by[0 .. 3] as the coefficients of
+// product^1, 3, 5 and 7.
+struct Cap {
+    float cap_log2, over_cap, near, near_by[4];
+};
+
 // What a call asks for, on its way to the kernels.
 struct PromptArgs {
     const uint16_t *q;
@@ -16,7 +22,7 @@ struct PromptArgs {
     uint32_t flip;                       // sign bits of the query that change: those of a negative scale
     bool flat;                           // a scale of zero: the query counts as zeros
     bool bent;                           // cap or slopes
-    float cap_log2, over_cap;            // cap * log2(e) and scale / cap; 0: no cap
+    Cap cap;
     int32_t window;                      // 0: none
     const float *slopes;                 // [H * G]
     const int32_t *prefix;               // [sequences]
@@ -42,25 +48,32 @@ __device__ __forceinline__ Seen seen_pages(int r0, int r1, int window, int prefi
 }
 __device__ __forceinline__ int rows_of(int len, int max_pages) { return max(0, min(len, max_pages * kRows)); }
 
-// A logit in powers of two from a product: capped, less its distance's share.  |x| <= 5/8: x (1 - 0.33 x^2 + ..), a minimax polynomial whose relative error is 2^-27.9;
-// beyond: (1 - e^-2x) / (1 + e^-2x), where nothing cancels.
-template <int N> __device__ __forceinline__ void bend(float (&s)[N], float scale_log2, float cap_log2, float over_cap)
+// A logit in powers of two from a product: scaled, or capped.  |x| <= 5/16, as most logits are that a cap is meant for: tanh(x) as x - x^3 / 3 + .., a minimax polynomial
+// whose relative error is 2^-26, with the scale and the cap in its coefficients; |x| <= 5/8: a longer one, 2^-27.9; beyond: (1 - e^-2x) / (1 + e^-2x), where nothing
+// cancels.
+constexpr double kNear[4] = {1.0, -0.33332862850586767, 0.13309054081886735, -0.049920588703130035}, kNearBound = 0.3125;
+template <int N> __device__ __forceinline__ void bend(float (&s)[N], float scale_log2, const Cap &c)
 {
-    if (cap_log2 == 0.f) {
+    if (c.cap_log2 == 0.f) {
 #pragma unroll
         for (int i = 0; i < N; ++i) s[i] *= scale_log2;
         return;
     }
-    float far = 0.f;
+    float most = 0.f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        s[i] *= over_cap;
-        far = fmaxf(far, fabsf(s[i]));
+    for (int i = 0; i < N; ++i) most = fmaxf(most, fabsf(s[i]));
+    if (!__any(most > c.near)) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float y = s[i] * s[i];
+            s[i] *= fmaf(y, fmaf(y, fmaf(y, c.near_by[3], c.near_by[2]), c.near_by[1]), c.near_by[0]);
+        }
+        return;
     }
-    const bool any_far = __any(far > 0.625f);
+    const bool any_far = __any(most * c.over_cap > 0.625f);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const float x = s[i], y = x * x;
+        const float x = s[i] * c.over_cap, y = x * x;
         float p = fmaf(y, -0.005659991875290871f, 0.020591000095009804f);
         p = fmaf(y, p, -0.053721074014902115f);
         p = fmaf(y, p, 0.13331127166748047f);
@@ -69,9 +82,9 @@ template <int N> __device__ __forceinline__ void bend(float (&s)[N], float scale
         if (any_far) {
             const float e = __builtin_amdgcn_exp2f(fabsf(x) * (-2.f * kToLog2));
             const float t = (1.f - e) * __builtin_amdgcn_rcpf(1.f + e);
-            p = fabsf(x) > 0.625f ? copysignf(t, x) : x != x ? x : p;
+            p = fabsf(x) > 0.625f ? copysignf(t, x) : p;
         }
-        s[i] = p * cap_log2;
+        s[i] = p * c.cap_log2;
     }
 }
 

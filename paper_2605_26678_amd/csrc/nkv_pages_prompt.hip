@@ -20,6 +20,21 @@ Grid grid_of(const nkv_pages &p, int n_q_heads, int n_new)
 // Columns that go with the single tokens: those that one product of theirs holds, so that a page is read once.
 bool few_columns(const nkv_pages &p, int n_q_heads, int n_new) { return (int64_t)(n_q_heads / p.H) * n_new <= 16; }
 
+Cap cap_of(double cap, double scale)
+{
+    const double x = scale / cap;
+    Cap c{};
+    c.cap_log2 = pages_scale(cap), c.over_cap = (float)x;
+    // the coefficients' powers, and those of the products that they meet, stay well within fp32
+    if (x >= 0x1p-14 && x <= 0x1p4 && cap >= 0x1p-8 && cap <= 0x1p16) {
+        c.near = (float)(kNearBound / x);
+        for (int i = 0; i < 4; ++i) c.near_by[i] = (float)(kNear[i] * cap * 1.4426950408889634 * pow(x, 2 * i + 1));
+    } else {
+        c.near = -1.f;
+    }
+    return c;
+}
+
 }  // namespace
 
 bool pages_prompt_one_launch(const nkv_pages &p, int n_q_heads, int n_new)
@@ -48,7 +63,7 @@ hipError_t launch_pages_prompt(const void *q, const nkv_pages &p, const nkv_logi
     a.flip = scale < 0 ? 0x80008000u : 0u;
     if (rules) {
         a.window = rules->window, a.slopes = rules->slopes, a.prefix = rules->prefix;
-        if (rules->cap > 0) a.cap_log2 = pages_scale(rules->cap), a.over_cap = a.flat ? 1.f : (float)(fabs(scale) / rules->cap);
+        if (rules->cap > 0) a.cap = cap_of(rules->cap, a.flat ? rules->cap : fabs(scale));
         a.bent = rules->cap > 0 || rules->slopes;
     }
     a.out = (uint16_t *)out, a.lse = lse, a.part = (float *)ws;

@@ -257,7 +257,7 @@ __global__ __launch_bounds__((Tile<D, F16, FP4>::kThreads), (Tile<D, F16, FP4>::
             const int base = first + 4 * g;                               // p[i] is of row base + row_at(i)
             auto row_at = [](int i) { return 32 * (i / 16) + 8 * (i % 16 / 4) + i % 4; };
             if constexpr (BENT) {
-                bend(p, a.scale_log2, a.cap_log2, a.over_cap);
+                bend(p, a.scale_log2, a.cap);
                 if (a.slopes) {
                     const float from = (float)(at - base);
 #pragma unroll

@@ -11,7 +11,7 @@ hipError_t launch_prompt_tokens(const PromptArgs &c, const nkv_pages &p, void *w
     a.q = c.q, a.pool = c.pool, a.table = c.table, a.lens = c.lens;
     a.n_units = c.n_units, a.H = c.H, a.G = c.G, a.n_new = c.n_new, a.n_pages = c.n_pages, a.max_pages = c.max_pages;
     a.scale_log2 = c.scale_log2, a.flip = c.flip, a.flat = c.flat;
-    a.bent = c.bent, a.cap_log2 = c.cap_log2, a.over_cap = c.over_cap, a.window = c.window, a.slopes = c.slopes, a.prefix = c.prefix;
+    a.bent = c.bent, a.cap = c.cap, a.window = c.window, a.slopes = c.slopes, a.prefix = c.prefix;
     if (p.dtype == NKV_DTYPE_F16) return launch_columns<true>(a, p, (_Float16 *)c.out, c.lse, ws, st);
     return launch_columns<true>(a, p, (__bf16 *)c.out, c.lse, ws, st);
 }

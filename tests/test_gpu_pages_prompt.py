@@ -131,7 +131,7 @@ def test_rules(d, dtype, fmt):
     slopes = slopes_of(6)
     for n in (1, 4, 90):
         q = queries(c, n, 6, n, 2.0)
-        for rules in (dict(cap=1.5), dict(cap=30.0), dict(window=1), dict(window=70), dict(prefix=np.array([100, 0, 500], np.int32)), dict(slopes=slopes),
+        for rules in (dict(cap=1.5), dict(cap=6.0), dict(cap=30.0), dict(window=1), dict(window=70), dict(prefix=np.array([100, 0, 500], np.int32)), dict(slopes=slopes),
                       dict(window=37, prefix=np.array([65, 129, 2], np.int32)), dict(cap=5.0, window=150, slopes=slopes, prefix=np.array([4, -3, 1 << 30], np.int32))):
             check(c, q, 6, 1 / np.sqrt(d), f"{n} tokens, {rules}", **rules)
 
