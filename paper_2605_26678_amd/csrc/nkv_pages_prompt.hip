@@ -6,6 +6,9 @@
 namespace nkv {
 namespace {
 
+// Tables of up to that many pages: all rows in one launch.  (8 KV heads of 400 rows: 14 us so, shared out 12; of 64 rows 7.5, single tokens' kernels 11.5)
+constexpr int kShort = 4;
+
 struct Grid {
     int tiles, splits;                   // workgroups of a unit: tiles of columns, and shares of the rows that one sees
 };
@@ -14,11 +17,22 @@ Grid grid_of(const nkv_pages &p, int n_q_heads, int n_new)
 {
     const int64_t cols = (int64_t)(n_q_heads / p.H) * n_new, at_once = 32 * prompt_waves(p.d, p.dtype == NKV_DTYPE_F16 && p.format == NKV_PAGES_FP4);
     const int64_t tiles = (cols + at_once - 1) / at_once, groups = (int64_t)p.n_seqs * p.H * tiles;
-    return {(int)tiles, (int)std::max<int64_t>(1, std::min<int64_t>(256 / groups, p.max_pages / 2))};
+    return {(int)tiles, p.max_pages <= kShort ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(256 / groups, p.max_pages / 2))};
 }
 
-// Columns that go with the single tokens: those that one product of theirs holds, so that a page is read once.
-bool few_columns(const nkv_pages &p, int n_q_heads, int n_new) { return (int64_t)(n_q_heads / p.H) * n_new <= 16; }
+// Whether a call goes with the single tokens' kernels.  They share out all units' pages evenly and take up to 16 columns at a time, in some 10 us and what memory takes; the
+// tiles take a page a microsecond in each workgroup whatever the columns, in one launch or two.  us, theirs / tiles, 8 KV heads of 128 dims:
+//   4 bits    16 columns: 1024 rows of 1, 32 sequences 10.6 / 11.6, 22 / 29; 16384 rows 15 / 24, 110 / 364
+//             32 columns: 1024 rows 11.1 / 11.8, 40 / 29; 4096 rows 12 / 16, 73 / 95; 16384 rows 24 / 25, 214 / 365
+//             64 columns: 4096 rows 15 / 19, 140 / 97
+//   16 bits   8 columns: 600 rows 11.8 / 10.1, 25 / 19; 1024 rows 12.5 / 10.9, 39 / 28; 4096 rows 12.5 / 13.6, 92 / 96; 16384 rows 21 / 23, 284 / 354
+//             32 columns: 4096 rows 19 / 16, 208 / 98
+bool few_columns(const nkv_pages &p, int n_q_heads, int n_new)
+{
+    const int64_t cols = (int64_t)(n_q_heads / p.H) * n_new;
+    if (p.max_pages <= kShort) return false;
+    return p.format == NKV_PAGES_FP4 ? cols <= (p.max_pages > 32 ? 32 : 16) : cols <= 16 && p.max_pages > 20;
+}
 
 Cap cap_of(double cap, double scale)
 {

@@ -397,14 +397,32 @@ template <int D, bool F16> __global__ __launch_bounds__(256) void prompt_join_ke
     if (threadIdx.x >= kLanes * kAtOnce || i >= total) return;
     float m = kNoMax, l = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.part[(s * total + i) * (D + 4) + D]);
-    for (int s = 0; s < a.splits; ++s) {
-        const float *p = a.part + (s * total + i) * (D + 4);
-        const float f = __builtin_amdgcn_exp2f(p[D] - m);
-        const f32x4 x = *reinterpret_cast<const f32x4 *>(p + e);
-        l = fmaf(f, p[D + 1], l);
+    constexpr int kParts = 8;                                             // parts asked for at once
+    for (int s0 = 0; s0 < a.splits; s0 += kParts) {
+        f32x4 x[kParts];
+        float pm[kParts], pl[kParts];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) o[r] = fmaf(f, x[r], o[r]);
+        for (int k = 0; k < kParts; ++k) {
+            const float *p = a.part + (min(s0 + k, a.splits - 1) * total + i) * (D + 4);
+            x[k] = *reinterpret_cast<const f32x4 *>(p + e);
+            pm[k] = s0 + k < a.splits ? p[D] : kNoMax, pl[k] = p[D + 1];
+        }
+        float top = m;
+#pragma unroll
+        for (int k = 0; k < kParts; ++k) top = fmaxf(top, pm[k]);
+        const float f0 = __builtin_amdgcn_exp2f(m - top);
+        m = top;
+        l *= f0;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[r] *= f0;
+#pragma unroll
+        for (int k = 0; k < kParts; ++k) {
+            if (s0 + k >= a.splits) break;
+            const float f = __builtin_amdgcn_exp2f(pm[k] - m);
+            l = fmaf(f, pl[k], l);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[r] = fmaf(f, x[k][r], o[r]);
+        }
     }
     const int u = (int)(i / cols), col = (int)(i - (int64_t)u * cols), sq = u / a.H, h = u - sq * a.H, token = col / a.G, head = col - token * a.G;
     const int64_t row = ((int64_t)sq * a.n_new + token) * a.H * a.G + h * a.G + head;

@@ -116,30 +116,37 @@ def slopes_of(Hq):
     return (2.0 ** (-8.0 * np.arange(1, Hq + 1) / Hq)).astype(np.float32)
 
 
+# pages of a unit's row of the table, by which calls of few columns go with one kernel or the other
+WIDTHS = [None, 40]
+
+
+@pytest.mark.parametrize("width", WIDTHS)
 @pytest.mark.parametrize("dtype,fmt", KINDS)
 @pytest.mark.parametrize("d", HEAD_DIMS)
-def test_lengths(d, dtype, fmt):
-    c = Cache(4, 4, d, dtype, fmt, EDGES, seed=d, rows=1.0)
-    for n, G in ((1, 1), (1, 8), (2, 16), (5, 3), (40, 1), (70, 4)):
+def test_lengths(d, dtype, fmt, width):
+    c = Cache(4, 4, d, dtype, fmt, EDGES, width=width, seed=d, rows=1.0)
+    for n, G in ((1, 1), (1, 8), (2, 16), (5, 3), (40, 1), (70, 4)) if width is None else ((1, 1), (1, 8), (2, 16), (5, 3)):
         check(c, queries(c, n, 4 * G, n), 4 * G, 1 / np.sqrt(d), f"{n} tokens of {G} heads")
 
 
 @pytest.mark.parametrize("dtype,fmt", KINDS)
 @pytest.mark.parametrize("d", HEAD_DIMS)
-def test_rules(d, dtype, fmt):
-    c = Cache(3, 2, d, dtype, fmt, [700, 333, 130, 64, 40, 3], seed=d + 1, rows=1.0)
+@pytest.mark.parametrize("width", WIDTHS)
+def test_rules(d, dtype, fmt, width):
+    c = Cache(3, 2, d, dtype, fmt, [700, 333, 130, 64, 40, 3], width=width, seed=d + 1, rows=1.0)
     slopes = slopes_of(6)
-    for n in (1, 4, 90):
+    for n in (1, 4, 90) if width is None else (1, 4):
         q = queries(c, n, 6, n, 2.0)
         for rules in (dict(cap=1.5), dict(cap=6.0), dict(cap=30.0), dict(window=1), dict(window=70), dict(prefix=np.array([100, 0, 500], np.int32)), dict(slopes=slopes),
                       dict(window=37, prefix=np.array([65, 129, 2], np.int32)), dict(cap=5.0, window=150, slopes=slopes, prefix=np.array([4, -3, 1 << 30], np.int32))):
             check(c, q, 6, 1 / np.sqrt(d), f"{n} tokens, {rules}", **rules)
 
 
+@pytest.mark.parametrize("width", WIDTHS)
 @pytest.mark.parametrize("dtype,fmt", KINDS)
-def test_windows_and_prefixes_at_page_borders(dtype, fmt):
-    c = Cache(2, 1, 64, dtype, fmt, [640, 577], seed=3, rows=1.0)
-    for n in (1, 3, 200):
+def test_windows_and_prefixes_at_page_borders(dtype, fmt, width):
+    c = Cache(2, 1, 64, dtype, fmt, [640, 577], width=width, seed=3, rows=1.0)
+    for n in (1, 3, 200) if width is None else (1, 3):
         q = queries(c, n, 2, n)
         for window in (1, 63, 64, 65, 128, 129, 640, 1 << 30):
             for prefix in (None, np.array([64, 1], np.int32), np.array([63, 65], np.int32), np.array([639, 577], np.int32)):
@@ -150,7 +157,7 @@ def test_windows_and_prefixes_at_page_borders(dtype, fmt):
 def test_long(dtype, fmt):
     # rows shared out among workgroups, and several tiles of columns
     c = Cache(1, 2, 128, dtype, fmt, [5000, 4321], seed=5, rows=1.0)
-    for n, G in ((1, 1), (1, 8), (3, 5), (16, 1), (17, 1), (150, 4)):
+    for n, G in ((1, 1), (1, 8), (3, 5), (16, 1), (17, 1), (4, 8), (33, 1), (150, 4)):
         check(c, queries(c, n, 2 * G, n), 2 * G, 1 / np.sqrt(128), f"{n} tokens of {G} heads")
     check(c, queries(c, 17, 4, 4), 4, 0.1, "rules", cap=20.0, window=1000, prefix=np.array([700], np.int32), slopes=slopes_of(4))
     check(c, queries(c, 1, 4, 4), 4, 0.1, "rules", cap=20.0, window=1000, prefix=np.array([700], np.int32), slopes=slopes_of(4))
@@ -179,12 +186,15 @@ def _plant(c, u, row, value, key=False, dim=5):
 
 
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("width", WIDTHS)
 @pytest.mark.parametrize("dtype,fmt", KINDS)
-def test_rows_that_are_not_seen_hold_anything(dtype, fmt, value):
+def test_rows_that_are_not_seen_hold_anything(dtype, fmt, value, width):
     for d in (64, 128, 256):
         for n, planted in ((1, [3, 100]), (3, [3, 150, 297, 299]), (90, [3, 70, 215, 260, 299]), (90, [5, 298])):
+            if width and n > 3:
+                continue
             for key in (False, True):                                     # (an infinite key is a logit of either infinity: keys of NaN)
-                c = Cache(1, 1, d, dtype, fmt, [300], seed=d, rows=1.0)
+                c = Cache(1, 1, d, dtype, fmt, [300], width=width, seed=d, rows=1.0)
                 for row in planted:
                     _plant(c, 0, row, float("nan") if key else value, key=key)
                 q = queries(c, n, 3, n)
@@ -193,10 +203,11 @@ def test_rows_that_are_not_seen_hold_anything(dtype, fmt, value):
                 check(c, q, 3, 0.1, f"{n} tokens", window=2)
 
 
+@pytest.mark.parametrize("width", WIDTHS)
 @pytest.mark.parametrize("dtype,fmt", KINDS)
 @pytest.mark.parametrize("n", [1, 2, 40])
-def test_scales(n, dtype, fmt):
-    c = Cache(1, 2, 64, dtype, fmt, [200, 77], seed=8, rows=1.0)
+def test_scales(n, dtype, fmt, width):
+    c = Cache(1, 2, 64, dtype, fmt, [200, 77], width=width, seed=8, rows=1.0)
     q = queries(c, n, 4, 2)
     for scale in (-0.2, 0.0, 1e-40, -1e-46, 3.0):
         check(c, q, 4, scale, f"scale {scale}")
@@ -207,11 +218,12 @@ def test_scales(n, dtype, fmt):
     check(c, q, 4, 0.5, "a small cap", cap=1e-3)
 
 
+@pytest.mark.parametrize("width", WIDTHS)
 @pytest.mark.parametrize("n", [1, 40])
 @pytest.mark.parametrize("dtype,fmt", KINDS)
-def test_far_logits(n, dtype, fmt):
+def test_far_logits(n, dtype, fmt, width):
     """Logits of 2^26 and more: one row has all the weight, or, where their places are wider than their distance, some."""
-    c = Cache(1, 1, 64, dtype, fmt, [150], seed=9, rows=1.0)
+    c = Cache(1, 1, 64, dtype, fmt, [150], width=width, seed=9, rows=1.0)
     for scale in (1e7, -1e7, 1e30):
         o, l = attend(c, queries(c, n, 2, 3), 2, scale)
         assert bool(o.isfinite().all()) and bool(l.isfinite().all())
@@ -228,7 +240,7 @@ def test_far_logits(n, dtype, fmt):
 
 def test_calls_are_deterministic_on_streams_and_in_graphs():
     side = torch.cuda.Stream()
-    for n, G, lens in ((1, 4, [5000, 700]), (2, 3, [900, 64]), (130, 4, [3000, 1000])):
+    for n, G, lens in ((1, 4, [5000, 700]), (2, 3, [900, 64]), (1, 2, [200, 100]), (130, 4, [3000, 1000])):
         c = Cache(1, 2, 128, "bf16", "fp4", lens, seed=n, rows=1.0)
         Hq, slopes = 2 * G, slopes_of(2 * G)
         q = queries(c, n, Hq, 7)
