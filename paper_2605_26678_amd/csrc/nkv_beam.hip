@@ -4,8 +4,9 @@
 // (beam_scan_kernel) and leaves its maximum, its sum of exponentials and its n_out largest logits; a workgroup for a prompt joins them
 // (beam_join_kernel): the sums in 64 bits, the candidates by their value in 64 bits.
 //
-// Within a beam the order of the candidates is that of the logits, so no sum is needed to drop nearly all of them: the n_out-th largest of a
-// wavefront's 64 lane maxima is a bound that at least n_out of its logits reach, and few more.  Lists are 64 keys, one a lane, sorted and joined by
+// Within a beam the order of the candidates is that of the logits, so no sum is needed to drop nearly all of them.  The threads' largest logits are dealt out to the W
+// wavefronts; the least of their n_out / W-th largest is a bound that n_out of the logits reach at least, and few more: those are gathered, and each counts those before
+// it.  Where too many reach it (equal ones, or large ones side by side in a few threads) lists are sorted and joined instead.  Lists are 64 keys, one a lane, sorted and joined by
 // bitonic steps between lanes (21 steps to sort, 7 to join two).  A key holds the logit and, of equal ones, the lower token as the larger key, so that
 // no two are alike and the answer does not depend on the order of anything.
 #include "nkv_device.h"
@@ -100,7 +101,7 @@ __device__ __forceinline__ int sum_of_8(int x)                            // ove
     return x + dpp_partner<0x141>(x);                                      // row_half_mirror: the other quad
 }
 
-// A number that n of the 64 lanes' reach, and few more of them: bit by bit from the first in which they differ.
+// The largest number that n of the 64 lanes' reach, bit by bit from the first in which they differ.  (Where a few more than n reach it a bit earlier that will do.)
 __device__ __forceinline__ uint32_t reached(uint32_t x, int n)
 {
     const uint32_t top = wave_reduce(x, [](uint32_t a, uint32_t b) { return max(a, b); }), least = wave_reduce(x, [](uint32_t a, uint32_t b) { return min(a, b); });
@@ -118,10 +119,32 @@ __device__ __forceinline__ uint32_t reached(uint32_t x, int n)
     return bound;
 }
 
+// A bound that n of a workgroup's numbers reach at least, and few more, with its barriers (what was written to LDS before it is there afterwards).  For few: the largest of the
+// wavefronts' n-th largest.  For more: the numbers are dealt out anew, so that all wavefronts have their share of any stretch of large ones, and the least of the
+// n / W-th largest is taken; tighter, and some 1 us more.
+template <int W> __device__ __forceinline__ uint32_t bound_of(uint32_t x, int n, uint32_t *dealt, uint32_t *bounds)
+{
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), w = tid / kWave;
+    const bool few = n < 12;
+    if (!few) {
+        dealt[tid] = x;
+        __syncthreads();
+        x = dealt[lane * W + ((w + lane) & (W - 1))];
+        n = (n + W - 1) / W;
+    }
+    const uint32_t mine = reached(x, n);
+    if (lane == 0) bounds[w] = mine;
+    __syncthreads();
+    uint32_t bound = bounds[0];
+#pragma unroll
+    for (int i = 1; i < W; ++i) bound = few ? max(bound, bounds[i]) : min(bound, bounds[i]);
+    return bound;
+}
+
 template <typename T> struct Logits;
-template <> struct Logits<float> { static constexpr int kWords = 8; static constexpr int kBits = 32; };
-template <> struct Logits<f16_t> { static constexpr int kWords = 4; static constexpr int kBits = 16; };
-template <> struct Logits<uint16_t> { static constexpr int kWords = 4; static constexpr int kBits = 16; };   // bf16
+template <> struct Logits<float> { static constexpr int kWords = 8; };
+template <> struct Logits<f16_t> { static constexpr int kWords = 4; };
+template <> struct Logits<uint16_t> { static constexpr int kWords = 4; };   // bf16
 
 template <typename T> __device__ __forceinline__ float logit(const uint32_t *w, int i)
 {
@@ -168,7 +191,7 @@ template <typename T, int E> __global__ __launch_bounds__(kThreads) void beam_sc
     __shared__ Key buffer[kWaves][2 * kWave];
     __shared__ uint64_t gathered[kGather];
     __shared__ Head heads[kWaves];
-    __shared__ uint32_t bounds[kWaves];
+    __shared__ uint32_t best[kThreads], bounds[kWaves];
     __shared__ int count;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), w = __builtin_amdgcn_readfirstlane(tid / kWave), n_out = a.n_out;
     const int row = blockIdx.x / a.stretches, stretch = blockIdx.x - row * a.stretches;
@@ -224,18 +247,9 @@ template <typename T, int E> __global__ __launch_bounds__(kThreads) void beam_sc
         add([base](float x) { return (x - base) * kLog2e; });
     }
     sum = wave_sum(sum);
-    // (all of 64 lanes count: those of -inf too, which are none in the end)
-    const uint32_t key = ord_key(mine);
-    uint32_t bound = 0u;
-    for (int bit = 31; bit >= 32 - L::kBits; --bit) {
-        const uint32_t trial = bound | 1u << bit;
-        const int reach = __popcll(__ballot(key >= trial));
-        if (reach >= n_out) bound = trial;
-        if (reach == n_out) break;
-    }
-    if (lane == 0) bounds[w] = bound, heads[w] = Head{top, sum};
+    if (lane == 0) heads[w] = Head{top, sum};
     if (tid == 0) count = 0;
-    __syncthreads();
+    const uint32_t bound = bound_of<kWaves>(ord_key(mine), n_out, best, bounds);
     const int64_t part = blockIdx.x;
     if (tid == 0) {
         float m = -INFINITY, s = 0.f;
@@ -245,8 +259,6 @@ template <typename T, int E> __global__ __launch_bounds__(kThreads) void beam_sc
         for (int i = 0; i < kWaves; ++i) s += heads[i].top == -INFINITY ? heads[i].sum : heads[i].sum * __builtin_amdgcn_exp2f((heads[i].top - m) * kLog2e);
         a.heads[part] = Head{m, s};
     }
-#pragma unroll
-    for (int i = 0; i < kWaves; ++i) bound = max(bound, bounds[i]);
     const float from = key_value(max(bound, ord_key(-3.402823466e38f)));   // -inf and NaN are no candidates
     uint32_t takes = 0u;                                                   // bit 8 j + i: the lane's logit i of vector j
     if (__any(mine >= from)) {
@@ -267,7 +279,7 @@ template <typename T, int E> __global__ __launch_bounds__(kThreads) void beam_sc
         for (int i = tid / 8; i < found; i += kThreads / 8) {              // eight threads a candidate
             const uint64_t key = gathered[i];
             int before = 0;
-#pragma unroll 4
+#pragma unroll 8
             for (int k = tid % 8; k < found; k += 8) before += gathered[k] > key ? 1 : 0;
             before = sum_of_8(before);
             if (tid % 8 == 0 && before < n_out) a.keys[part * n_out + before] = Key{(uint32_t)(key >> 32), (uint32_t)key};
@@ -320,9 +332,9 @@ __device__ __forceinline__ uint64_t ord64(double x)
 }
 __device__ __forceinline__ double value64(uint64_t k) { return __builtin_bit_cast(double, k >> 63 ? k & ~(1ull << 63) : ~k); }
 
-// grid: a workgroup a prompt.  Nearly all of its time is waiting, so it does little in a row: a wavefront finds the n_out-th largest of its lanes' best candidates, which
-// bounds the prompt's n_out-th from below; those that reach the largest such bound, a few times n_out, are gathered, and each counts those before it.  (Joining the
-// lists in the wavefronts and then in a tree took 8, 12 and 12 us of the three measured cases.)  Where too many are equal the lists are joined after all.
+// grid: a workgroup a prompt.  Nearly all of its time is waiting, so it does little in a row: all candidates (of many lists: the first ones) at once to a bound, and those
+// that reach it one against the other.  (Lists joined in the wavefronts and then in a tree: 8, 12 and 12 us for one prompt of 4 beams and 64 lists of 8, 16 of 8 and 128 lists of 16, 5 of 5 and 125
+// lists of 10.)
 constexpr int kHold = 8;
 __global__ __launch_bounds__(kJoin) void beam_join_kernel(const Head *__restrict__ heads, const Key *__restrict__ keys, const float *__restrict__ scores, int B,
                                                          int V, int n_out, int stretches, float *__restrict__ out_scores, int32_t *__restrict__ out_beams,
@@ -337,7 +349,7 @@ __global__ __launch_bounds__(kJoin) void beam_join_kernel(const Head *__restrict
     } lds;
     __shared__ double lses[NKV_MAX_BEAMS];
     __shared__ float score_of[NKV_MAX_BEAMS];
-    __shared__ uint32_t bounds[kJoinWaves];
+    __shared__ uint32_t all_best[kJoin], bounds[kJoinWaves];
     __shared__ int count;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), w = __builtin_amdgcn_readfirstlane(tid / kWave), p = blockIdx.x;
     const int parts = B * stretches, in_beam = stretches * n_out;
@@ -345,7 +357,7 @@ __global__ __launch_bounds__(kJoin) void beam_join_kernel(const Head *__restrict
     keys += p * total;
     Key held[kHold];
 #pragma unroll
-    for (int k = 0; k < kHold; ++k) held[k] = tid + kJoin * k < total ? keys[tid + kJoin * k] : Key::none();
+    for (int k = 0; k < kHold; ++k) held[k] = tid + kJoin * k < total && total <= kJoin * kHold ? keys[tid + kJoin * k] : Key::none();
     // log sum exp of every beam, NaN for a beam without candidates: where it is not finite, or the beam's score is not
     for (int b = w; b < B; b += kJoinWaves) {
         const Head *h = heads + ((int64_t)p * B + b) * stretches;
@@ -374,25 +386,36 @@ __global__ __launch_bounds__(kJoin) void beam_join_kernel(const Head *__restrict
 #pragma unroll
     for (int k = 0; k < kHold; ++k) {
         some[k] = Candidate::none();
-        if (kJoin * k >= total) continue;
+        if (kJoin * k >= total || total > kJoin * kHold) continue;
         some[k] = candidate(held[k], (int)min((uint32_t)(tid + kJoin * k) / (uint32_t)in_beam, (uint32_t)(B - 1)));
         best = max(best, some[k].hi);
     }
-    for (int64_t i = kJoin * kHold + tid; i < total; i += kJoin) best = max(best, candidate(keys[i], (int)(i / in_beam)).hi);
-    uint32_t bound = reached(best, n_out);
-    if (lane == 0) bounds[w] = bound;
-    __syncthreads();
-    bound = 1u;                                                            // (0: no candidate)
-#pragma unroll
-    for (int i = 0; i < kJoinWaves; ++i) bound = max(bound, bounds[i]);
+    auto best_at = [&](int r) {                                            // of the thread's lists' r-th candidates
+        uint32_t b = 0u;
+        for (int i = tid; i < parts; i += kJoin) b = max(b, candidate(keys[(int64_t)i * n_out + r], i / stretches).hi);
+        return b;
+    };
+    if (total > kJoin * kHold) best = best_at(0);
+    uint32_t bound = max(bound_of<kJoinWaves>(best, n_out, all_best, bounds), 1u);   // (0: no candidate)
+    // Of many lists a few may hold nearly all: n_out / r lists whose r-th candidates reach a number have n_out that do.
+    if (total > kJoin * kHold)
+        for (int r = 4; r <= n_out; r *= 4) {
+            __syncthreads();
+            bound = max(bound, bound_of<kJoinWaves>(best_at(r - 1), (n_out + r - 1) / r, all_best, bounds));
+        }
     auto gather = [&](const Candidate &c) {
-        if (c.hi < bound) return;
+        if (c.hi < bound) return false;
         const int at = atomicAdd(&count, 1);
         if (at < kGather) lds.gathered.value[at] = c.value(), lds.gathered.at[at] = c.at;
+        return true;
     };
+    if (total <= kJoin * kHold) {
 #pragma unroll
-    for (int k = 0; k < kHold; ++k) gather(some[k]);
-    for (int64_t i = kJoin * kHold + tid; i < total; i += kJoin) gather(candidate(keys[i], (int)(i / in_beam)));
+        for (int k = 0; k < kHold; ++k) gather(some[k]);
+    } else {
+        for (int i = tid; i < parts; i += kJoin)
+            for (int r = 0; r < n_out && gather(candidate(keys[(int64_t)i * n_out + r], i / stretches)); ++r) {}
+    }
     __syncthreads();
     const int found = count;
     auto put = [&](int at, const Candidate &c) {
@@ -407,10 +430,11 @@ __global__ __launch_bounds__(kJoin) void beam_join_kernel(const Head *__restrict
             const uint64_t value = lds.gathered.value[i];
             const uint32_t at = lds.gathered.at[i];
             int before = 0;
-#pragma unroll 4
+#pragma unroll 8
             for (int k = tid % 8; k < found; k += 8) {
                 const uint64_t other = lds.gathered.value[k];
-                before += other > value || (other == value && lds.gathered.at[k] > at) ? 1 : 0;
+                const uint32_t other_at = lds.gathered.at[k];
+                before += (other > value) | ((other == value) & (other_at > at)) ? 1 : 0;
             }
             before = sum_of_8(before);
             if (tid % 8 == 0 && before < n_out) put(before, Candidate{(uint32_t)(value >> 32), (uint32_t)value, at});
