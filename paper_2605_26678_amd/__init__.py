@@ -777,8 +777,8 @@ class Compressor:
 class PagedCache:
     """Owns a paged cache's pool, table and lengths and hands out its pages, on the host: ``pages`` is what the calls
     take.  ``lens`` (device) is the program's to write; ``reserve`` only sees to it that there are pages.  ``layers`` gives a
-    ``Pages`` for every layer where the sequences are (prompt, layer).  ``reserve`` and ``release`` write tables and lengths
-    where they lie, so recorded graphs go by them, in the current stream's order: that of the calls on the pages."""
+    ``Pages`` for every layer where the sequences are (prompt, layer).  ``reserve``, ``release``, ``fork`` and ``compact`` write tables
+    and lengths where they lie, so recorded graphs go by them, in the current stream's order: that of the calls on the pages."""
 
     def __init__(self, n_seqs: int, H: int, d: int, dtype: int, format: int, n_pages: int, max_rows: int,
                  device="cuda:0"):
@@ -793,6 +793,7 @@ class PagedCache:
         self.lens = torch.zeros(n_seqs * H, dtype=torch.int32, device=device)
         self.pages = Pages(n_seqs, H, d, dtype, format, self.pool, self.table, self.lens)
         self._free = list(range(int(n_pages) - 1, -1, -1))
+        self._users = [0] * int(n_pages)                 # units that hold a page
         self._held = [[] for _ in range(n_seqs * H)]
         self._layers, self.layer_table, self.layer_lens = [], None, None
 
@@ -812,8 +813,9 @@ class PagedCache:
         return list(self._layers)
 
     def _by_layer(self, x, n_layers: int):
-        """[(prompt, layer, head), ...] as a copy [layer, (prompt, head), ...]."""
-        return x.unflatten(0, (self.n_seqs // n_layers, n_layers, self.H)).transpose(0, 1).flatten(1, 2).clone()
+        """[(prompt, layer, head), ...] as a dense copy [layer, (prompt, head), ...]."""
+        import torch
+        return x.unflatten(0, (self.n_seqs // n_layers, n_layers, self.H)).transpose(0, 1).flatten(1, 2).clone(memory_format=torch.contiguous_format)
 
     @property
     def free_pages(self) -> int:
@@ -831,7 +833,7 @@ class PagedCache:
         if sum(more) > len(self._free):
             raise MemoryError(f"{sum(more)} pages are wanted and {len(self._free)} free")
         for h, m in zip(self._held, more):
-            h.extend(self._free.pop() for _ in range(m))
+            h.extend(self._new() for _ in range(m))
         if any(more):
             self._write()
 
@@ -840,7 +842,7 @@ class PagedCache:
         if not 0 <= seq < self.n_seqs:
             raise IndexError(f"sequence {seq} of {self.n_seqs}")
         for u in range(seq * self.H, (seq + 1) * self.H):
-            self._free.extend(reversed(self._held[u]))
+            self._drop(self._held[u])
             self._held[u] = []
         self.lens[seq * self.H:(seq + 1) * self.H] = 0
         if self._layers:
@@ -848,11 +850,102 @@ class PagedCache:
             self.layer_lens[l, p * self.H:(p + 1) * self.H] = 0
         self._write()
 
-    def _write(self) -> None:
+    def _new(self) -> int:
+        page = self._free.pop()
+        self._users[page] = 1
+        return page
+
+    def _drop(self, pages) -> None:
+        for page in reversed(pages):
+            self._users[page] -= 1
+            if not self._users[page]:
+                self._free.append(page)
+
+    def fork(self, parents: Sequence[int], rows: Sequence[int]) -> None:
+        """Every sequence s goes on from what sequence parents[s] holds (itself, where it is s), as the beams of a search do that
+        ``beam_select`` chose; rows: how many every unit holds now.  Full pages are shared from then on.  Of one that is not full the first
+        of a parent's sequences keeps the page, and the others get copies; so they do of pages reserved behind it.  Lengths follow.  With
+        too few pages nothing changes."""
+        import torch
+        parents, rows = [int(x) for x in parents], [int(x) for x in rows]
+        if len(parents) != self.n_seqs or len(rows) != len(self._held) or any(not 0 <= p < self.n_seqs for p in parents):
+            raise ValueError("one parent, a sequence's number, per sequence, and one number of rows per unit")
+        if any(n < 0 or n > PAGE_ROWS * len(h) for n, h in zip(rows, self._held)):
+            raise ValueError("a unit holds no more rows than its pages do")
+        n_layers = len(self._layers) or 1
+        if any(p % n_layers != s % n_layers for s, p in enumerate(parents)):
+            raise ValueError("a sequence goes on from one of its own layer")
+        if parents == list(range(self.n_seqs)):
+            return
+        heir = {}                                        # of a parent, the sequence that keeps its pages: itself before others
+        for s, p in enumerate(parents):
+            if p not in heir or p == s:
+                heir[p] = s
+        held, users, copies = [], [0] * len(self._users), []                  # copies: (unit, its page's number in the unit, page)
+        for s, p in enumerate(parents):
+            for v in range(p * self.H, (p + 1) * self.H):
+                full, mine = rows[v] // PAGE_ROWS, self._held[v]
+                if heir[p] != s and rows[v] % PAGE_ROWS:
+                    copies.append((len(held), full, mine[full]))
+                held.append(list(mine if heir[p] == s else mine[:full]))
+                for page in held[-1]:
+                    users[page] += 1
+        free = [page for page in self._free if not users[page]] + [page for page, n in enumerate(self._users) if n and not users[page]]
+        if len(copies) > len(free):
+            raise MemoryError(f"{len(copies)} pages are wanted and {len(free)} free")
+        if copies:
+            for u, j, _ in copies:
+                held[u].append(free.pop())
+                users[held[u][j]] = 1
+            of = dict(dtype=torch.int32, device=self.pool.device)
+            pages_copy(torch.tensor([page for _, _, page in copies], **of), torch.tensor([held[u][j] for u, j, _ in copies], **of), self.pages)
+        self._held, self._users, self._free = held, users, free
+        at = torch.tensor(parents, device=self.pool.device)
+        self.lens.copy_(self.lens.view(self.n_seqs, self.H)[at].flatten())
+        if self._layers:
+            by_seq = self.layer_lens.view(n_layers, -1, self.H).transpose(0, 1).reshape(self.n_seqs, self.H)
+            self.layer_lens.copy_(self._by_layer(by_seq[at].flatten(), n_layers))
+        self._write()
+
+    def compact(self, kept_idx, head_off, counts: Sequence[int]) -> None:
+        """Thins out all sequences: unit u keeps its rows kept_idx[head_off[u] .. head_off[u + 1] - 1], counts[u] of them, as its rows 0, 1, ..
+        on pages of its own, and gives the others back; lengths follow.  There have to be pages for the rows that stay beside those that
+        are there; with too few nothing changes."""
+        import torch
+        counts = [int(x) for x in counts]
+        if len(counts) != len(self._held) or any(n < 0 for n in counts):
+            raise ValueError("one number of rows per unit")
+        need = [(n + PAGE_ROWS - 1) // PAGE_ROWS for n in counts]
+        if max(need) > self.table.shape[1]:
+            raise ValueError(f"a unit holds {self.table.shape[1] * PAGE_ROWS} rows")
+        if sum(need) > len(self._free):
+            raise MemoryError(f"{sum(need)} pages are wanted and {len(self._free)} free")
+        p = self.pages
+        held = [[self._new() for _ in range(n)] for n in need]
+        to = Pages(p.n_seqs, p.H, p.d, p.dtype, p.format, self.pool, self._table_of(held).to(self.pool.device), self.lens)
+        try:
+            pages_compact(kept_idx, head_off, sum(counts), p, to)
+        except Exception:
+            for pages in held:
+                self._drop(pages)
+            raise
+        for pages in self._held:
+            self._drop(pages)
+        self._held = held
+        self.lens.copy_(torch.tensor(counts, dtype=torch.int32))
+        if self._layers:
+            self.layer_lens.copy_(self._by_layer(self.lens, len(self._layers)))
+        self._write()
+
+    def _table_of(self, held):
         import torch
         host = torch.full(tuple(self.table.shape), -1, dtype=torch.int32)
-        for u, h in enumerate(self._held):
+        for u, h in enumerate(held):
             host[u, :len(h)] = torch.tensor(h, dtype=torch.int32)
+        return host
+
+    def _write(self) -> None:
+        host = self._table_of(self._held)
         self.table.copy_(host)
         if self._layers:
             self.layer_table.copy_(self._by_layer(host, len(self._layers)))

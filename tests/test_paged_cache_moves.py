@@ -1,0 +1,251 @@
+"""PagedCache.fork and compact: whose pages are whose, without a GPU (the calls on the pages are recorded), and on one, what the pages hold."""
+import random
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2605_26678_amd as nkv
+
+DEV = "cuda:0"
+
+
+def _cache(S, H, n_pages, max_rows=400, device="cpu", d=64, fmt=nkv.PAGES_FP4):
+    return nkv.PagedCache(S, H, d, nkv.DTYPE_BF16, fmt, n_pages=n_pages, max_rows=max_rows, device=device)
+
+
+def _consistent(c):
+    """Every page is free or held, as often as it is said to be, and the table says what is held."""
+    users = [0] * len(c._users)
+    for u, held in enumerate(c._held):
+        row = c.table[u].cpu().tolist()
+        assert row[:len(held)] == held and all(x == -1 for x in row[len(held):])
+        for page in held:
+            users[page] += 1
+    assert users == c._users
+    assert sorted(c._free) == [page for page, n in enumerate(users) if n == 0] and len(set(c._free)) == len(c._free)
+
+
+@pytest.fixture
+def recorded(monkeypatch):
+    calls = []
+    monkeypatch.setattr(nkv, "pages_copy", lambda src, dst, pages, stream=None: calls.append((src.tolist(), dst.tolist())))
+    monkeypatch.setattr(nkv, "pages_compact", lambda kept, off, rows, old, new, stream=None: calls.append((rows, old.table.clone(), new.table.clone())))
+    return calls
+
+
+def test_fork_shares_full_pages_and_copies_the_last(recorded):
+    c = _cache(4, 2, 40)
+    rows = [130, 64, 10, 0, 200, 65, 0, 0]
+    c.reserve([r + 64 for r in rows])                       # a page in reserve behind each
+    c.lens.copy_(torch.tensor(rows, dtype=torch.int32))
+    before = [list(h) for h in c._held]
+    c.fork([0, 0, 2, 0], rows)                              # sequence 1 and 3 go on from 0; 2 from itself
+    _consistent(c)
+    assert c._held[0] == before[0] and c._held[1] == before[1] and c._held[4:6] == before[4:6]
+    assert c._held[2][:2] == before[0][:2] and len(c._held[2]) == 3 and c._held[2][2] not in before[0]
+    assert c._held[3] == before[1][:1] and c._held[7] == before[1][:1]         # (full: nothing to copy)
+    (src, dst), = recorded
+    assert src == [before[0][2]] * 2 and dst == [c._held[2][2], c._held[6][2]] and not set(src) & set(dst)
+    assert c.lens.tolist() == [130, 64, 130, 64, 200, 65, 130, 64]
+    c.release(0)
+    _consistent(c)
+    assert c._users[before[0][0]] == 2                      # the other two still read it
+    c.release(1), c.release(3), c.release(2)
+    _consistent(c)
+    assert c.free_pages == 40
+
+
+def test_fork_changes_nothing_where_it_cannot(recorded):
+    c = _cache(3, 1, 4, 128)
+    rows = [100, 70, 0]
+    c.reserve(rows)
+    c.lens.copy_(torch.tensor(rows, dtype=torch.int32))
+    state = ([list(h) for h in c._held], list(c._users), list(c._free), c.table.clone(), c.lens.clone())
+    for bad, kind in ((([0, 1], rows), ValueError), (([0, 1, 3], rows), ValueError), (([0, 1, -1], rows), ValueError), (([0, 1, 1], [100, 70]), ValueError),
+                      (([0, 1, 1], [129, 70, 0]), ValueError), (([0, 1, 1], [100, -1, 0]), ValueError), (([0, 1, 0], rows), MemoryError)):
+        with pytest.raises(kind):
+            c.fork(*bad)
+        assert state[0] == c._held and state[1] == c._users and state[2] == c._free and torch.equal(state[3], c.table) and torch.equal(state[4], c.lens)
+    c.fork([0, 1, 2], rows)                                 # nothing to do
+    c.fork([1, 1, 1], rows)                                 # what the first held is there for the copies
+    _consistent(c)
+    assert len(recorded) == 1 and c.lens.tolist() == [70, 70, 70]
+
+
+def test_fork_follows_layers(recorded):
+    P, L, H = 2, 3, 1
+    c = _cache(P * L, H, 40)
+    c.reserve([64] * 6)
+    c.lens.copy_(torch.arange(1, 7, dtype=torch.int32))
+    layers = c.layers(L)
+    c.layer_lens.add_(10)
+    c.fork([3, 4, 5, 3, 4, 5], [64] * 6)                    # the first prompt goes on from the second, in every layer
+    _consistent(c)
+    assert c.lens.tolist() == [4, 5, 6, 4, 5, 6] and c.layer_lens.tolist() == [[14, 14], [15, 15], [16, 16]]
+    assert all(torch.equal(layers[l].table, c.table.view(P, L, -1)[:, l]) for l in range(L))
+    with pytest.raises(ValueError):
+        c.fork([1, 1, 2, 3, 4, 5], [4, 5, 6, 4, 5, 6])
+
+
+def test_compact_gives_pages_back(recorded):
+    c = _cache(2, 2, 20)
+    rows = [300, 65, 64, 0]
+    c.reserve(rows)
+    c.lens.copy_(torch.tensor(rows, dtype=torch.int32))
+    c.fork([0, 0], rows)
+    before, kept = [list(h) for h in c._held], torch.zeros(0, dtype=torch.int32)
+    counts = [128, 1, 0, 65]
+    c.compact(kept, None, counts)
+    _consistent(c)
+    assert [len(h) for h in c._held] == [2, 1, 0, 2] and c.lens.tolist() == counts and c.free_pages == 15
+    assert not set(sum(before, [])) & set(sum(c._held, []))
+    n, old, new = recorded[-1]
+    assert n == 194 and old[0, 0] == before[0][0] and new[0, 0] == c._held[0][0]
+    for bad, kind in (([1, 1, 1], ValueError), ([1, 1, 1, -1], ValueError), ([1, 1, 1, 10000], ValueError), ([400, 400, 400, 400], MemoryError)):
+        with pytest.raises(kind):
+            c.compact(kept, None, bad)
+        _consistent(c)
+
+
+def test_a_call_that_fails_leaves_the_owner_as_it_was(monkeypatch):
+    def fails(*a, **k):
+        raise nkv.NkvError(nkv.NKV_EHIP, "no")
+    monkeypatch.setattr(nkv, "pages_copy", fails)
+    monkeypatch.setattr(nkv, "pages_compact", fails)
+    c = _cache(2, 1, 10)
+    c.reserve([70, 0])
+    c.lens.copy_(torch.tensor([70, 0], dtype=torch.int32))
+    for call in (lambda: c.fork([0, 0], [70, 0]), lambda: c.compact(None, None, [30, 0])):
+        with pytest.raises(nkv.NkvError):
+            call()
+        _consistent(c)
+        assert c.free_pages == 8 and c.lens.tolist() == [70, 0]
+
+
+def test_many_forks_and_releases(recorded):
+    rng = random.Random(5)
+    c = _cache(6, 2, 60, 640)
+    rows = [0] * 12
+    for _ in range(300):
+        what = rng.random()
+        try:
+            if what < 0.5:
+                more = [min(600, r + rng.choice([0, 1, 40, 64])) for r in rows]
+                c.reserve(more)
+                rows = more
+            elif what < 0.8:
+                parents = [rng.randrange(6) for _ in range(6)]
+                c.fork(parents, rows)
+                rows = [rows[p * 2 + h] for p in parents for h in range(2)]
+            elif what < 0.9:
+                counts = [rng.randint(0, r) for r in rows]
+                c.compact(None, None, counts)
+                rows = counts
+            else:
+                s = rng.randrange(6)
+                c.release(s)
+                rows[2 * s:2 * s + 2] = [0, 0]
+        except MemoryError:
+            pass
+        c.lens.copy_(torch.tensor(rows, dtype=torch.int32))
+        _consistent(c)
+
+
+# ---- on the GPU ----
+
+def _append(c, k, v):
+    c.lens.add_(1)
+    nkv.pages_append(k, v, c.pages)
+
+
+def _all_rows(c, rows):
+    """K and V of every unit, as lists."""
+    off = torch.zeros(len(rows) + 1, dtype=torch.int64)
+    off[1:] = torch.cumsum(torch.tensor(rows), 0)
+    n, d = int(off[-1]), c.pages.d
+    k, v = (torch.empty(n, d, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    nkv.pages_read(k, v, off.to(DEV), n, c.pages)
+    return [(k[a:b].cpu(), v[a:b].cpu()) for a, b in zip(off[:-1].tolist(), off[1:].tolist())]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", [nkv.PAGES_FP4, nkv.PAGES_16BIT])
+def test_a_search_over_pages(fmt):
+    """Prompts read in chunks, beams chosen, sequences reordered, tokens appended, the cache thinned out on the way: at every step the attention is that over the rows
+    that each beam has, kept by the test in lists of its own."""
+    P, B, H, G, d, V, dt = 2, 3, 2, 2, 64, 501, torch.bfloat16
+    S, Hq, scale = P * B, H * G, 0.125
+    g = torch.Generator(device=DEV).manual_seed(3)
+    rand = lambda *s: torch.randn(*s, device=DEV, generator=g).to(dt)  # noqa: E731
+    c = _cache(S, H, 60, 300, DEV, d, fmt)
+    rules = nkv.LogitRules(cap=20.0, window=100, slopes=torch.linspace(0.01, 0.2, Hq, device=DEV), prefix=torch.full((S,), 5, dtype=torch.int32, device=DEV))
+    rows, steps = [0] * (S * H), []
+    # the prompts, the same in a prompt's beams, in chunks
+    for n in (70, 3, 50):
+        k, v, q = (x.repeat_interleave(B, 0).contiguous() for x in (rand(P, n, H, d), rand(P, n, H, d), rand(P, n, Hq, d)))
+        rows = [r + n for r in rows]
+        c.reserve(rows)
+        c.lens.add_(n)
+        nkv.pages_append(k, v, c.pages)
+        steps.append((n, q))
+        _attention_is_right(c, rows, q, scale, rules)
+    scores = torch.full((P, B), -float("inf"), device=DEV)
+    scores[:, 0] = 0.0
+    ws = torch.empty(nkv.beam_workspace_bytes(P, B, V, B), dtype=torch.uint8, device=DEV)
+    out_s, out_b, out_t = torch.empty(P, B, device=DEV), *(torch.empty(P, B, dtype=torch.int32, device=DEV) for _ in range(2))
+    mine = _all_rows(c, rows)
+    for step in range(12):
+        x = rand(P, B, V)
+        nkv.beam_select(x, scores, out_s, out_b, out_t, ws)
+        value = (scores[..., None].double() + torch.log_softmax(x.double(), -1)).flatten(1)
+        best = value.sort(dim=1, descending=True, stable=True)                  # (equal ones: the lower beam, then the lower token)
+        assert torch.equal(out_b.long() * V + out_t.long(), best.indices[:, :B]) and torch.allclose(out_s.double(), best.values[:, :B], atol=1e-5)
+        scores.copy_(out_s)
+        parents = (out_b.cpu() + torch.arange(P)[:, None] * B).flatten().tolist()
+        c.fork(parents, rows)
+        _consistent(c)
+        mine = [mine[p * H + h] for p in parents for h in range(H)]
+        rows = [rows[p * H + h] for p in parents for h in range(H)]
+        k, v, q = rand(S, 1, H, d), rand(S, 1, H, d), rand(S, 1, Hq, d)
+        rows = [r + 1 for r in rows]
+        c.reserve(rows)
+        _append(c, k, v)
+        got = _all_rows(c, rows)
+        for u, (a, b) in enumerate(zip(got, mine)):
+            for x, y in zip(a, b):
+                assert torch.equal(x[:-1], y), f"step {step}, unit {u}"
+        mine = got
+        _attention_is_right(c, rows, q, scale, rules)
+        if step % 5 == 4:
+            r = np.random.RandomState(step)
+            kept = [np.sort(r.choice(n, n * 2 // 3, replace=False)) for n in rows]
+            counts = [len(x) for x in kept]
+            off = torch.zeros(len(rows) + 1, dtype=torch.int64)
+            off[1:] = torch.cumsum(torch.tensor(counts), 0)
+            c.compact(torch.from_numpy(np.concatenate(kept).astype(np.int32)).to(DEV), off.to(DEV), counts)
+            _consistent(c)
+            mine = [(a[x], b[x]) for (a, b), x in zip(mine, kept)]
+            rows = counts
+            for a, b in zip(_all_rows(c, rows), mine):
+                assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def _attention_is_right(c, rows, q, scale, rules):
+    S, n, Hq, d = q.shape
+    out, lse = torch.empty_like(q), torch.empty(S, n, Hq, device=DEV)
+    ws = torch.empty(max(256, nkv.pages_prompt_workspace_bytes(c.pages, Hq, n)), dtype=torch.uint8, device=DEV)
+    nkv.pages_prompt_attention(q, c.pages, Hq, n, scale, out, lse, ws, rules=rules)
+    H, G = c.H, Hq // c.H
+    for u, (k, v) in enumerate(_all_rows(c, rows)):
+        s, h = divmod(u, H)
+        i, r = torch.arange(rows[u]), rows[u] - n + torch.arange(n)[:, None]
+        see = (i <= r) & (i > r - rules.window) | (i < int(rules.prefix[s]))
+        for j in range(h * G, (h + 1) * G):
+            z = rules.cap * torch.tanh(scale * (q[s, :, j].cpu().double() @ k.double().T) / rules.cap) - float(rules.slopes[j]) * (r - i).abs()
+            z = z.masked_fill(~see, -float("inf"))
+            w = torch.softmax(z, -1)
+            # (a weight's rounding and the output's: half a step of bf16 each; 1e-5 for what is computed in 32 bits)
+            bar = 2.0 ** -8 * (w @ v.double().abs() + (w @ v.double()).abs()) + 1e-5 * 5
+            assert ((out[s, :, j].cpu().double() - w @ v.double()).abs() <= bar).all()
+            assert torch.allclose(lse[s, :, j].cpu().double(), torch.logsumexp(z, -1), rtol=1e-5, atol=1e-5)
