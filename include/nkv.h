@@ -451,7 +451,7 @@ int nkv_pages_copy(const int32_t *src, const int32_t *dst, int64_t n, const nkv_
  * is wanted) become rows 0, 1, .. of unit u of `to`, bit by bit, 4-bit rows as the codes and scales that they are.  head_off (int64 [units + 1]) is
  * clamped to `rows`, how many numbers kept_idx (int32) holds.  A number that is no row of the unit, or whose page is none, gives a row of zeros; rows whose
  * page in `to` is none are not written, and neither are those behind a unit's last one on its last page.  The two have the same sequences, heads, rows and
- * format (NKV_ESHAPE) and may share a pool, but no page of `to` is one that `from` reads.  lens of `to` is not read: the caller sets it to the counts.
+ * format (NKV_ESHAPE) and may share a pool, but no page of `to` is one that `from` reads (the same table of the same pool: NKV_EINVAL).  lens of `to` is not read: the caller sets it to the counts.
  */
 int nkv_pages_compact(const int32_t *kept_idx, const int64_t *head_off, int64_t rows, const nkv_pages *from, const nkv_pages *to,
                       void *hip_stream);
@@ -467,7 +467,7 @@ int nkv_pages_compact(const int32_t *kept_idx, const int64_t *head_off, int64_t 
  * A token whose logit is -inf is no candidate, and a beam has none whose score is infinite or NaN (a beam that is not there yet: -inf) or whose log sum is (one of
  * its logits is NaN or +inf, or all are -inf).  Where there are fewer than n_out the rest is score -inf, beam -1, token -1.
  * NKV_ESHAPE: n_beams over NKV_MAX_BEAMS, n_beams * vocab of 2^32 and more, vocab over 2^30, or 2^24 and more stretches of 2048 logits (8192 where there are 1024 and more of these).
- * Deterministic; scratch: nkv_beam_workspace_bytes, n_out * 8 + 8 bytes a stretch.
+ * Deterministic; out_scores may be scores where n_out is n_beams.  Scratch: nkv_beam_workspace_bytes, n_out * 8 + 8 bytes a stretch.
  */
 #define NKV_MAX_BEAMS 1024
 #define NKV_MAX_BEAMS_OUT 64

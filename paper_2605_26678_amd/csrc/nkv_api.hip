@@ -680,6 +680,7 @@ int nkv_pages_compact(const int32_t *kept_idx, const int64_t *head_off, int64_t 
     rc = check_pages(to);
     if (rc) return rc;
     if (from->n_seqs != to->n_seqs || from->H != to->H || from->d != to->d || from->dtype != to->dtype || from->format != to->format) return NKV_ESHAPE;
+    if (from->pool == to->pool && from->table == to->table) return NKV_EINVAL;   // rows would be overwritten before they are read
     if (!head_off || rows < 0 || (rows > 0 && !kept_idx) || (uintptr_t)kept_idx % 4 || (uintptr_t)head_off % 8) return NKV_EINVAL;
     if (!one_launch(rows / NKV_PAGE_ROWS + 2 * (int64_t)to->n_seqs * to->H, 2 * to->d)) return NKV_ESHAPE;   // a workgroup for a page
     return launch_pages_compact(kept_idx, head_off, rows, *from, *to, (hipStream_t)hip_stream) == hipSuccess ? NKV_OK : NKV_EHIP;

@@ -336,8 +336,8 @@ __device__ __forceinline__ double value64(uint64_t k) { return __builtin_bit_cas
 // that reach it one against the other.  (Lists joined in the wavefronts and then in a tree: 8, 12 and 12 us for one prompt of 4 beams and 64 lists of 8, 16 of 8 and 128 lists of 16, 5 of 5 and 125
 // lists of 10.)
 constexpr int kHold = 8;
-__global__ __launch_bounds__(kJoin) void beam_join_kernel(const Head *__restrict__ heads, const Key *__restrict__ keys, const float *__restrict__ scores, int B,
-                                                         int V, int n_out, int stretches, float *__restrict__ out_scores, int32_t *__restrict__ out_beams,
+__global__ __launch_bounds__(kJoin) void beam_join_kernel(const Head *__restrict__ heads, const Key *__restrict__ keys, const float *scores, int B,
+                                                         int V, int n_out, int stretches, float *out_scores, int32_t *__restrict__ out_beams,
                                                          int32_t *__restrict__ out_tokens)
 {
     __shared__ union {

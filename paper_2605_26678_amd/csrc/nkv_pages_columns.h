@@ -689,7 +689,7 @@ template <int D, bool F16, bool FP4, int COLS, bool RULES> __global__ __launch_b
                     // all of the half's rows are seen by all tokens
                     const int r0 = len - a.n_new, r1 = len - 1;
                     if (!(r0 >= 0 && rel >= Q::kStep && (row0 + Q::kStep <= prefix || (least >= Q::kStep && (a.window <= 0 || row0 > r1 - a.window))))) {
-                        const int at = r0 + token, since = a.window > 0 ? at - a.window + 1 : 0;
+                        const int at = r0 + token, since = a.window > 0 ? max(at, 0) - a.window + 1 : 0;
                         const bool some = at >= 0, all = r0 >= 0;          // (a token in front of the unit's first row sees nothing)
                         mask_rows_by_rules<D, F16, FP4>(f, s, g, rel, some ? at + 1 - row0 : 0, some ? since - row0 : 0, some ? prefix - row0 : 0, all ? least : 0,
                                                         all && a.window > 0 ? r1 - a.window + 1 - row0 : 0, all ? prefix - row0 : 0);

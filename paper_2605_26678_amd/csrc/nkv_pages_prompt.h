@@ -43,7 +43,7 @@ struct Seen {
 __device__ __forceinline__ Seen seen_pages(int r0, int r1, int window, int prefix)
 {
     if (r1 < 0) return {0, 0, 0};
-    const int lo = window > 0 ? max(0, r0 - window + 1) / kRows : 0, all = (prefix + kRows - 1) / kRows, front = min(all, lo);
+    const int lo = window > 0 ? max(0, max(r0, 0) - window + 1) / kRows : 0, all = (prefix + kRows - 1) / kRows, front = min(all, lo);
     return {front, lo - front, front + max(r1 / kRows + 1, all) - lo};
 }
 __device__ __forceinline__ int rows_of(int len, int max_pages) { return max(0, min(len, max_pages * kRows)); }

@@ -151,7 +151,7 @@ __global__ __launch_bounds__((Tile<D, F16, FP4>::kThreads), (Tile<D, F16, FP4>::
     const int col = wcol + n;
     const bool there = col < cols;
     const int token = (there ? col : cols - 1) / a.G, head = (there ? col : cols - 1) - token * a.G, at = len - a.n_new + token;
-    const int since = a.window > 0 ? at - a.window + 1 : 0;               // the first row of the lane's window
+    const int since = a.window > 0 ? max(at, 0) - a.window + 1 : 0;       // the first row of the lane's window
     const int64_t row_out = ((int64_t)sq * a.n_new + token) * a.H * a.G + h * a.G + head;
 
     const Seen seen = seen_pages(r_first, r_last, a.window, prefix);
@@ -195,7 +195,7 @@ __global__ __launch_bounds__((Tile<D, F16, FP4>::kThreads), (Tile<D, F16, FP4>::
     auto page_of = [&](int p) { return a.pool + (int64_t)(p >= 0 && p < a.n_pages ? p : 0) * (FP4 ? Fp4Page<D>::kBytes : WidePage<D>::kBytes); };
     // all rows of a page are seen by all tokens on rows r0 .. r1
     auto all_seen = [&](int first, int r0, int r1) { return r0 >= 0 && first + kRows <= len && (first + kRows <= prefix || (first + kRows - 1 <= r0 && (a.window <= 0 || first > r1 - a.window))); };
-    auto none_seen = [&](int first, int r0, int r1) { return first >= prefix && (first > r1 || (a.window > 0 && first + kRows - 1 <= r0 - a.window)); };
+    auto none_seen = [&](int first, int r0, int r1) { return first >= prefix && (first > r1 || (a.window > 0 && first + kRows - 1 <= max(r0, 0) - a.window)); };
 
     Stage<D, F16, FP4> stage;
     int this_id = id_of(begin);

@@ -134,6 +134,16 @@ def test_what_is_no_candidate(dtype):
         assert tokens[2].tolist() == [0] + [-1] * 11 and beams[2, 0] == 5 and abs(got[2, 0] - float(scores[2, 5])) <= BAR
 
 
+def test_scores_in_place():
+    x, scores = _logits(40, 5, 3000, torch.bfloat16, 4)
+    want = _select(x, scores, 5)
+    ws = torch.empty(nkv.beam_workspace_bytes(40, 5, 3000, 5), dtype=torch.uint8, device=DEV)
+    beams, tokens = (torch.empty(40, 5, dtype=torch.int32, device=DEV) for _ in range(2))
+    nkv.beam_select(x, scores, scores, beams, tokens, ws)
+    for g, w in zip((scores, beams, tokens), want):
+        assert np.array_equal(g.cpu().numpy(), w)
+
+
 def test_far_logits():
     x = torch.tensor([[[3e38, -3e38, 2.9e38, 0.0], [1e30, 1e30, 5.0, -1e30]]], device=DEV)
     got, beams, tokens = _select(x, torch.zeros(1, 2, device=DEV), 3)

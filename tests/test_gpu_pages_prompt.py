@@ -129,6 +129,16 @@ def test_lengths(d, dtype, fmt, width):
         check(c, queries(c, n, 4 * G, n), 4 * G, 1 / np.sqrt(d), f"{n} tokens of {G} heads")
 
 
+@pytest.mark.parametrize("width", WIDTHS)
+@pytest.mark.parametrize("dtype,fmt", KINDS)
+def test_the_largest_window_and_tokens_in_front_of_the_first_row(dtype, fmt, width):
+    c = Cache(4, 4, 64, dtype, fmt, EDGES, width=width, seed=2, rows=1.0)
+    for n, G in ((300, 1), (7, 2)):
+        q = queries(c, n, 4 * G, n)
+        for window in ((1 << 31) - 1, 1 << 30, 3):
+            check(c, q, 4 * G, 0.125, f"{n} tokens, window {window}", window=window, prefix=np.array([0, 40, 1 << 30, 20], np.int32))
+
+
 @pytest.mark.parametrize("dtype,fmt", KINDS)
 @pytest.mark.parametrize("d", HEAD_DIMS)
 @pytest.mark.parametrize("width", WIDTHS)

@@ -24,7 +24,8 @@ def test_copy_and_compact_refuse():
         assert L.nkv_pages_copy(src, dst, n, C.byref(p), 0) == status
     for kept, off, rows, status in ((0, FAKE, 1, nkv.NKV_EINVAL), (FAKE, 0, 1, nkv.NKV_EINVAL), (FAKE + 1, FAKE, 1, nkv.NKV_EINVAL), (FAKE, FAKE + 4, 1, nkv.NKV_EINVAL),
                                     (FAKE, FAKE, -1, nkv.NKV_EINVAL), (FAKE, FAKE, 1 << 40, nkv.NKV_ESHAPE), (0, FAKE, 0, nkv.NKV_OK)):
-        assert L.nkv_pages_compact(kept, off, rows, C.byref(p), C.byref(p), 0) == status
+        assert L.nkv_pages_compact(kept, off, rows, C.byref(p), C.byref(_pages(table=2 * FAKE)), 0) == status
+    assert L.nkv_pages_compact(FAKE, FAKE, 0, C.byref(p), C.byref(p), 0) == nkv.NKV_EINVAL                  # onto itself
     for other in (dict(n_seqs=1), dict(H=2), dict(d=64), dict(dtype=nkv.DTYPE_F16), dict(format=nkv.PAGES_16BIT)):
         assert L.nkv_pages_compact(FAKE, FAKE, 1, C.byref(p), C.byref(_pages(**other)), 0) == nkv.NKV_ESHAPE
 
