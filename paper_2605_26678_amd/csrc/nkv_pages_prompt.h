@@ -92,7 +92,7 @@ size_t prompt_token_ws_bytes(const nkv_pages &p, int n_q_heads, int n_new);
 hipError_t launch_prompt_tokens(const PromptArgs &a, const nkv_pages &p, void *ws, hipStream_t st);
 
 // Wavefronts of a workgroup, of 32 columns each: eight, or four where a lane's queries and weighted values take more than half of its registers.
-constexpr int prompt_waves(int d, bool two_pieces) { return d > 128 || (d == 128 && two_pieces) ? 4 : 8; }
+constexpr int prompt_waves(int d, bool two_pieces) { return d == 64 || d > 128 || (d == 128 && two_pieces) ? 4 : 8; }
 template <int D> hipError_t launch_prompt_tiles(const PromptArgs &a, const nkv_pages &p, hipStream_t st);
 
 }  // namespace nkv

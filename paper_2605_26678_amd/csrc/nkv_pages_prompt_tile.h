@@ -27,6 +27,7 @@ using i16x4 = short __attribute__((ext_vector_type(4)));
 template <int D, bool F16, bool FP4> struct Tile {
     static constexpr int kWaves = prompt_waves(D, F16 && FP4), kThreads = kWaves * 64, kCols = kWaves * 32;
     static constexpr bool kTwo = F16 && FP4;                              // two pieces
+    static constexpr int kAtOnce = D == 64 && !kTwo ? 3 : D > 128 || (D == 128 && kTwo) ? 1 : 2;   // wavefronts a SIMD
     static constexpr bool kHalf = F16 && !FP4;                            // the products' type is fp16
     static constexpr int kCpr = D / 8;                                    // 16-byte chunks of a row
     static constexpr int kStride = (D == 96 ? 128 : D) * 2;               // bytes of a row in LDS
@@ -128,7 +129,7 @@ __device__ __forceinline__ float other_half(float x)                      // of 
 // grid: units * tiles * splits.  The unit changes first: a GPU's eight dies take workgroups in turn, so that a die works on few units at a time and finds their pages in its L2.  The
 // last columns, which see the most rows, go first.
 template <int D, bool F16, bool FP4, bool BENT>
-__global__ __launch_bounds__((Tile<D, F16, FP4>::kThreads), (Tile<D, F16, FP4>::kWaves / 4)) void prompt_kernel(const PromptArgs a)
+__global__ __launch_bounds__((Tile<D, F16, FP4>::kThreads), (Tile<D, F16, FP4>::kAtOnce)) void prompt_kernel(const PromptArgs a)
 {
     using T = Tile<D, F16, FP4>;
     constexpr int kSteps = D / 16, kDims = D / 32;                        // of a row's products; of V's dims
