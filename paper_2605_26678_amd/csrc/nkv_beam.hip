@@ -181,9 +181,9 @@ struct ScanArgs {
     Key *keys;                           // [row][stretch][n_out]
 };
 
-// grid: rows * stretches.  E logits a thread, eight at a time: of which thread does not depend on where a row begins, so that equal rows have
-// equal sums.
-template <typename T, int E> __global__ __launch_bounds__(kThreads) void beam_scan_kernel(const ScanArgs a)
+// grid: rows * stretches.  E logits a thread, eight side by side, or (SPREAD, rows of one stretch) a workgroup's width apart, so that short rows have one for as many
+// threads as there are.  Which thread has which does not depend on where a row begins, so that equal rows have equal sums.
+template <typename T, int E, bool SPREAD> __global__ __launch_bounds__(kThreads) void beam_scan_kernel(const ScanArgs a)
 {
     using L = Logits<T>;
     using Words = unsigned int __attribute__((ext_vector_type(4), aligned(sizeof(T))));
@@ -201,8 +201,9 @@ template <typename T, int E> __global__ __launch_bounds__(kThreads) void beam_sc
     uint32_t raw[kVecs][L::kWords];
 #pragma unroll
     for (int j = 0; j < kVecs; ++j) {
-        const int at = first + (j * kThreads + tid) * 8;
-        if (at + 8 <= a.V) {
+        const int at = SPREAD ? tid : first + (j * kThreads + tid) * 8;
+        constexpr int kApart = SPREAD ? kThreads : 1;
+        if (!SPREAD && at + 8 <= a.V) {
 #pragma unroll
             for (int i = 0; i < L::kWords; i += 4) {
                 const Words v = __builtin_nontemporal_load(reinterpret_cast<const Words *>(x + at) + i / 4);
@@ -211,11 +212,12 @@ template <typename T, int E> __global__ __launch_bounds__(kThreads) void beam_sc
         } else {                                                           // the row's end: what is behind it counts as -inf
 #pragma unroll
             for (int i = 0; i < L::kWords; ++i) {
-                if constexpr (std::is_same_v<T, float>) raw[j][i] = at + i < a.V ? reinterpret_cast<const uint32_t *>(x)[at + i] : 0xff800000u;
+                if constexpr (std::is_same_v<T, float>) raw[j][i] = at + i * kApart < a.V ? reinterpret_cast<const uint32_t *>(x)[at + i * kApart] : 0xff800000u;
                 else {
                     constexpr uint32_t none = std::is_same_v<T, f16_t> ? 0xfc00u : 0xff80u;
                     const uint16_t *h = reinterpret_cast<const uint16_t *>(x);
-                    const uint32_t lo = at + 2 * i < a.V ? h[at + 2 * i] : none, hi = at + 2 * i + 1 < a.V ? h[at + 2 * i + 1] : none;
+                    const int lo_at = at + 2 * i * kApart, hi_at = lo_at + kApart;
+                    const uint32_t lo = lo_at < a.V ? h[lo_at] : none, hi = hi_at < a.V ? h[hi_at] : none;
                     raw[j][i] = lo | hi << 16;
                 }
             }
@@ -267,7 +269,9 @@ template <typename T, int E> __global__ __launch_bounds__(kThreads) void beam_sc
 #pragma unroll
             for (int i = 0; i < 8; ++i) takes |= logit<T>(raw[j], i) >= from ? 1u << (8 * j + i) : 0u;
     }
-    auto key_of = [&](int e) { return Key{ord_key(logit_at<T, kVecs>(raw, e)), ~(uint32_t)(first + (e / 8 * kThreads + tid) * 8 + e % 8)}; };
+    auto key_of = [&](int e) {
+        return Key{ord_key(logit_at<T, kVecs>(raw, e)), ~(uint32_t)(SPREAD ? e * kThreads + tid : first + (e / 8 * kThreads + tid) * 8 + e % 8)};
+    };
     for (uint32_t left = takes; left != 0u; left &= left - 1u) {
         const Key k = key_of(__builtin_ctz(left));
         const int at = atomicAdd(&count, 1);
@@ -461,8 +465,12 @@ __global__ __launch_bounds__(kJoin) void beam_join_kernel(const Head *__restrict
     if (tid < n_out) put(tid, list);
 }
 
-// Long stretches where there are enough of them to fill the chip: fewer lists to join.
-int logits_of_thread(const nkv_beams &s) { return (int64_t)s.n_prompts * s.n_beams * ((s.vocab + kThreads * 32 - 1) / (kThreads * 32)) >= 1024 ? 32 : 8; }
+// Long stretches where there are enough of them to fill the chip: fewer lists to join.  (4 x 8 rows of 141945 fp32 logits, 576 of them: 16.0 us, with short
+// ones 24.8.)
+int logits_of_thread(const nkv_beams &s)
+{
+    return s.vocab > kThreads * 8 && (int64_t)s.n_prompts * s.n_beams * ((s.vocab + kThreads * 32 - 1) / (kThreads * 32)) >= 512 ? 32 : 8;
+}
 int stretches_of(const nkv_beams &s)
 {
     const int at_once = kThreads * logits_of_thread(s);
@@ -490,8 +498,9 @@ hipError_t launch_beam_select(const nkv_beams &s, float *out_scores, int32_t *ou
     const unsigned grid = (unsigned)(rows * stretches);
     auto go = [&](auto type) {
         using T = decltype(type);
-        if (logits_of_thread(s) == 32) beam_scan_kernel<T, 32><<<grid, kThreads, 0, st>>>(a);
-        else beam_scan_kernel<T, 8><<<grid, kThreads, 0, st>>>(a);
+        if (logits_of_thread(s) == 32) beam_scan_kernel<T, 32, false><<<grid, kThreads, 0, st>>>(a);
+        else if (stretches == 1) beam_scan_kernel<T, 8, true><<<grid, kThreads, 0, st>>>(a);
+        else beam_scan_kernel<T, 8, false><<<grid, kThreads, 0, st>>>(a);
     };
     if (s.dtype == NKV_DTYPE_F32) go(float{});
     else if (s.dtype == NKV_DTYPE_F16) go(f16_t{});

@@ -91,8 +91,11 @@ template <int N> __device__ __forceinline__ void bend(float (&s)[N], float scale
 size_t prompt_token_ws_bytes(const nkv_pages &p, int n_q_heads, int n_new);
 hipError_t launch_prompt_tokens(const PromptArgs &a, const nkv_pages &p, void *ws, hipStream_t st);
 
-// Wavefronts of a workgroup, of 32 columns each: eight, or four where a lane's queries and weighted values take more than half of its registers.
-constexpr int prompt_waves(int d, bool two_pieces) { return d == 64 || d > 128 || (d == 128 && two_pieces) ? 4 : 8; }
+// Wavefronts of a workgroup, of 32 columns each.  128 dims: eight, one workgroup a compute unit (a chunk of 2048 tokens and 32 heads behind 30720 rows 1120 us, with two of four
+// 1230; 16 prompts of 512 tokens 87 and 94).  64 dims: four, three of them a compute unit (8 prompts of 509 tokens behind 300 that all see 26.9 us, with one of
+// eight 34.6; that chunk 785 and 775).  96 dims: four, two of them (35 prompts of 547 tokens 112 and 127 us; that chunk 966 and 932).  More dims, and two pieces of 128: four, one of
+// them, since a lane's queries and weighted values take more than half of its registers.
+constexpr int prompt_waves(int d, bool two_pieces) { return d == 128 && !two_pieces ? 8 : 4; }
 template <int D> hipError_t launch_prompt_tiles(const PromptArgs &a, const nkv_pages &p, hipStream_t st);
 
 }  // namespace nkv
