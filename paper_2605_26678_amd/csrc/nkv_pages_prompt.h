@@ -7,9 +7,10 @@
 namespace nkv {
 
 // A logit's cap: cap * log2(e) tanh(x), x = product * over_cap; none where cap_log2 is 0.  Products of up to `near` take near_by[0 .. 3] as the coefficients of
-// product^1, 3, 5 and 7.
+// product^1, 3, 5 and 7, those of up to `mid` take mid_by for those up to 11.
 struct Cap {
-    float cap_log2, over_cap, near, near_by[4];
+    float cap_log2, over_cap, near, near_by[4], mid, mid_by[6];
+    bool small;                          // up to 64
 };
 
 // What a call asks for, on its way to the kernels.
@@ -49,9 +50,10 @@ __device__ __forceinline__ Seen seen_pages(int r0, int r1, int window, int prefi
 __device__ __forceinline__ int rows_of(int len, int max_pages) { return max(0, min(len, max_pages * kRows)); }
 
 // A logit in powers of two from a product: scaled, or capped.  |x| <= 5/16, as most logits are that a cap is meant for: tanh(x) as x - x^3 / 3 + .., a minimax polynomial
-// whose relative error is 2^-26, with the scale and the cap in its coefficients; |x| <= 5/8: a longer one, 2^-27.9; beyond: (1 - e^-2x) / (1 + e^-2x), where nothing
-// cancels.
+// whose relative error is 2^-26, with the scale and the cap in its coefficients; |x| <= 5/8: a longer one, 2^-27.9; beyond: (1 - e^-2x) / (1 + e^-2x), which is off by 2^-23 at
+// most, 64 * 2^-23 of a logit capped at 64.  Of larger caps' logits small ones keep to the polynomial, each by itself.
 constexpr double kNear[4] = {1.0, -0.33332862850586767, 0.13309054081886735, -0.049920588703130035}, kNearBound = 0.3125;
+constexpr double kMid[6] = {1.0, -0.3333325982093811, 0.13331127166748047, -0.053721074014902115, 0.020591000095009804, -0.005659991875290871}, kMidBound = 0.625;
 template <int N> __device__ __forceinline__ void bend(float (&s)[N], float scale_log2, const Cap &c)
 {
     if (c.cap_log2 == 0.f) {
@@ -70,21 +72,30 @@ template <int N> __device__ __forceinline__ void bend(float (&s)[N], float scale
         }
         return;
     }
-    const bool any_far = __any(most * c.over_cap > 0.625f);
+    if (!__any(most > c.mid)) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float y = s[i] * s[i];
+            s[i] *= fmaf(y, fmaf(y, fmaf(y, fmaf(y, fmaf(y, c.mid_by[5], c.mid_by[4]), c.mid_by[3]), c.mid_by[2]), c.mid_by[1]), c.mid_by[0]);
+        }
+        return;
+    }
+    auto far = [](float x) {
+        const float e = __builtin_amdgcn_exp2f(fabsf(x) * (-2.f * kToLog2));
+        return copysignf((1.f - e) * __builtin_amdgcn_rcpf(1.f + e), x);
+    };
+    if (c.small) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) s[i] = far(s[i] * c.over_cap) * c.cap_log2;
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const float x = s[i] * c.over_cap, y = x * x;
-        float p = fmaf(y, -0.005659991875290871f, 0.020591000095009804f);
-        p = fmaf(y, p, -0.053721074014902115f);
-        p = fmaf(y, p, 0.13331127166748047f);
-        p = fmaf(y, p, -0.3333325982093811f);
-        p = fmaf(y, p, 1.f) * x;
-        if (any_far) {
-            const float e = __builtin_amdgcn_exp2f(fabsf(x) * (-2.f * kToLog2));
-            const float t = (1.f - e) * __builtin_amdgcn_rcpf(1.f + e);
-            p = fabsf(x) > 0.625f ? copysignf(t, x) : p;
-        }
-        s[i] = p * c.cap_log2;
+        float p = (float)kMid[5];
+#pragma unroll
+        for (int k = 4; k >= 0; --k) p = fmaf(y, p, (float)kMid[k]);
+        s[i] = (fabsf(x) > (float)kMidBound ? far(x) : p * x) * c.cap_log2;
     }
 }
 

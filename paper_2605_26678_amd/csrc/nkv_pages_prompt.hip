@@ -24,13 +24,13 @@ Grid grid_of(const nkv_pages &p, int n_q_heads, int n_new)
 // tiles take a page a microsecond in each workgroup whatever the columns, in one launch or two.  us, theirs / tiles, 8 KV heads of 128 dims:
 //   4 bits    16 columns: 1024 rows of 1, 32 sequences 10.6 / 11.6, 22 / 29; 16384 rows 15 / 24, 110 / 364
 //             32 columns: 1024 rows 11.1 / 11.8, 40 / 29; 4096 rows 12 / 16, 73 / 95; 16384 rows 24 / 25, 214 / 365
-//             64 columns: 4096 rows 15 / 19, 140 / 97
+//             64 columns: 4096 rows 15 / 19, 140 / 97;  one column, 3 rows of 33 sequences with 32 heads 15 / 29
 //   16 bits   8 columns: 600 rows 11.8 / 10.1, 25 / 19; 1024 rows 12.5 / 10.9, 39 / 28; 4096 rows 12.5 / 13.6, 92 / 96; 16384 rows 21 / 23, 284 / 354
 //             32 columns: 4096 rows 19 / 16, 208 / 98
 bool few_columns(const nkv_pages &p, int n_q_heads, int n_new)
 {
     const int64_t cols = (int64_t)(n_q_heads / p.H) * n_new;
-    if (p.max_pages <= kShort) return false;
+    if (p.max_pages <= kShort && p.n_seqs * p.H <= 512) return false;
     return p.format == NKV_PAGES_FP4 ? cols <= (p.max_pages > 32 ? 32 : 16) : cols <= 16 && p.max_pages > 20;
 }
 
@@ -39,12 +39,16 @@ Cap cap_of(double cap, double scale)
     const double x = scale / cap;
     Cap c{};
     c.cap_log2 = pages_scale(cap), c.over_cap = (float)x;
-    // the coefficients' powers, and those of the products that they meet, stay well within fp32
+    c.small = cap <= 64;
+    // the coefficients' powers, and those of the products that they meet, stay well within fp32; otherwise no product is near
+    c.near = c.mid = -1.f;
     if (x >= 0x1p-14 && x <= 0x1p4 && cap >= 0x1p-8 && cap <= 0x1p16) {
         c.near = (float)(kNearBound / x);
         for (int i = 0; i < 4; ++i) c.near_by[i] = (float)(kNear[i] * cap * 1.4426950408889634 * pow(x, 2 * i + 1));
-    } else {
-        c.near = -1.f;
+    }
+    if (x >= 0x1p-10 && x <= 0x1p4 && cap >= 0x1p-4 && cap <= 0x1p16) {
+        c.mid = (float)(kMidBound / x);
+        for (int i = 0; i < 6; ++i) c.mid_by[i] = (float)(kMid[i] * cap * 1.4426950408889634 * pow(x, 2 * i + 1));
     }
     return c;
 }

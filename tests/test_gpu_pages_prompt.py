@@ -147,7 +147,7 @@ def test_rules(d, dtype, fmt, width):
     slopes = slopes_of(6)
     for n in (1, 4, 90) if width is None else (1, 4):
         q = queries(c, n, 6, n, 2.0)
-        for rules in (dict(cap=1.5), dict(cap=6.0), dict(cap=30.0), dict(window=1), dict(window=70), dict(prefix=np.array([100, 0, 500], np.int32)), dict(slopes=slopes),
+        for rules in (dict(cap=1.5), dict(cap=6.0), dict(cap=30.0), dict(cap=100.0), dict(window=1), dict(window=70), dict(prefix=np.array([100, 0, 500], np.int32)), dict(slopes=slopes),
                       dict(window=37, prefix=np.array([65, 129, 2], np.int32)), dict(cap=5.0, window=150, slopes=slopes, prefix=np.array([4, -3, 1 << 30], np.int32))):
             check(c, q, 6, 1 / np.sqrt(d), f"{n} tokens, {rules}", **rules)
 
@@ -226,6 +226,9 @@ def test_scales(n, dtype, fmt, width):
             check(c, q, 4, scale, f"scale {scale}, {rules}", **rules)
     check(c, q, 4, 0.5, "a cap that nothing comes near", cap=1e6)
     check(c, q, 4, 0.5, "a small cap", cap=1e-3)
+    for cap in (0.2, 2.0, 5.0, 20.0, 63.0, 65.0, 300.0):
+        for scale in (0.02, 0.3, 5.0, 40.0):
+            check(c, q, 4, scale, f"scale {scale}, cap {cap}", cap=cap)
 
 
 @pytest.mark.parametrize("width", WIDTHS)
