@@ -53,34 +53,41 @@ template <bool HALF> __device__ __forceinline__ f32x16 product32(const u32x4 &a,
     else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-// A page on its way to LDS.
+// V's rows that go to LDS: those behind the last one become zeros, since 0 times NaN is NaN.  Where some columns do not see all of the rows infinities and NaN become zeros as
+// well, and their rows' bits are set in `odd`: the columns that do see them get a NaN for a logit.
+template <bool HALF> __device__ __forceinline__ u32x4 only_finite(u32x4 y, int row, int valid, uint32_t *odd)
+{
+    constexpr uint32_t e = HALF ? 0x7c00u : 0x7f80u;
+    bool found = false;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const bool lo = (y[w] & e) == e, hi = (y[w] >> 16 & e) == e;
+        found |= lo || hi;
+        y[w] = (lo ? 0u : y[w] & 0xffffu) | (hi ? 0u : y[w] & 0xffff0000u);
+    }
+    if (row >= valid) return u32x4{0u, 0u, 0u, 0u};
+    if (found) atomicOr(odd + row / 32, 1u << row % 32);
+    return y;
+}
+
+// A page on its way to LDS.  ODD: some columns do not see all of its rows, of which `valid` are there.
 template <int D, bool F16, bool FP4> struct Stage {
     using T = Tile<D, F16, FP4>;
-    uint32_t k[T::kItems][FP4 ? 1 : 4], v[T::kItems][FP4 ? 1 : 4];
-    uint8_t ks[T::kItems], vs[T::kItems];
+    uint32_t k[T::kItems][4], v[T::kItems][4];
 
     __device__ __forceinline__ void load(const uint8_t *__restrict__ page, int tid)
     {
+        using P = WidePage<D>;
 #pragma unroll
         for (int i = 0; i < T::kItems; ++i) {
             const int idx = i * T::kThreads + tid;
             if (!T::kEven && idx >= kRows * T::kCpr) break;
             const int row = idx / T::kCpr, c = idx - row * T::kCpr;
-            if constexpr (FP4) {
-                using P = Fp4Page<D>;
-                k[i][0] = *reinterpret_cast<const uint32_t *>(page + P::k_code(row, 8 * c));
-                v[i][0] = load_v_codes<D>(page, row, c);
-                ks[i] = page[P::k_scale(row, c / 4)], vs[i] = page[P::v_scale(row, c / 4)];
-            } else {
-                using P = WidePage<D>;
-                const u32x4 x = *reinterpret_cast<const u32x4 *>(page + P::k(row, 8 * c)), y = *reinterpret_cast<const u32x4 *>(page + P::v(row, 8 * c));
+            const u32x4 x = *reinterpret_cast<const u32x4 *>(page + P::k(row, 8 * c)), y = *reinterpret_cast<const u32x4 *>(page + P::v(row, 8 * c));
 #pragma unroll
-                for (int w = 0; w < 4; ++w) k[i][w] = x[w], v[i][w] = y[w];
-            }
+            for (int w = 0; w < 4; ++w) k[i][w] = x[w], v[i][w] = y[w];
         }
     }
-    // valid: rows that are there; V's others become zeros, since 0 times NaN is NaN.  ODD: some columns do not see all of the rows, so infinities and NaN among V
-    // become zeros as well, and their rows' bits are set in `odd`: the columns that do see them get a NaN for a logit.
     template <bool ODD> __device__ __forceinline__ void store(uint8_t *lds_k, uint8_t *lds_v, int tid, int valid, uint32_t *odd) const
     {
 #pragma unroll
@@ -88,33 +95,82 @@ template <int D, bool F16, bool FP4> struct Stage {
             const int idx = i * T::kThreads + tid;
             if (!T::kEven && idx >= kRows * T::kCpr) break;
             const int row = idx / T::kCpr, c = idx - row * T::kCpr;
-            u32x4 x, y;
-            if constexpr (FP4) {
-                x = codes(k[i][0], ks[i]);
-                y = codes(v[i][0], vs[i]);
-            } else {
-#pragma unroll
-                for (int w = 0; w < 4; ++w) x[w] = k[i][w], y[w] = v[i][w];
-            }
-            if constexpr (ODD) {
-                constexpr uint32_t e = T::kHalf ? 0x7c00u : 0x7f80u;
-                bool found = false;
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const bool lo = (y[w] & e) == e, hi = (y[w] >> 16 & e) == e;
-                    found |= lo || hi;
-                    y[w] = (lo ? 0u : y[w] & 0xffffu) | (hi ? 0u : y[w] & 0xffff0000u);
-                }
-                if (row >= valid) y = u32x4{0u, 0u, 0u, 0u};
-                else if (found) atomicOr(odd + row / 32, 1u << row % 32);
-            }
-            *reinterpret_cast<u32x4 *>(lds_k + row * T::kStride + (c ^ k_swizzle<T::kStride>(row)) * 16) = x;
+            u32x4 y{v[i][0], v[i][1], v[i][2], v[i][3]};
+            if constexpr (ODD) y = only_finite<T::kHalf>(y, row, valid, odd);
+            *reinterpret_cast<u32x4 *>(lds_k + row * T::kStride + (c ^ k_swizzle<T::kStride>(row)) * 16) = u32x4{k[i][0], k[i][1], k[i][2], k[i][3]};
             *reinterpret_cast<u32x4 *>(lds_v + row * T::kStride + (c ^ v_swizzle<T::kStride>(row)) * 16) = y;
         }
     }
-    __device__ __forceinline__ static u32x4 codes(uint32_t w, uint8_t scale)
+};
+
+// 4 bits: pieces of 16 bytes, K's 2 D first, then V's; a wavefront's are all of one kind.  A piece of K is a block of a row, with its scale; of V four rows of 8 dims (of head dims from
+// 192 on: two of 16), with the scales of four rows.  It becomes four chunks.  (A chunk at a time, 4 bytes and a scale each: 83 tokens of 64 heads of 256 dims over 320 units of 1531
+// rows 382 us, so 237.)
+template <int D, bool F16> struct Stage<D, F16, true> {
+    using T = Tile<D, F16, true>;
+    using P = Fp4Page<D>;
+    static constexpr int kOf = 2 * D, kItems = (2 * kOf + T::kThreads - 1) / T::kThreads;
+    u32x4 x[kItems];
+    uint32_t scale[kItems];
+
+    // V's piece: its quad of rows, the first of its rows in the quad, and its first chunk
+    __device__ __forceinline__ static void place(int piece, int &quad, int &half, int &chunk)
     {
-        const float s = __uint_as_float((uint32_t)scale << 23);
+        if constexpr (P::C == 16) {
+            half = 2 * (piece & 1);
+            quad = piece / 2 / (D / 16);
+            chunk = 2 * (piece / 2 - quad * (D / 16));
+        } else {
+            half = 0;
+            quad = piece / (D / 8);
+            chunk = piece - quad * (D / 8);
+        }
+    }
+    __device__ __forceinline__ void load(const uint8_t *__restrict__ page, int tid)
+    {
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) {
+            const int piece = i * T::kThreads + tid;
+            if (2 * kOf % T::kThreads != 0 && piece >= 2 * kOf) break;
+            x[i] = *reinterpret_cast<const u32x4 *>(page + 16 * piece);
+            if (piece < kOf) {
+                scale[i] = page[P::k_scale(piece / P::NB, piece % P::NB)];
+            } else {
+                int quad, half, chunk;
+                place(piece - kOf, quad, half, chunk);
+                scale[i] = *reinterpret_cast<const uint32_t *>(page + P::v_scale(4 * quad, chunk / 4));
+            }
+        }
+    }
+    template <bool ODD> __device__ __forceinline__ void store(uint8_t *lds_k, uint8_t *lds_v, int tid, int valid, uint32_t *odd) const
+    {
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) {
+            const int piece = i * T::kThreads + tid;
+            if (2 * kOf % T::kThreads != 0 && piece >= 2 * kOf) break;
+            if (piece < kOf) {
+                const int row = piece / P::NB, b = piece % P::NB;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    *reinterpret_cast<u32x4 *>(lds_k + row * T::kStride + ((4 * b + j) ^ k_swizzle<T::kStride>(row)) * 16) = codes(x[i][j], scale[i] << 23);
+            } else {
+                int quad, half, chunk;
+                place(piece - kOf, quad, half, chunk);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int of_quad = P::C == 16 ? half + j / 2 : j, row = 4 * quad + of_quad, c = P::C == 16 ? chunk + j % 2 : chunk;
+                    uint32_t w = x[i][j];
+                    if constexpr (P::C == 4) w = (x[i][j / 2] >> 16 * (j % 2) & 0xffffu) | (x[i][2 + j / 2] >> 16 * (j % 2)) << 16;
+                    u32x4 y = codes(w, (scale[i] >> 8 * of_quad & 255u) << 23);
+                    if constexpr (ODD) y = only_finite<false>(y, row, valid, odd);
+                    *reinterpret_cast<u32x4 *>(lds_v + row * T::kStride + (c ^ v_swizzle<T::kStride>(row)) * 16) = y;
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ static u32x4 codes(uint32_t w, uint32_t exponent)
+    {
+        const float s = __uint_as_float(exponent);
         return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1)),
                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3))};
     }
