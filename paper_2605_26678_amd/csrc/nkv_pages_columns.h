@@ -288,6 +288,7 @@ __device__ __forceinline__ void mask_rows(Rows<D, F16, FP4> &f, f32x4 (&s)[Geo<D
         }
 }
 
+__device__ __forceinline__ bool sees_row(int row, int rel, int upto, int from, int front) { return row < rel && ((row < upto && row >= from) || row < front); }
 // The same by rules: a column sees rows from .. upto - 1 of the half and those before `front`, all columns do all_from .. and so on.  Where a row that not all columns see
 // holds a NaN or infinity, its V becomes 0 or 1, and the columns that do see it get a NaN for a product.
 template <int D, bool F16, bool FP4>
@@ -315,20 +316,24 @@ __device__ __forceinline__ void mask_rows_by_rules(Rows<D, F16, FP4> &f, f32x4 (
             else
 #pragma unroll
                 for (int k = 0; k < Q::C / 2; ++k) f.v[t][i * (Q::C / 2) + k] = clear ? 0u : f.v[t][i * (Q::C / 2) + k];
-            const bool sees = row < rel && ((row < upto && row >= from) || row < front);
-            s[t][i] = !sees ? -INFINITY : poison ? __uint_as_float(0x7fc00000u) : s[t][i];
+            s[t][i] = !sees_row(row, rel, upto, from, front) ? -INFINITY : poison ? __uint_as_float(0x7fc00000u) : s[t][i];
         }
 }
 
 // Products to logits in powers of two, by cap and distance.  from: rows between the lane's first one and its token's.
 template <int D, bool F16, bool FP4>
-__device__ __forceinline__ void bend_products(const AttendArgs &a, f32x4 (&s)[Geo<D, F16, FP4>::kTiles], float from, float slope)
+__device__ __forceinline__ void bend_products(const AttendArgs &a, f32x4 (&s)[Geo<D, F16, FP4>::kTiles], float most, float from, float slope)
 {
     constexpr int N = 4 * Geo<D, F16, FP4>::kTiles;
     float z[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) z[i] = s[i / 4][i % 4];
-    bend(z, a.scale_log2, a.cap);
+    if (a.cap.cap_log2 != 0.f) {
+        bend(z, most, a.cap);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] *= a.scale_log2;
+    }
 #pragma unroll
     for (int i = 0; i < N; ++i) s[i / 4][i % 4] = a.slopes ? fmaf(-slope, fabsf(from - (float)(16 * (i / 4) + i % 4)), z[i]) : z[i];
 }
@@ -685,15 +690,21 @@ template <int D, bool F16, bool FP4, int COLS, bool RULES> __global__ __launch_b
             keys_on();
             if constexpr (RULES) {
                 if (works) {
-                    if (a.bent) bend_products<D, F16, FP4>(a, s, (float)(len - a.n_new + token - row0 - 4 * g), slope);
                     // all of the half's rows are seen by all tokens
                     const int r0 = len - a.n_new, r1 = len - 1;
-                    if (!(r0 >= 0 && rel >= Q::kStep && (row0 + Q::kStep <= prefix || (least >= Q::kStep && (a.window <= 0 || row0 > r1 - a.window))))) {
-                        const int at = r0 + token, since = a.window > 0 ? max(at, 0) - a.window + 1 : 0;
-                        const bool some = at >= 0, all = r0 >= 0;          // (a token in front of the unit's first row sees nothing)
-                        mask_rows_by_rules<D, F16, FP4>(f, s, g, rel, some ? at + 1 - row0 : 0, some ? since - row0 : 0, some ? prefix - row0 : 0, all ? least : 0,
-                                                        all && a.window > 0 ? r1 - a.window + 1 - row0 : 0, all ? prefix - row0 : 0);
+                    const bool part = !(r0 >= 0 && rel >= Q::kStep && (row0 + Q::kStep <= prefix || (least >= Q::kStep && (a.window <= 0 || row0 > r1 - a.window))));
+                    const int at = r0 + token, since = a.window > 0 ? max(at, 0) - a.window + 1 : 0;
+                    const bool some = at >= 0, all = r0 >= 0;              // (a token in front of the unit's first row sees nothing)
+                    const int upto = some ? at + 1 - row0 : 0, from = some ? since - row0 : 0, front = some ? prefix - row0 : 0;
+                    if (a.bent) {
+                        float most = 0.f;
+                        if (a.cap.cap_log2 != 0.f)
+#pragma unroll
+                            for (int k = 0; k < 4 * Q::kTiles; ++k) most = !part || sees_row(16 * (k / 4) + 4 * g + k % 4, rel, upto, from, front) ? fmaxf(most, fabsf(s[k / 4][k % 4])) : most;
+                        bend_products<D, F16, FP4>(a, s, most, (float)(len - a.n_new + token - row0 - 4 * g), slope);
                     }
+                    if (part)
+                        mask_rows_by_rules<D, F16, FP4>(f, s, g, rel, upto, from, front, all ? least : 0, all && a.window > 0 ? r1 - a.window + 1 - row0 : 0, all ? prefix - row0 : 0);
                     accumulate<D, F16, FP4, COLS, false>(st, f, s, a.bent ? 1.f : a.scale_log2, slot);
                 }
             } else if (works) {

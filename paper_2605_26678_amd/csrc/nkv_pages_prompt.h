@@ -49,21 +49,14 @@ __device__ __forceinline__ Seen seen_pages(int r0, int r1, int window, int prefi
 }
 __device__ __forceinline__ int rows_of(int len, int max_pages) { return max(0, min(len, max_pages * kRows)); }
 
-// A logit in powers of two from a product: scaled, or capped.  |x| <= 5/16, as most logits are that a cap is meant for: tanh(x) as x - x^3 / 3 + .., a minimax polynomial
+// A capped logit in powers of two from a product.  |x| <= 5/16, as most logits are that a cap is meant for: tanh(x) as x - x^3 / 3 + .., a minimax polynomial
 // whose relative error is 2^-26, with the scale and the cap in its coefficients; |x| <= 5/8: a longer one, 2^-27.9; beyond: (1 - e^-2x) / (1 + e^-2x), which is off by 2^-23 at
-// most, 64 * 2^-23 of a logit capped at 64.  Of larger caps' logits small ones keep to the polynomial, each by itself.
+// most, 64 * 2^-23 of a logit capped at 64.  Of larger caps' logits small ones keep to the polynomial, each by itself.  Every lane, which has one column, chooses by
+// `most`, the largest of its products with rows that the column sees: no other rows have a part in how these are rounded.
 constexpr double kNear[4] = {1.0, -0.33332862850586767, 0.13309054081886735, -0.049920588703130035}, kNearBound = 0.3125;
 constexpr double kMid[6] = {1.0, -0.3333325982093811, 0.13331127166748047, -0.053721074014902115, 0.020591000095009804, -0.005659991875290871}, kMidBound = 0.625;
-template <int N> __device__ __forceinline__ void bend(float (&s)[N], float scale_log2, const Cap &c)
+template <int N> __device__ __forceinline__ void bend(float (&s)[N], float most, const Cap &c)
 {
-    if (c.cap_log2 == 0.f) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) s[i] *= scale_log2;
-        return;
-    }
-    float most = 0.f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) most = fmaxf(most, fabsf(s[i]));
     if (!__any(most > c.near)) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
@@ -72,12 +65,17 @@ template <int N> __device__ __forceinline__ void bend(float (&s)[N], float scale
         }
         return;
     }
-    if (!__any(most > c.mid)) {
+    const bool beyond = most > c.mid;
+    float by[6];                                                           // (two zeros in front leave the short one's bits as they are)
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const float y = s[i] * s[i];
-            s[i] *= fmaf(y, fmaf(y, fmaf(y, fmaf(y, fmaf(y, c.mid_by[5], c.mid_by[4]), c.mid_by[3]), c.mid_by[2]), c.mid_by[1]), c.mid_by[0]);
-        }
+    for (int k = 0; k < 6; ++k) by[k] = most > c.near ? c.mid_by[k] : k < 4 ? c.near_by[k] : 0.f;
+    auto close = [&by](float x) {
+        const float y = x * x;
+        return x * fmaf(y, fmaf(y, fmaf(y, fmaf(y, fmaf(y, by[5], by[4]), by[3]), by[2]), by[1]), by[0]);
+    };
+    if (!__any(beyond)) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) s[i] = close(s[i]);
         return;
     }
     auto far = [](float x) {
@@ -86,7 +84,7 @@ template <int N> __device__ __forceinline__ void bend(float (&s)[N], float scale
     };
     if (c.small) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) s[i] = far(s[i] * c.over_cap) * c.cap_log2;
+        for (int i = 0; i < N; ++i) s[i] = beyond ? far(s[i] * c.over_cap) * c.cap_log2 : close(s[i]);
         return;
     }
 #pragma unroll
@@ -95,7 +93,7 @@ template <int N> __device__ __forceinline__ void bend(float (&s)[N], float scale
         float p = (float)kMid[5];
 #pragma unroll
         for (int k = 4; k >= 0; --k) p = fmaf(y, p, (float)kMid[k]);
-        s[i] = (fabsf(x) > (float)kMidBound ? far(x) : p * x) * c.cap_log2;
+        s[i] = beyond ? (fabsf(x) > (float)kMidBound ? far(x) : p * x) * c.cap_log2 : close(s[i]);
     }
 }
 

@@ -37,6 +37,7 @@ template <int D, bool F16, bool FP4> struct Tile {
     // fp16 weights of up to 2^(6 + 8), see kRoom: those of 2^-30 of the largest one still have all of their bits
     static constexpr float kShift = kHalf ? 6.f : 0.f;
 };
+enum Bends { kStraight, kSloped, kCapped };                                  // logits as they are, less slopes times distances, capped (with slopes or without)
 constexpr int kProducts = 0x8, kReads = 0x100;   // groups of instructions, as sched_group_barrier numbers them
 // A column's maximum is only moved when a logit is more than this above it (in powers of two): weights of up to 2^8 have the bits that those of up to 1 have, and
 // the weighted values in their registers are seldom multiplied.
@@ -184,7 +185,7 @@ __device__ __forceinline__ float other_half(float x)                      // of 
 
 // grid: units * tiles * splits.  The unit changes first: a GPU's eight dies take workgroups in turn, so that a die works on few units at a time and finds their pages in its L2.  The
 // last columns, which see the most rows, go first.
-template <int D, bool F16, bool FP4, bool BENT>
+template <int D, bool F16, bool FP4, Bends BENT>
 __global__ __launch_bounds__((Tile<D, F16, FP4>::kThreads), (Tile<D, F16, FP4>::kAtOnce)) void prompt_kernel(const PromptArgs a)
 {
     using T = Tile<D, F16, FP4>;
@@ -241,7 +242,7 @@ __global__ __launch_bounds__((Tile<D, F16, FP4>::kThreads), (Tile<D, F16, FP4>::
     for (int t = 0; t < kDims; ++t)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
-    const float slope = BENT && a.slopes ? a.slopes[h * a.G + head] * kToLog2 : 0.f;
+    const float slope = BENT != kStraight && a.slopes ? a.slopes[h * a.G + head] * kToLog2 : 0.f;
 
     // the pages' numbers, 64 steps' at a time, one a lane: a load for every step would be waited for at every step
     int ids = -1;
@@ -313,33 +314,46 @@ __global__ __launch_bounds__((Tile<D, F16, FP4>::kThreads), (Tile<D, F16, FP4>::
             for (int i = 0; i < 32; ++i) p[i] = s[i / 16][i % 16];
             const int base = first + 4 * g;                               // p[i] is of row base + row_at(i)
             auto row_at = [](int i) { return 32 * (i / 16) + 8 * (i % 16 / 4) + i % 4; };
-            if constexpr (BENT) {
-                bend(p, a.scale_log2, a.cap);
-                if (a.slopes) {
-                    const float from = (float)(at - base);
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) p[i] = fmaf(-slope, fabsf(from - (float)row_at(i)), p[i]);
-                }
-            }
-            if (!all_seen(first, r_first, r_last)) {
-                // the page's rows that the lane's token sees, a bit each (in front of the unit's first row it sees nothing)
+            // the page's rows that the lane's token sees, a bit each (in front of the unit's first row it sees nothing)
+            const bool some = !all_seen(first, r_first, r_last);
+            uint32_t sees[2] = {~0u, ~0u};
+            if (some) {
                 const int lo = max(since - first, 0), hi = at < 0 ? 0 : min(at + 1 - first, kRows), fr = at < 0 ? 0 : min(prefix - first, kRows);
                 uint64_t bits = hi > lo ? ~0ull >> (kRows - (hi - lo)) << lo : 0ull;
                 bits |= fr > 0 ? ~0ull >> (kRows - fr) : 0ull;
+                sees[0] = (uint32_t)bits >> 4 * g, sees[1] = (uint32_t)(bits >> 32) >> 4 * g;
+            }
+            if constexpr (BENT == kCapped) {                             // (what a token does not see has no part in how the others are capped)
+                float most = 0.f;
+                if (some) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) most = fmaxf(most, __uint_as_float(__float_as_uint(p[i]) & (uint32_t)((int)(sees[i / 16] << (31 - row_at(i % 16))) >> 31) >> 1));
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) most = fmaxf(most, fabsf(p[i]));
+                }
+                bend(p, most, a.cap);
+            }
+            if (BENT == kSloped || (BENT == kCapped && a.slopes)) {
+                const float from = (float)(at - base);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) p[i] = fmaf(-slope, fabsf(from - (float)row_at(i)), BENT == kSloped ? p[i] * a.scale_log2 : p[i]);
+            }
+            if (some) {
                 const uint64_t bad = (uint64_t)odd[(step - begin) % 3][1] << 32 | odd[(step - begin) % 3][0];
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
-                    const uint32_t sees = (uint32_t)(bits >> 32 * t) >> 4 * g, poison = (uint32_t)(bad >> 32 * t) >> 4 * g;
+                    const uint32_t poison = (uint32_t)(bad >> 32 * t) >> 4 * g;
                     if (__any(poison != 0u)) {
 #pragma unroll
                         for (int i = 0; i < 16; ++i) p[16 * t + i] = poison & 1u << row_at(i) ? __uint_as_float(0x7fc00000u) : p[16 * t + i];
                     }
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) p[16 * t + i] = sees & 1u << row_at(i) ? p[16 * t + i] : -INFINITY;
+                    for (int i = 0; i < 16; ++i) p[16 * t + i] = sees[t] & 1u << row_at(i) ? p[16 * t + i] : -INFINITY;
                 }
             }
             // ---- weights ----
-            const float scale = BENT ? 1.f : a.scale_log2;
+            const float scale = BENT != kStraight ? 1.f : a.scale_log2;
             float top = p[0];
 #pragma unroll
             for (int i = 1; i < 32; ++i) top = fmaxf(top, p[i]);
@@ -353,15 +367,16 @@ __global__ __launch_bounds__((Tile<D, F16, FP4>::kThreads), (Tile<D, F16, FP4>::
 #pragma unroll
                     for (int i = 0; i < 16; ++i) o[t][i] *= f;
             }
-            if (__any(fabsf(m) >= kFarMax && m > kNoMax)) {
+            const bool far = fabsf(m) >= kFarMax && m > kNoMax;
+            float factor = scale, less = T::kShift - m;
+            if (__any(far)) {
 #pragma clang fp contract(off)
 #pragma unroll
-                for (int i = 0; i < 32; ++i) p[i] = __builtin_amdgcn_exp2f((p[i] * scale - m) + T::kShift);
-            } else {
-                const float less = T::kShift - m;
-#pragma unroll
-                for (int i = 0; i < 32; ++i) p[i] = __builtin_amdgcn_exp2f(BENT ? p[i] + less : fmaf(p[i], scale, less));
+                for (int i = 0; i < 32; ++i) p[i] = far ? p[i] * scale - m : p[i];
+                if (far) factor = 1.f, less = T::kShift;
             }
+#pragma unroll
+            for (int i = 0; i < 32; ++i) p[i] = __builtin_amdgcn_exp2f(BENT != kStraight ? p[i] + less : fmaf(p[i], factor, less));
             float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < 32; ++i) sum[i % 4] += p[i];
@@ -502,7 +517,7 @@ template <int D> hipError_t launch_prompt_tiles(const PromptArgs &a, const nkv_p
     auto go = [&](auto f16, auto fp4) {
         constexpr bool F16 = decltype(f16)::value, FP4 = decltype(fp4)::value;
         const unsigned groups = (unsigned)((int64_t)a.n_units * a.tiles * a.splits);
-        (a.bent ? prompt_kernel<D, F16, FP4, true> : prompt_kernel<D, F16, FP4, false>)<<<groups, Tile<D, F16, FP4>::kThreads, 0, st>>>(a);
+        (a.cap.cap_log2 != 0.f ? prompt_kernel<D, F16, FP4, kCapped> : a.slopes ? prompt_kernel<D, F16, FP4, kSloped> : prompt_kernel<D, F16, FP4, kStraight>)<<<groups, Tile<D, F16, FP4>::kThreads, 0, st>>>(a);
         constexpr int kAtOnce = 256 / (D / 4);
         if (a.splits > 1) prompt_join_kernel<D, F16><<<(unsigned)(((int64_t)a.n_units * a.n_new * a.G + kAtOnce - 1) / kAtOnce), 256, 0, st>>>(a);
     };

@@ -213,6 +213,42 @@ def test_rows_that_are_not_seen_hold_anything(dtype, fmt, value, width):
                 check(c, q, 3, 0.1, f"{n} tokens", window=2)
 
 
+def _enlarge(c, u, row):
+    """Keys of a row 2^6 times as large: finite, and far beyond any cap."""
+    page = c.pool[c.table[u, row // 64]]
+    if c.fp4:
+        page[op.places(c.d)[2][row % 64]] += 6
+    else:
+        k = page.view(np.uint16).reshape(2, 64, c.d)[0, row % 64]
+        k[:] = (torch.from_numpy(k.view(np.int16).copy()).view(c.torch_dtype) * 64).view(torch.int16).numpy().view(np.uint16)
+
+
+@pytest.mark.parametrize("cap", [0.0, 5.0, 20.0, 50.0, 100.0])
+@pytest.mark.parametrize("width", WIDTHS)
+@pytest.mark.parametrize("dtype,fmt", KINDS)
+def test_rows_that_are_not_seen_leave_every_bit(dtype, fmt, width, cap):
+    """Of other tokens' rows, and of those behind the last one, no part has any: outputs and log sums of the tokens that do not see them are the same to the bit."""
+    for d in (64, 128, 192):
+        for n, G, scale in ((1, 2, 0.1), (3, 2, 0.1), (90, 3, 0.1), (90, 3, 0.9)):
+            if width and n > 3:
+                continue
+            c = Cache(1, 1, d, dtype, fmt, [300], width=width, seed=d, rows=1.0)
+            q = queries(c, n, G, n)
+            rules = dict(cap=cap, window=60, prefix=np.array([7], np.int32))
+            o, l = (x.clone() for x in attend(c, q, G, scale, **rules))
+            # in front of all windows or of some, behind the last one, in the middle of the tokens, the last one
+            rows = [20, 230, 303] + ([299 - n // 2, 299] if n > 1 else [])
+            for row in rows:
+                _enlarge(c, 0, row)
+            o2, l2 = attend(c, q, G, scale, **rules)
+            r = 300 - n + np.arange(n)
+            blind = np.ones(n, bool)
+            for row in rows:
+                blind &= ~((row <= r) & (row > r - 60))
+            assert blind.all() if n == 1 else 0 < blind.sum() < n
+            assert torch.equal(o[:, blind], o2[:, blind]) and torch.equal(l[:, blind], l2[:, blind]), f"{d}, {n}, {scale}"
+
+
 @pytest.mark.parametrize("width", WIDTHS)
 @pytest.mark.parametrize("dtype,fmt", KINDS)
 @pytest.mark.parametrize("n", [1, 2, 40])
