@@ -19,6 +19,10 @@
 // Whole calls, us, and what reading the same bytes alone takes (6.8 TB/s): 36 x 8 units of about 8192 rows, head dim 128, 4 query heads a KV head, bf16, 4
 // bits 65 (kernel 60.1), 49; one layer of them 10.1, 1.4: the launches, and three trips to memory one after the other (lengths, page, rows).  A call that
 // fills the device takes some 10 us beside 4.1 a page and wavefront (6.5 TB/s); the vector and matrix instructions of that page take 2.8.
+//
+// RULES: the pages that a unit's tokens see are its prefix's and its windows', numbered through (seen_pages), so that stretches hold no page that nobody sees; logits are capped and
+// lessened by distances in between; the output is rounded to 16 bits, so that a weight is rounded to them too, one product with V for three.  A decode step of 32 sequences, 8 KV
+// heads of 8 query heads, 4100 of 8193 4-bit rows seen, capped: 36.7 us and 4.7 for the parts; its bytes alone 19.6.
 #pragma once
 
 #include "nkv_pages_prompt.h"

@@ -12,7 +12,8 @@ constexpr int kShort = 4;
 struct Grid {
     int tiles, splits;                   // workgroups of a unit: tiles of columns, and shares of the rows that one sees
 };
-// A compute unit holds one workgroup.  Where the tiles are few, the rows are shared out too, until there is one for (nearly) every compute unit.
+// Where the tiles are few, the rows are shared out too, until there is a workgroup for (nearly) every compute unit.  (More than one of them, where it holds more, would have twice the
+// parts to write and join.)
 Grid grid_of(const nkv_pages &p, int n_q_heads, int n_new)
 {
     const int64_t cols = (int64_t)(n_q_heads / p.H) * n_new, at_once = 32 * prompt_waves(p.d, p.dtype == NKV_DTYPE_F16 && p.format == NKV_PAGES_FP4);

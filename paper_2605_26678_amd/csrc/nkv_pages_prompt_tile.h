@@ -9,6 +9,13 @@
 // in registers (4-bit rows become 16-bit ones there, once for all columns).  K's products are exact; a weight is rounded to the rows' 16 bits, off by half
 // a step of the type that the output is rounded to, and the sum that divides is that of the unrounded ones in fp32.  fp16 rows of 4-bit pages are outside of fp16's range
 // where their scales are: they become bf16, exactly, and queries and weights are two pieces of bf16 then.
+//
+// What bounds it: 2048 tokens of 32 heads of 128 dims behind 30720 rows of 8 KV heads (1.07e12 operations) take 1040 to 1180 us, 0.9 to 1.0 PFLOP/s, by the card and how warm it is; a
+// large matrix product reaches 1.27 on the same cards, and both are held back by power (zeros for inputs: 936 us, and 1.75 PFLOP/s).  The matrix cores are busy for 45 % of the cycles: a
+// wavefront has six vector operations (exponentials, sums, roundings) for a product of 32 x 32 x 16, and a product holds up the SIMD's other wavefront's for 13 of its 32
+// cycles.  LDS is active for 28 % of the cycles, without bank conflicts.  Tried: two groups of wavefronts that a barrier holds in opposite phases (products against
+// exponentials): 1024 for 1046 us there, but 210 for 194 and 40 for 35 us in short prompts, where a page is seen by some wavefronts only; two pages between barriers
+// (-2 %; at 192 dims +20); raised priority for the one or the other phase (no change).
 #pragma once
 
 #include "nkv_pages_prompt.h"
@@ -460,7 +467,7 @@ __global__ __launch_bounds__((Tile<D, F16, FP4>::kThreads), (Tile<D, F16, FP4>::
     if (a.lse && g == 0) a.lse[row_out] = none ? -INFINITY : (m - T::kShift + log2f(l)) * kToLn;
 }
 
-// The splits' parts of a column: D / 4 threads, several columns a workgroup.
+// The splits' parts of a column: D / 4 threads, several columns a workgroup, eight parts asked for at once.  Bound by two trips to memory: 32 columns of 8 parts 3.4 us.
 template <int D, bool F16> __global__ __launch_bounds__(256) void prompt_join_kernel(const PromptArgs a)
 {
     constexpr int kLanes = D / 4, kAtOnce = 256 / kLanes;

@@ -87,6 +87,16 @@ def test_long_stretches(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("left", [1, 7, 255, 419, 2047, 2048, 2049])
+def test_short_last_stretches(left, dtype):
+    # 640 stretches of 8192 and short ones; the best tokens among the latter's too
+    x, scores = _logits(16, 8, 4 * 8192 + left, dtype, left)
+    x[1::2, ..., 4 * 8192:] += 6.0
+    for n_out in (1, 17, 64):
+        _check(x, scores, n_out, f"{left}, {n_out}")
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
 @pytest.mark.parametrize("V", [300, 2500, 9000])
 def test_orders(V, dtype):
     """Rows that hold what is looked for side by side, in ascending and descending order, few values many times, one value only."""
