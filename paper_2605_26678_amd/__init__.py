@@ -863,9 +863,9 @@ class PagedCache:
 
     def fork(self, parents: Sequence[int], rows: Sequence[int]) -> None:
         """Every sequence s goes on from what sequence parents[s] holds (itself, where it is s), as the beams of a search do that
-        ``beam_select`` chose; rows: how many every unit holds now.  Full pages are shared from then on.  Of one that is not full the first
-        of a parent's sequences keeps the page, and the others get copies; so they do of pages reserved behind it.  Lengths follow.  With
-        too few pages nothing changes."""
+        ``beam_select`` chose; rows: how many every unit holds now.  Full pages are shared from then on.  One that is not full stays
+        with one of a parent's sequences (the parent itself, if it goes on), as do pages reserved behind it, and the others get copies of it.
+        Lengths follow.  With too few pages nothing changes."""
         import torch
         parents, rows = [int(x) for x in parents], [int(x) for x in rows]
         if len(parents) != self.n_seqs or len(rows) != len(self._held) or any(not 0 <= p < self.n_seqs for p in parents):

@@ -249,3 +249,18 @@ def _attention_is_right(c, rows, q, scale, rules):
             bar = 2.0 ** -8 * (w @ v.double().abs() + (w @ v.double()).abs()) + 1e-5 * 5
             assert ((out[s, :, j].cpu().double() - w @ v.double()).abs() <= bar).all()
             assert torch.allclose(lse[s, :, j].cpu().double(), torch.logsumexp(z, -1), rtol=1e-5, atol=1e-5)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["fp4", "16bit"])
+def test_the_example_runs(fmt, monkeypatch, capsys):
+    import importlib.util
+    import os
+    import sys
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "paged_beams.py")
+    spec = importlib.util.spec_from_file_location("paged_beams", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    monkeypatch.setattr(sys, "argv", [path, "--format", fmt, "--prompt", "700", "--chunk", "256", "--tokens", "7", "--vocab", "2000", "--beams", "3"])
+    assert example.main() == 0
+    assert f"{fmt} pages" in capsys.readouterr().out
