@@ -4,7 +4,7 @@
 // (beam_scan_kernel) and leaves its maximum, its sum of exponentials and its n_out largest logits; a workgroup for a prompt joins them
 // (beam_join_kernel): the sums in 64 bits, the candidates by their value in 64 bits.
 //
-// us, scan and join (reading the logits alone): one prompt of 4 beams of 32768 fp32 logits 4.8 + 4.4 (0.1), 16 of 8 of 131072 bf16 12.7 + 7.4 (4.8), 5 of 5 of 50021 fp16 6.1 + 6.6 (0.4).
+// us, scan and join (reading the logits alone): one prompt of 4 beams of 32768 fp32 logits 5.0 + 4.3 (0.1), 16 of 8 of 131072 bf16 13.0 + 6.3 (4.8), 5 of 5 of 50021 fp16 6.1 + 6.2 (0.4).
 // The small ones are what a launch takes with a few trips to memory one after the other; in the large one a compute unit's eight workgroups load at once, then bound, gather and count at
 // once, in some 8 us that no load hides.
 //
@@ -356,7 +356,8 @@ __device__ __forceinline__ double value64(uint64_t k) { return __builtin_bit_cas
 // that reach it one against the other.  (Lists joined in the wavefronts and then in a tree: 8, 12 and 12 us for one prompt of 4 beams and 64 lists of 8, 16 of 8 and 128 lists of 16, 5 of 5 and 125
 // lists of 10.)
 constexpr int kHold = 8;
-__global__ __launch_bounds__(kJoin) void beam_join_kernel(const Head *__restrict__ heads, const Key *__restrict__ keys, const float *scores, int B,
+// MANY: more candidates than the threads hold, of which more are left after the first bound: 6 prompts of 32 beams and 11 lists of 64, 15.3 us.  (In one kernel for both 0.3 us more for few.)
+template <bool MANY> __global__ __launch_bounds__(kJoin) void beam_join_kernel(const Head *__restrict__ heads, const Key *__restrict__ keys, const float *scores, int B,
                                                          int V, int n_out, int stretches, float *out_scores, int32_t *__restrict__ out_beams,
                                                          int32_t *__restrict__ out_tokens)
 {
@@ -370,30 +371,35 @@ __global__ __launch_bounds__(kJoin) void beam_join_kernel(const Head *__restrict
     __shared__ double lses[NKV_MAX_BEAMS];
     __shared__ float score_of[NKV_MAX_BEAMS];
     __shared__ uint32_t all_best[kJoin], bounds[kJoinWaves];
-    __shared__ int count;
+    __shared__ int count, again;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), w = __builtin_amdgcn_readfirstlane(tid / kWave), p = blockIdx.x;
     const int parts = B * stretches, in_beam = stretches * n_out;
     const int64_t total = (int64_t)parts * n_out;
     keys += p * total;
     Key held[kHold];
 #pragma unroll
-    for (int k = 0; k < kHold; ++k) held[k] = tid + kJoin * k < total && total <= kJoin * kHold ? keys[tid + kJoin * k] : Key::none();
-    // log sum exp of every beam, NaN for a beam without candidates: where it is not finite, or the beam's score is not
+    for (int k = 0; k < kHold; ++k) held[k] = !MANY && tid + kJoin * k < total ? keys[tid + kJoin * k] : Key::none();
+    // log sum exp of every beam, NaN for a beam without candidates: where it is not finite, or the beam's score is not.  The stretches' sums are of 32 bits and so are their
+    // factors; 64 bits where they are added up and for the logarithm, a thread a beam.  (Factors in 64 bits, and a wavefront a logarithm: 2 us more with 32 beams, 0.2 with a few.)
     for (int b = w; b < B; b += kJoinWaves) {
         const Head *h = heads + ((int64_t)p * B + b) * stretches;
-        const float score = scores[(int64_t)p * B + b];
         const Head first = lane < stretches ? h[lane] : Head{-INFINITY, 0.f};
         float m = first.top;
         for (int i = lane + kWave; i < stretches; i += kWave) m = fmaxf(m, h[i].top);
         m = wave_max(m);
-        auto share = [m](const Head &x) { return x.top == -INFINITY ? (double)x.sum : (double)x.sum * exp((double)x.top - (double)m); };
+        auto share = [m](const Head &x) { return x.top == -INFINITY ? (double)x.sum : (double)(x.sum * __builtin_amdgcn_exp2f((x.top - m) * kLog2e)); };
         double s = share(first);
         for (int i = lane + kWave; i < stretches; i += kWave) s += share(h[i]);
         s = wave_sum(s);
-        const double lse = (double)m + log(s);
-        if (lane == 0) lses[b] = isfinite(lse) && isfinite(score) ? lse : (double)NAN, score_of[b] = score;
+        if (lane == 0) lses[b] = s, score_of[b] = m;
     }
-    if (tid == 0) count = 0;
+    __syncthreads();
+    for (int b = tid; b < B; b += kJoin) {
+        const double lse = (double)score_of[b] + log(lses[b]);
+        const float score = scores[(int64_t)p * B + b];
+        lses[b] = isfinite(lse) && isfinite(score) ? lse : (double)NAN, score_of[b] = score;
+    }
+    if (tid == 0) count = 0, again = 0;
     __syncthreads();
     auto candidate = [&](const Key &k, int b) {
         const double lse = lses[b];
@@ -406,7 +412,7 @@ __global__ __launch_bounds__(kJoin) void beam_join_kernel(const Head *__restrict
 #pragma unroll
     for (int k = 0; k < kHold; ++k) {
         some[k] = Candidate::none();
-        if (kJoin * k >= total || total > kJoin * kHold) continue;
+        if (MANY || kJoin * k >= total) continue;
         some[k] = candidate(held[k], (int)min((uint32_t)(tid + kJoin * k) / (uint32_t)in_beam, (uint32_t)(B - 1)));
         best = max(best, some[k].hi);
     }
@@ -415,21 +421,24 @@ __global__ __launch_bounds__(kJoin) void beam_join_kernel(const Head *__restrict
         for (int i = tid; i < parts; i += kJoin) b = max(b, candidate(keys[(int64_t)i * n_out + r], i / stretches).hi);
         return b;
     };
-    if (total > kJoin * kHold) best = best_at(0);
+    if constexpr (MANY) best = best_at(0);
     uint32_t bound = max(bound_of<kJoinWaves>(best, n_out, all_best, bounds), 1u);   // (0: no candidate)
     // Of many lists a few may hold nearly all: n_out / r lists whose r-th candidates reach a number have n_out that do.
-    if (total > kJoin * kHold)
-        for (int r = 4; r <= n_out; r *= 4) {
+    if constexpr (MANY) {
+        constexpr int kRank = 8;
+        if (n_out >= kRank) {
             __syncthreads();
-            bound = max(bound, bound_of<kJoinWaves>(best_at(r - 1), (n_out + r - 1) / r, all_best, bounds));
+            bound = max(bound, bound_of<kJoinWaves>(best_at(kRank - 1), (n_out + kRank - 1) / kRank, all_best, bounds));
         }
-    auto gather = [&](const Candidate &c) {
+    }
+    auto gather_by = [&](const Candidate &c, int *n) {
         if (c.hi < bound) return false;
-        const int at = atomicAdd(&count, 1);
+        const int at = atomicAdd(n, 1);
         if (at < kGatherJoin) lds.gathered.value[at] = c.value(), lds.gathered.at[at] = c.at;
         return true;
     };
-    if (total <= kJoin * kHold) {
+    auto gather = [&](const Candidate &c) { return gather_by(c, &count); };
+    if constexpr (!MANY) {
 #pragma unroll
         for (int k = 0; k < kHold; ++k) gather(some[k]);
     } else {
@@ -443,7 +452,14 @@ __global__ __launch_bounds__(kJoin) void beam_join_kernel(const Head *__restrict
         }
     }
     __syncthreads();
-    const int found = count;
+    int found = count;
+    if (MANY && found > 2 * n_out + kWave && found <= kGatherJoin) {               // a thread each: a tighter bound, and fewer to count (400 of them 9 us, 200 of them 3)
+        const Candidate c = tid < found ? Candidate{(uint32_t)(lds.gathered.value[tid] >> 32), (uint32_t)lds.gathered.value[tid], lds.gathered.at[tid]} : Candidate::none();
+        bound = max(bound, bound_of<kJoinWaves>(c.hi, n_out, all_best, bounds));
+        gather_by(c, &again);
+        __syncthreads();
+        found = again;
+    }
     auto put = [&](int at, const Candidate &c) {
         const bool none = c.value() == 0ull;
         const uint32_t number = ~c.at;
@@ -525,7 +541,8 @@ hipError_t launch_beam_select(const nkv_beams &s, float *out_scores, int32_t *ou
     if (s.dtype == NKV_DTYPE_F32) go(float{});
     else if (s.dtype == NKV_DTYPE_F16) go(f16_t{});
     else go(uint16_t{});
-    beam_join_kernel<<<(unsigned)s.n_prompts, kJoin, 0, st>>>(heads, keys, s.scores, s.n_beams, s.vocab, s.n_out, stretches, out_scores, out_beams, out_tokens);
+    const bool many = (int64_t)s.n_beams * stretches * s.n_out > kJoin * kHold;
+    (many ? beam_join_kernel<true> : beam_join_kernel<false>)<<<(unsigned)s.n_prompts, kJoin, 0, st>>>(heads, keys, s.scores, s.n_beams, s.vocab, s.n_out, stretches, out_scores, out_beams, out_tokens);
     return hipGetLastError();
 }
 

@@ -97,6 +97,24 @@ def test_short_last_stretches(left, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
+def test_many_lists(dtype):
+    """More lists than a workgroup's threads hold candidates of: the best ones in all beams, in one, in one stretch of it, equal everywhere, equal in one beam, fewer than asked for."""
+    x, scores = _logits(6, 24, 33000, dtype, 11)
+    scores[1], scores[1, 7] = -60.0, 0.0
+    x[2, 5, 20000:20100] += 12.0
+    x[3], x[4, 3] = 1.0, 2.0
+    scores[4] = -1000.0
+    scores[4, 3] = 0.0
+    x[5] = -float("inf")
+    x[5, 20, 32990:] = 1.0
+    for n_out in (7, 8, 48, 64):
+        _check(x, scores, n_out, f"{n_out}")
+    got, beams, tokens = _select(x, scores, 64)
+    assert (beams[1] == 7).all() and (beams[4] == 3).all() and tokens[4].tolist() == list(range(64))
+    assert tokens[5, :10].tolist() == list(range(32990, 33000)) and (tokens[5, 10:] == -1).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
 @pytest.mark.parametrize("V", [300, 2500, 9000])
 def test_orders(V, dtype):
     """Rows that hold what is looked for side by side, in ascending and descending order, few values many times, one value only."""
