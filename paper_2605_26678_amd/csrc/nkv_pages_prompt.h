@@ -105,6 +105,7 @@ hipError_t launch_prompt_tokens(const PromptArgs &a, const nkv_pages &p, void *w
 // eight 34.6; that chunk 785 and 775).  96 dims: four, two of them (35 prompts of 547 tokens 112 and 127 us; that chunk 966 and 932).  More dims, and two pieces of 128: four, one of
 // them, since a lane's queries and weighted values take more than half of its registers.
 constexpr int prompt_waves(int d, bool two_pieces) { return d == 128 && !two_pieces ? 8 : 4; }
+constexpr int prompt_groups(int d, bool two_pieces) { return d == 64 && !two_pieces ? 3 : d <= 96 ? 2 : 1; }   // workgroups a compute unit holds
 template <int D> hipError_t launch_prompt_tiles(const PromptArgs &a, const nkv_pages &p, hipStream_t st);
 
 }  // namespace nkv

@@ -2,6 +2,7 @@
 #include "nkv_pages_prompt.h"
 
 #include <algorithm>
+#include <cmath>
 
 namespace nkv {
 namespace {
@@ -12,13 +13,20 @@ constexpr int kShort = 4;
 struct Grid {
     int tiles, splits;                   // workgroups of a unit: tiles of columns, and shares of the rows that one sees
 };
-// Where the tiles are few, the rows are shared out too, until there is a workgroup for (nearly) every compute unit.  (More than one of them, where it holds more, would have twice the
-// parts to write and join.)
+// Where the tiles are few, the rows are shared out too, up to as many workgroups as the chip holds at once, two pages each at least.  That shortens the walk over the pages, at 0.7 us each
+// and 0.8 for products of 256 columns by 128 dims, but every share's weighted values are written and read again, at some 4 TB/s: the sum is least where both are equal.  us, without
+// shares, with those and with as many as the chip holds (8 by 4 heads of 128 dims where nothing else is said):
+//   512 tokens 24.7, 24.7 (none), 29.2;  100 tokens behind 1000 40, 23.2 (6), 25.2;  256 tokens behind 8192 243, 57.7 (8), 57.7;  twice what it holds 72;  32 heads of 64 dims, 500 tokens
+//   15.3, 15.3 (none), 20.6;  2000 tokens, 4 by 2 heads of 64 dims 39.1, 25.4 (4), 26.4;  4000 tokens, 1 by 8 heads of 96 dims 87, 64 (2), 64;  with one workgroup a compute unit 87
 Grid grid_of(const nkv_pages &p, int n_q_heads, int n_new)
 {
-    const int64_t cols = (int64_t)(n_q_heads / p.H) * n_new, at_once = 32 * prompt_waves(p.d, p.dtype == NKV_DTYPE_F16 && p.format == NKV_PAGES_FP4);
-    const int64_t tiles = (cols + at_once - 1) / at_once, groups = (int64_t)p.n_seqs * p.H * tiles;
-    return {(int)tiles, p.max_pages <= kShort ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(256 / groups, p.max_pages / 2))};
+    const bool two = p.dtype == NKV_DTYPE_F16 && p.format == NKV_PAGES_FP4;
+    const int64_t cols = (int64_t)(n_q_heads / p.H) * n_new, at_once = 32 * prompt_waves(p.d, two), units = (int64_t)p.n_seqs * p.H;
+    const int64_t tiles = (cols + at_once - 1) / at_once, most = std::min<int64_t>(256 * prompt_groups(p.d, two) / (units * tiles), p.max_pages / 2);
+    if (p.max_pages <= kShort || most <= 1) return {(int)tiles, 1};
+    const double walk = p.max_pages * (0.7 + 0.8 * (two ? 2 : 1) * std::min(cols, at_once) * p.d / 32768.0), part = units * cols * (p.d + 4) * 8 / 4e6;
+    const int splits = (int)std::min((double)most, std::max(1.0, std::floor(std::sqrt(walk / part) + 0.5)));
+    return {(int)tiles, splits > 1 && walk / splits + splits * part + 2 < walk ? splits : 1};
 }
 
 // Whether a call goes with the single tokens' kernels.  They share out all units' pages evenly and take up to 16 columns at a time, in some 10 us and what memory takes; the

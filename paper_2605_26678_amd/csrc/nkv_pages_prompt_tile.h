@@ -34,7 +34,7 @@ using i16x4 = short __attribute__((ext_vector_type(4)));
 template <int D, bool F16, bool FP4> struct Tile {
     static constexpr int kWaves = prompt_waves(D, F16 && FP4), kThreads = kWaves * 64, kCols = kWaves * 32;
     static constexpr bool kTwo = F16 && FP4;                              // two pieces
-    static constexpr int kAtOnce = D == 64 && !kTwo ? 3 : D > 128 || (D == 128 && kTwo) ? 1 : 2;   // wavefronts a SIMD
+    static constexpr int kAtOnce = prompt_groups(D, kTwo) * kWaves / 4;    // wavefronts a SIMD
     static constexpr bool kHalf = F16 && !FP4;                            // the products' type is fp16
     static constexpr int kCpr = D / 8;                                    // 16-byte chunks of a row
     static constexpr int kStride = (D == 96 ? 128 : D) * 2;               // bytes of a row in LDS
