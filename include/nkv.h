@@ -443,6 +443,7 @@ int nkv_pages_prompt_attention(const void *q, const nkv_pages *pages, const nkv_
  * Copies whole pages inside the pool, page src[i] to page dst[i] (device, i < n): a sequence that continues another one shares
  * the other's full pages and gets copies of those that it will write.  Pairs of which one is outside [0, n_pages) are left out.  No page is
  * in dst twice or in both dst and src, but where src[i] = dst[i]: such pages' contents are undefined afterwards.  table and lens are not read.
+ * NKV_ESHAPE from 2^22 pairs on.
  */
 int nkv_pages_copy(const int32_t *src, const int32_t *dst, int64_t n, const nkv_pages *pages, void *hip_stream);
 
