@@ -66,6 +66,9 @@ struct AttendArgs {
     int32_t window;
     const float *slopes;
     const int32_t *prefix;
+    // a workgroup a unit
+    void *out;
+    float *lse;
 };
 
 // COLS: columns a workgroup takes, 16, or of 4-bit pages 5 where there are no more: their weights' three pieces then lie side by side in the 16 columns of a
@@ -606,23 +609,34 @@ __device__ __forceinline__ void by_what_is_left(uint32_t left, uint32_t run)
     else __builtin_amdgcn_s_setprio(0);
 }
 
-// grid: (stretches / kWaves, groups of columns)
-template <int D, bool F16, bool FP4, int COLS, bool RULES> __global__ __launch_bounds__(kThreads, groups_at_once(D)) void pages_attend_kernel(const AttendArgs a)
+// Wavefronts of a workgroup that has a unit to itself.
+constexpr int kUnitWaves = 8;
+
+// grid: (stretches / kWaves, groups of columns).  ALONE: (units, groups of columns), a workgroup a unit, whose pages its wavefronts share out; nothing is left to join.
+template <int D, bool F16, bool FP4, int COLS, bool RULES, bool ALONE = false>
+__global__ __launch_bounds__((ALONE ? kUnitWaves * kWave : kThreads), (ALONE ? 2 : groups_at_once(D))) void pages_attend_kernel(const AttendArgs a)
 {
     using Q = Geo<D, F16, FP4, COLS>;
+    constexpr int kWaves = ALONE ? kUnitWaves : nkv::kWaves, kThreads = kWaves * kWave;
     constexpr int kBytes = FP4 ? Fp4Page<D>::kBytes : WidePage<D>::kBytes;
     __shared__ __align__(16) float lds_o[kWaves][16][D + 4];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
     __builtin_amdgcn_s_setprio(3);
-    const Place at = a.n_units <= kWave * kUnitsLane ? placed_by_wave<RULES>(a, w) : placed_by_workgroup<RULES>(a, w);
-    const uint32_t group_lo = at.cut.first(blockIdx.x * kWaves);
-    if (group_lo >= at.total) return;
+    Place at;
+    if constexpr (ALONE) {
+        at.unit = at.unit0 = blockIdx.x, at.joined = true, at.first = 0u;
+    } else {
+        at = a.n_units <= kWave * kUnitsLane ? placed_by_wave<RULES>(a, w) : placed_by_workgroup<RULES>(a, w);
+        const uint32_t group_lo = at.cut.first(blockIdx.x * kWaves);
+        if (group_lo >= at.total) return;
+    }
     // ---- columns ----
     const int cols = a.n_new * a.G, col0 = blockIdx.y * COLS, col = col0 + n % COLS, slot = n / COLS;
     const bool there = col < cols;
     const int token = (there ? col : cols - 1) / a.G, head = (there ? col : cols - 1) - token * a.G;
 
-    const uint32_t stretch = blockIdx.x * kWaves + w, lo = at.cut.first(stretch), hi = at.cut.first(stretch + 1);
+    const uint32_t stretch = blockIdx.x * kWaves + w, all = ALONE ? pages_of<RULES>(a, at.unit) : 0u;
+    const uint32_t lo = ALONE ? all * w / kWaves : at.cut.first(stretch), hi = ALONE ? all * (w + 1) / kWaves : at.cut.first(stretch + 1);
     int u = at.unit;
     uint32_t step = lo - at.first;                                         // page of the unit
     const bool joined = at.joined;
@@ -651,6 +665,18 @@ template <int D, bool F16, bool FP4, int COLS, bool RULES> __global__ __launch_b
                 ll = fmaf(f, l, ll);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) oo[k] = fmaf(f, x[k], oo[k]);
+            }
+            if constexpr (ALONE) {                                         // (as pages_combine_kernel does)
+                const int t = (col0 + c) / a.G, sq = unit / a.H;
+                const int64_t row = ((int64_t)sq * a.n_new + t) * a.H * a.G + (unit - sq * a.H) * a.G + (col0 + c - t * a.G);
+                const bool none = ll == 0.f;                               // (NaN is handed on)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) oo[k] = none ? 0.f : oo[k] / ll;
+                using Out = std::conditional_t<F16, _Float16, __bf16>;
+                using Out4 = Out __attribute__((ext_vector_type(4)));
+                *reinterpret_cast<Out4 *>((Out *)a.out + row * D + e) = Out4{(Out)oo[0], (Out)oo[1], (Out)oo[2], (Out)oo[3]};
+                if (a.lse && e == 0) a.lse[row] = none ? -INFINITY : (mm + log2f(ll)) * kLn2;
+                continue;
             }
             *reinterpret_cast<f32x4 *>(dst + c * (D + 4) + e) = oo;
             if (e == 0) {
@@ -838,6 +864,26 @@ size_t columns_ws_bytes(const nkv_pages &p, int n_q_heads, int n_new)
 {
     const size_t cols = (size_t)(n_q_heads / p.H) * n_new;
     return plan_bytes(p) + ((size_t)groups_of(p) * kWaves + (size_t)p.n_seqs * p.H) * cols * (p.d + 4) * sizeof(float);
+}
+
+// f(head dim, whether rows are fp16, whether pages are of 4 bits), as types
+template <typename F> void for_rows(const nkv_pages &p, F f)
+{
+    for_head_dim(p.d, [&](auto dim) {
+        const bool half = p.dtype == NKV_DTYPE_F16, four = p.format == NKV_PAGES_FP4;
+        if (half && four) f(dim, std::true_type{}, std::true_type{});
+        else if (half) f(dim, std::true_type{}, std::false_type{});
+        else if (four) f(dim, std::false_type{}, std::true_type{});
+        else f(dim, std::false_type{}, std::false_type{});
+    });
+}
+
+// One launch, a workgroup a unit.
+hipError_t launch_units(const AttendArgs &a, const nkv_pages &p, hipStream_t st)
+{
+    const dim3 grid(a.n_units, (unsigned)((a.G * a.n_new + 15) / 16));
+    for_rows(p, [&](auto dim, auto f16, auto fp4) { pages_attend_kernel<decltype(dim)::value, decltype(f16)::value, decltype(fp4)::value, 16, true, true><<<grid, kUnitWaves * kWave, 0, st>>>(a); });
+    return hipGetLastError();
 }
 
 // Both launches of a call; Out: what the output is of.

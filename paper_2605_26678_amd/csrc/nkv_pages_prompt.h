@@ -98,6 +98,7 @@ template <int N> __device__ __forceinline__ void bend(float (&s)[N], float most,
 }
 
 size_t prompt_token_ws_bytes(const nkv_pages &p, int n_q_heads, int n_new);
+hipError_t launch_prompt_units(const PromptArgs &a, const nkv_pages &p, hipStream_t st);
 hipError_t launch_prompt_tokens(const PromptArgs &a, const nkv_pages &p, void *ws, hipStream_t st);
 
 // Wavefronts of a workgroup, of 32 columns each.  128 dims: eight, one workgroup a compute unit (a chunk of 2048 tokens and 32 heads behind 30720 rows 1120 us, with two of four

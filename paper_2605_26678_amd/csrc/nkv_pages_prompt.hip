@@ -43,6 +43,29 @@ bool few_columns(const nkv_pages &p, int n_q_heads, int n_new)
     return p.format == NKV_PAGES_FP4 ? cols <= (p.max_pages > 32 ? 32 : 16) : cols <= 16 && p.max_pages > 20;
 }
 
+// Whether up to 16 columns have a workgroup a unit, in one launch: where that takes less than two launches' 10 us and what memory takes, by the pages that a unit may have, of which it
+// has 0.7 in the mean (the stretches' pages are shared out evenly, a unit's by the workgroup alone).  A workgroup takes a unit's pages at 25 to 34 us a MiB, 4-bit ones 33 to 38, by how many
+// others there are; 4 us for the next one on the same compute unit.  us, alone / otherwise, 8 KV heads of 128 dims:
+//   4 bits    1 sequence of 250, 500, 1024, 2000 rows 6.9 / 10.3, 7.0 / 10.2, 9.6 / 10.2, 13.3 / 10.4;  32 sequences 7.0 / 13.4, 7.4 / 15.3, 10.7 / 20, 15.3 / 24, of 4000 rows 26.6 / 32.4
+//   16 bits   1 sequence 7.7 / 10.9, 10.6 / 10.9, 17.4 / 11.1;  16 sequences 8.5 / 11.1, 13.4 / 14.1, 22.2 / 22.3, of 4000 rows 64.8 / 56.9;  32 9.4 / 11.6, 14.9 / 18.8, 25 / 32, 76 / 100
+//   one token of 33 sequences with 32 KV heads, 3 rows each: 21 / 15 (so: 512 units at most)
+bool alone(const nkv_pages &p, int n_q_heads, int n_new, int64_t pages, double slack = 1.0)
+{
+    const int64_t units = (int64_t)p.n_seqs * p.H, cols = (int64_t)(n_q_heads / p.H) * n_new;
+    if (cols > 16 || units > 512) return false;
+    const bool four = p.format == NKV_PAGES_FP4;
+    const double kib = (four ? p.d * 64 + p.d * 4 : p.d * 256) / 1024.0, full = units / 256.0, share = std::min(1.0, full);
+    const double page = kib * (four ? 0.033 * (1 + 0.15 * share) : 0.025 + 0.009 * share) * std::max(1.0, full);
+    return 5.5 + 4 * (std::max(1.0, full) - 1) + pages * page < slack * ((p.d > 128 ? 14.3 : 10.3) + 0.7 * units * pages * kib / 5500);
+}
+// The same by the rows that a window leaves.  A prefix may hold any rows beside them, how many is on the device: then only where all of a unit's would not take much longer, either.
+bool alone_by_window(const nkv_pages &p, const PromptArgs &a, int n_q_heads, int n_new)
+{
+    if (a.window <= 0) return false;
+    const int64_t pages = std::min<int64_t>(p.max_pages, ((int64_t)a.window + n_new) / NKV_PAGE_ROWS + 2);
+    return alone(p, n_q_heads, n_new, pages) && (!a.prefix || alone(p, n_q_heads, n_new, p.max_pages, 1.5));
+}
+
 Cap cap_of(double cap, double scale)
 {
     const double x = scale / cap;
@@ -73,6 +96,7 @@ bool pages_prompt_one_launch(const nkv_pages &p, int n_q_heads, int n_new)
 
 size_t pages_prompt_ws_bytes(const nkv_pages &p, int n_q_heads, int n_new)
 {
+    if (alone(p, n_q_heads, n_new, p.max_pages)) return 0;
     if (few_columns(p, n_q_heads, n_new)) return prompt_token_ws_bytes(p, n_q_heads, n_new);
     const Grid g = grid_of(p, n_q_heads, n_new);
     return g.splits == 1 ? 0 : (size_t)g.splits * p.n_seqs * (n_q_heads * (size_t)n_new) * (p.d + 4) * sizeof(float);
@@ -94,6 +118,7 @@ hipError_t launch_pages_prompt(const void *q, const nkv_pages &p, const nkv_logi
         a.bent = rules->cap > 0 || rules->slopes;
     }
     a.out = (uint16_t *)out, a.lse = lse, a.part = (float *)ws;
+    if (alone(p, n_q_heads, n_new, p.max_pages) || alone_by_window(p, a, n_q_heads, n_new)) return launch_prompt_units(a, p, st);
     if (few_columns(p, n_q_heads, n_new)) return launch_prompt_tokens(a, p, ws, st);
     const Grid g = grid_of(p, n_q_heads, n_new);
     a.tiles = g.tiles, a.splits = g.splits;

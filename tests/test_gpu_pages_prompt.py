@@ -184,6 +184,28 @@ def test_pages_that_are_none_and_wide_tables(n, dtype, fmt):
     check(c, queries(c, n, 8, 1), 8, 0.1, "lengths")
 
 
+@pytest.mark.parametrize("dtype,fmt", KINDS)
+@pytest.mark.parametrize("d", HEAD_DIMS)
+def test_short_caches(d, dtype, fmt):
+    """Up to 16 columns of units of a few pages, in one launch."""
+    for lens in ([0, 1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 100, 120, 127, 128], [5, 500, 64, 449, 448, 1, 0, 129] * 2):
+        c = Cache(4, 4, d, dtype, fmt, lens, seed=d, rows=1.0)
+        for n, G in ((1, 1), (1, 16), (2, 8), (3, 5), (16, 1)):
+            q = queries(c, n, 4 * G, n)
+            check(c, q, 4 * G, 1 / np.sqrt(d), f"{n} tokens of {G} heads")
+            check(c, q, 4 * G, 0.3, f"{n} tokens of {G} heads, rules", cap=20.0, window=70, slopes=slopes_of(4 * G), prefix=np.array([0, 3, 100, 1000], np.int32))
+
+
+@pytest.mark.parametrize("dtype,fmt", KINDS)
+def test_short_windows_of_long_caches(dtype, fmt):
+    """One launch by the window, without a prefix or with many units; prefixes of any number of pages."""
+    c = Cache(2, 2, 128, dtype, fmt, [1500, 2999, 3, 1111], width=200, seed=3, rows=1.0)
+    for n, window, prefix in ((1, 1, [0, 0]), (1, 64, None), (2, 65, None), (3, 200, [1000, 1400]), (1, 130, [5000, -3]), (1, 700, None)):
+        check(c, queries(c, n, 8, n), 8, 0.1, f"{n} tokens, window {window}, prefix {prefix}", window=window, prefix=None if prefix is None else np.array(prefix, np.int32), cap=30.0)
+    c = Cache(64, 4, 64, dtype, fmt, [65 + u * 7 % 400 for u in range(256)], width=24, seed=4, rows=1.0)
+    check(c, queries(c, 2, 4, 2), 4, 0.1, "many units", window=40, prefix=np.arange(-3, 61, dtype=np.int32) * 5, slopes=slopes_of(4))
+
+
 def _plant(c, u, row, value, key=False, dim=5):
     """Infinity or NaN into a row of V (or K)."""
     page = c.pool[c.table[u, row // 64]]

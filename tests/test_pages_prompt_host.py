@@ -39,10 +39,12 @@ def test_bad_arguments():
         assert _call(heads=heads, new=new) == status
     for kw in (dict(q=0), dict(out=0), dict(q=FAKE + 8), dict(out=FAKE + 2), dict(lse=FAKE + 2), dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=1e39)):
         assert _call(**kw) == nkv.NKV_EINVAL
-    assert L.nkv_pages_prompt_workspace_bytes(C.byref(p), 8, 1, C.byref(n)) == 0 and n.value > 0
+    wide = _pages(max_pages=1000)
+    assert L.nkv_pages_prompt_workspace_bytes(C.byref(wide), 8, 1, C.byref(n)) == 0 and n.value > 0
     for ws, size in ((0, n.value), (FAKE + 16, n.value), (FAKE, n.value - 1)):
-        assert _call(ws=ws, size=size) == nkv.NKV_EWORKSPACE
-    # enough columns: no scratch
+        assert _call(wide, ws=ws, size=size) == nkv.NKV_EWORKSPACE
+    # a short table, or enough columns: no scratch
+    assert L.nkv_pages_prompt_workspace_bytes(C.byref(_pages(max_pages=2)), 8, 1, C.byref(n)) == 0 and n.value == 0
     assert L.nkv_pages_prompt_workspace_bytes(C.byref(p), 32, 4096, C.byref(n)) == 0 and n.value == 0
 
 
