@@ -22,7 +22,8 @@
 //
 // RULES: the pages that a unit's tokens see are its prefix's and its windows', numbered through (seen_pages), so that stretches hold no page that nobody sees; logits are capped and
 // lessened by distances in between; the output is rounded to 16 bits, so that a weight is rounded to them too, one product with V for three.  A decode step of 32 sequences, 8 KV
-// heads of 8 query heads, 4100 of 8193 4-bit rows seen, capped: 36.7 us and 4.7 for the parts; its bytes alone 19.6.
+// heads of 8 query heads, 4100 of 8193 4-bit rows seen, capped: 38.4 us and 4.7 for the parts; its bytes alone 19.6.
+// ALONE: a workgroup of eight wavefronts a unit, with nothing to count at the start and nothing to join at the end: 34.6 us there, in one launch.
 #pragma once
 
 #include "nkv_pages_prompt.h"
