@@ -817,6 +817,10 @@ class PagedCache:
         import torch
         return x.unflatten(0, (self.n_seqs // n_layers, n_layers, self.H)).transpose(0, 1).flatten(1, 2).clone(memory_format=torch.contiguous_format)
 
+    def _by_unit(self, x):
+        """The way back: [layer, (prompt, head)] as [(prompt, layer, head)]."""
+        return x.view(len(self._layers), -1, self.H).transpose(0, 1).flatten()
+
     @property
     def free_pages(self) -> int:
         return len(self._free)
@@ -903,14 +907,13 @@ class PagedCache:
         at = torch.tensor(parents, device=self.pool.device)
         self.lens.copy_(self.lens.view(self.n_seqs, self.H)[at].flatten())
         if self._layers:
-            by_seq = self.layer_lens.view(n_layers, -1, self.H).transpose(0, 1).reshape(self.n_seqs, self.H)
-            self.layer_lens.copy_(self._by_layer(by_seq[at].flatten(), n_layers))
+            self.layer_lens.copy_(self._by_layer(self._by_unit(self.layer_lens).view(self.n_seqs, self.H)[at].flatten(), n_layers))
         self._write()
 
     def compact(self, kept_idx, head_off, counts: Sequence[int]) -> None:
         """Thins out all sequences: unit u keeps its rows kept_idx[head_off[u] .. head_off[u + 1] - 1], counts[u] of them, as its rows 0, 1, ..
-        on pages of its own, and gives the others back; lengths follow.  There have to be pages for the rows that stay beside those that
-        are there; with too few nothing changes."""
+        on pages of its own, and gives the others back; lengths follow.  A unit has the rows that ``lens`` says or, with layers, ``layer_lens`` if that is more.
+        There have to be pages for the rows that stay beside those that are there; with too few nothing changes."""
         import torch
         counts = [int(x) for x in counts]
         if len(counts) != len(self._held) or any(n < 0 for n in counts):
@@ -921,8 +924,11 @@ class PagedCache:
         if sum(need) > len(self._free):
             raise MemoryError(f"{sum(need)} pages are wanted and {len(self._free)} free")
         p = self.pages
+        of = (p.n_seqs, p.H, p.d, p.dtype, p.format, self.pool)
+        if self._layers:                                 # (a program counts its steps in one of the two, and the other stays behind)
+            p = Pages(*of, self.table, torch.maximum(self.lens, self._by_unit(self.layer_lens)))
         held = [[self._new() for _ in range(n)] for n in need]
-        to = Pages(p.n_seqs, p.H, p.d, p.dtype, p.format, self.pool, self._table_of(held).to(self.pool.device), self.lens)
+        to = Pages(*of, self._table_of(held).to(self.pool.device), self.lens)
         try:
             pages_compact(kept_idx, head_off, sum(counts), p, to)
         except Exception:

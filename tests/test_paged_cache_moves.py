@@ -108,6 +108,23 @@ def test_compact_gives_pages_back(recorded):
         _consistent(c)
 
 
+@pytest.mark.parametrize("counted", ["layer_lens", "lens"])
+def test_compact_reads_the_rows_that_the_layers_have(monkeypatch, counted):
+    """A program that goes layer by layer counts its steps in layer_lens, one that goes by the owner's pages in lens: the rows are there either way."""
+    P, L, H = 2, 3, 2
+    c = _cache(P * L, H, 60)
+    start, seen = torch.arange(40, 40 + P * L * H, dtype=torch.int32), []
+    c.reserve([100] * (P * L * H))
+    c.lens.copy_(start)
+    c.layers(L)
+    getattr(c, counted).add_(30)
+    monkeypatch.setattr(nkv, "pages_compact", lambda kept, off, rows, old, new, stream=None: seen.append((old.lens.clone(), old.table.clone())))
+    table = c.table.clone()
+    c.compact(None, None, [5] * (P * L * H))
+    assert torch.equal(seen[0][0], start + 30) and torch.equal(seen[0][1], table)
+    assert c.lens.tolist() == [5] * 12 and c.layer_lens.tolist() == [[5] * 4] * 3
+
+
 def test_a_call_that_fails_leaves_the_owner_as_it_was(monkeypatch):
     def fails(*a, **k):
         raise nkv.NkvError(nkv.NKV_EHIP, "no")
@@ -229,6 +246,45 @@ def test_a_search_over_pages(fmt):
             rows = counts
             for a, b in zip(_all_rows(c, rows), mine):
                 assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", [nkv.PAGES_FP4, nkv.PAGES_16BIT])
+def test_rows_appended_layer_by_layer_are_compacted(fmt):
+    """Lengths that only layer_lens knows of: the rows of every layer's appends stay, bit by bit, and go on from there."""
+    P, L, H, d = 2, 3, 2, 64
+    units = P * L * H
+    g = torch.Generator(device=DEV).manual_seed(6)
+    c = _cache(P * L, H, 100, 300, DEV, d, fmt)
+    c.reserve([200] * units)
+    layers, rows, kept = c.layers(L), 0, None
+
+    def layer_rows(n):
+        """K and V [L, P * H, n, d] by the layers' own pages."""
+        k, v = (torch.empty(L, P * H * n, d, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+        off = torch.arange(P * H + 1, device=DEV) * n
+        for l, p in enumerate(layers):
+            nkv.pages_read(k[l], v[l], off, P * H * n, p)
+        return (x.view(L, P * H, n, d).clone() for x in (k, v))
+
+    for n in (70, 1, 29, 50):
+        if rows == 100:
+            before = [x.cpu() for x in layer_rows(rows)]
+            kept = torch.cat([torch.arange(0, 60, 3), torch.arange(60, 100)])
+            c.compact(kept.int().repeat(units).to(DEV), torch.arange(units + 1, device=DEV) * 60, [60] * units)
+            _consistent(c)
+            rows = 60
+            assert c.lens.tolist() == [60] * units and c.layer_lens.tolist() == [[60] * (P * H)] * L
+            after = [x.cpu() for x in layer_rows(rows)]
+            for a, b in zip(after, before):
+                assert bool((b[:, :, 64:] != 0).any()) and torch.equal(a, b[:, :, kept])
+            c.reserve([120] * units)
+        rows += n
+        c.layer_lens.add_(n)
+        for p in layers:
+            k, v = (torch.randn(P, n, H, d, device=DEV, generator=g).to(torch.bfloat16) for _ in range(2))
+            nkv.pages_append(k, v, p)
+    assert rows == 110 and all(torch.equal(x[:, :, :60].cpu(), y) for x, y in zip(layer_rows(rows), after))
 
 
 def _attention_is_right(c, rows, q, scale, rules):
