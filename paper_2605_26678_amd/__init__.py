@@ -776,8 +776,9 @@ class Compressor:
 
 class PagedCache:
     """Owns a paged cache's pool, table and lengths and hands out its pages, on the host: ``pages`` is what the calls
-    take.  ``lens`` (device) is the program's to write; ``reserve`` only sees to it that there are pages.  ``layers`` gives a
-    ``Pages`` for every layer where the sequences are (prompt, layer).  ``reserve``, ``release``, ``fork`` and ``compact`` write tables
+    take.  ``lens`` (device) is the program's to write; ``reserve`` only sees to it that there are pages: where lengths have gone back
+    below rows that sequences share, ``fork`` gives each its own before the next append.  ``layers`` gives a ``Pages`` for every
+    layer where the sequences are (prompt, layer).  ``reserve``, ``release``, ``fork`` and ``compact`` write tables
     and lengths where they lie, so recorded graphs go by them, in the current stream's order: that of the calls on the pages."""
 
     def __init__(self, n_seqs: int, H: int, d: int, dtype: int, format: int, n_pages: int, max_rows: int,
@@ -868,7 +869,9 @@ class PagedCache:
     def fork(self, parents: Sequence[int], rows: Sequence[int]) -> None:
         """Every sequence s goes on from what sequence parents[s] holds (itself, where it is s), as the beams of a search do that
         ``beam_select`` chose; rows: how many every unit holds now.  Full pages are shared from then on.  One that is not full stays
-        with one of a parent's sequences (the parent itself, if it goes on), as do pages reserved behind it, and the others get copies of it.
+        with one of a parent's sequences (the parent itself, if it goes on), as do pages reserved behind it, and the others get copies of it; so do all where
+        it is one of another unit's full pages.  That is how rows go back that were there at an earlier fork (rejected tokens): lengths as they are
+        to be, and a fork with those rows, each sequence its own parent or another's, before anything is appended.
         Lengths follow.  With too few pages nothing changes."""
         import torch
         parents, rows = [int(x) for x in parents], [int(x) for x in rows]
@@ -879,27 +882,41 @@ class PagedCache:
         n_layers = len(self._layers) or 1
         if any(p % n_layers != s % n_layers for s, p in enumerate(parents)):
             raise ValueError("a sequence goes on from one of its own layer")
-        if parents == list(range(self.n_seqs)):
+        if parents == list(range(self.n_seqs)) and not any(self._users[page] > 1 for n, h in zip(rows, self._held) for page in h[n // PAGE_ROWS:]):
             return
         heir = {}                                        # of a parent, the sequence that keeps its pages: itself before others
         for s, p in enumerate(parents):
             if p not in heir or p == s:
                 heir[p] = s
-        held, users, copies = [], [0] * len(self._users), []                  # copies: (unit, its page's number in the unit, page)
-        for s, p in enumerate(parents):
+        held, users = [], [0] * len(self._users)
+        for p in parents:
             for v in range(p * self.H, (p + 1) * self.H):
-                full, mine = rows[v] // PAGE_ROWS, self._held[v]
-                if heir[p] != s and rows[v] % PAGE_ROWS:
-                    copies.append((len(held), full, mine[full]))
-                held.append(list(mine if heir[p] == s else mine[:full]))
+                held.append(self._held[v][:rows[v] // PAGE_ROWS])
                 for page in held[-1]:
                     users[page] += 1
-        free = [page for page in self._free if not users[page]] + [page for page, n in enumerate(self._users) if n and not users[page]]
+        # A page that is written on has one user.  Where rows went back it may be another unit's full page, or two heirs' last one.
+        units = [(s * self.H + h, p * self.H + h) for keeps in (True, False) for s, p in enumerate(parents) if (heir[p] == s) == keeps for h in range(self.H)]
+        copies = []                                      # (unit, its page's number in the unit, page)
+        for u, v in units:
+            if rows[v] % PAGE_ROWS:
+                full = rows[v] // PAGE_ROWS
+                page = self._held[v][full]
+                held[u].append(page)
+                if users[page]:
+                    copies.append((u, full, page))
+                users[page] = max(users[page], 1)
+        for u, v in units[:len(heir) * self.H]:          # in reserve behind it
+            for page in self._held[v][-(-rows[v] // PAGE_ROWS):]:
+                if not users[page]:
+                    held[u].append(page)
+                    users[page] = 1
+        copies.sort()
+        free = self._free + [page for page, n in enumerate(self._users) if n and not users[page]]
         if len(copies) > len(free):
             raise MemoryError(f"{len(copies)} pages are wanted and {len(free)} free")
         if copies:
             for u, j, _ in copies:
-                held[u].append(free.pop())
+                held[u][j] = free.pop()
                 users[held[u][j]] = 1
             of = dict(dtype=torch.int32, device=self.pool.device)
             pages_copy(torch.tensor([page for _, _, page in copies], **of), torch.tensor([held[u][j] for u, j, _ in copies], **of), self.pages)

@@ -169,6 +169,123 @@ def test_many_forks_and_releases(recorded):
         _consistent(c)
 
 
+def _unfinished_pages_have_one_user(c, rows):
+    for u, (n, held) in enumerate(zip(rows, c._held)):
+        for page in held[n // nkv.PAGE_ROWS:]:
+            assert c._users[page] == 1, f"page {page}, that unit {u} writes from row {n} on, is also another's"
+
+
+def test_fork_after_rows_went_back(recorded):
+    """Rejected drafts: what was a full page, and is shared, is written again."""
+    c = _cache(3, 1, 20)
+    c.reserve([128, 0, 0])
+    c.fork([0, 0, 0], [128, 0, 0])
+    first, last = c._held[0]
+    assert c._held == [[first, last]] * 3
+    rows = [100, 100, 128]
+    c.fork([0, 0, 2], rows)                                 # the last page is sequence 2's, which has all of its rows
+    _consistent(c)
+    _unfinished_pages_have_one_user(c, rows)
+    assert c._held[2] == [first, last] and all(c._held[s][0] == first and len(c._held[s]) == 2 for s in (0, 1))
+    assert recorded == [([last, last], [c._held[0][1], c._held[1][1]])]
+    # every sequence its own parent: one of them keeps the page, and a second call has nothing to do
+    c = _cache(2, 1, 20)
+    c.reserve([128, 0])
+    c.fork([0, 0], [128, 0])
+    first, last = c._held[0]
+    for _ in range(2):
+        c.fork([0, 1], [100, 100])
+        _consistent(c)
+        _unfinished_pages_have_one_user(c, [100, 100])
+        assert c._held[0] == [first, last] and c._held[1][0] == first and recorded[1:] == [([last], [c._held[1][1]])]
+    c.fork([1, 0], [100, 100])                              # (they change places)
+    _consistent(c)
+    _unfinished_pages_have_one_user(c, [100, 100])
+
+
+def test_fork_after_rows_went_back_by_pages(recorded):
+    """Shared pages behind the last row stay with no more than one of those that would write them, and with none where they are another's rows."""
+    c = _cache(3, 1, 8)
+    c.reserve([256, 0, 0])
+    c.fork([0, 0, 0], [256, 0, 0])
+    pages = list(c._held[0])
+    rows = [10, 64, 256]
+    c.fork([0, 1, 2], rows)
+    _consistent(c)
+    _unfinished_pages_have_one_user(c, rows)
+    assert c._held[2] == pages and c._held[1] == pages[:1] and len(c._held[0]) == 1 and recorded == [([pages[0]], c._held[0])]
+    rows = [10, 64, 70]
+    c.fork([0, 1, 2], rows)                                 # (pages that nobody shares stay in reserve)
+    assert c._held[2] == pages
+    rows = [10, 64, 0]
+    c.fork([0, 1, 1], [10, 64, 70])
+    _consistent(c)
+    assert c._held[2] == pages[:1] == c._held[1] and c.free_pages == 6
+    # too few pages: nothing changes
+    c = _cache(2, 1, 2)
+    c.reserve([128, 0])
+    c.fork([0, 0], [128, 0])
+    state = ([list(h) for h in c._held], list(c._users), list(c._free), c.table.clone())
+    with pytest.raises(MemoryError):
+        c.fork([0, 1], [100, 100])
+    assert state[0] == c._held and state[1] == c._users and state[2] == c._free and torch.equal(state[3], c.table)
+    c.fork([0, 1], [64, 100])
+    _consistent(c)
+    _unfinished_pages_have_one_user(c, [64, 100])
+    assert c._held == [state[0][0][:1], state[0][0]]
+
+
+@pytest.mark.parametrize("seed", range(6))
+def test_rows_of_sequences_that_share_pages_stay_theirs(monkeypatch, seed):
+    """Appends, forks, rows that go back, releases: pages as lists of what was written to them.  Every unit's rows are those that it has by itself."""
+    rng, pool, R = random.Random(seed), {}, nkv.PAGE_ROWS
+    S, H, n_pages = 5, 2, 60
+
+    def copy(src, dst, pages, stream=None):
+        src, dst = src.tolist(), dst.tolist()
+        assert not set(src) & set(dst) and len(set(dst)) == len(dst)
+        for a, b in zip(src, dst):
+            pool[b] = list(pool[a])
+
+    monkeypatch.setattr(nkv, "pages_copy", copy)
+    c = _cache(S, H, n_pages, 640)
+    for page in range(n_pages):
+        pool[page] = [None] * R
+    mine, written = [[] for _ in range(S * H)], 0
+    for _ in range(400):
+        what, rows = rng.random(), [len(m) for m in mine]
+        try:
+            if what < 0.5:
+                n = rng.choice([1, 1, 5, 40, 64, 130])
+                more = [min(600, r + n) for r in rows]
+                c.reserve(more)
+                for u, upto in enumerate(more):
+                    for i in range(rows[u], upto):
+                        written += 1
+                        mine[u].append(written)
+                        pool[c._held[u][i // R]][i % R] = written
+            elif what < 0.75:
+                parents = [rng.randrange(S) for _ in range(S)]
+                c.fork(parents, rows)
+                mine = [list(mine[p * H + h]) for p in parents for h in range(H)]
+            elif what < 0.95:
+                back = [max(0, r - rng.choice([0, 0, 1, 3, 64, 100, 200])) for r in rows]
+                parents = list(range(S)) if rng.random() < 0.5 else [rng.randrange(S) for _ in range(S)]
+                c.fork(parents, back)
+                mine = [m[:n] for m, n in zip(mine, back)]
+                mine = [list(mine[p * H + h]) for p in parents for h in range(H)]
+                _unfinished_pages_have_one_user(c, [len(m) for m in mine])
+            else:
+                s = rng.randrange(S)
+                c.release(s)
+                mine[2 * s:2 * s + 2] = [], []
+        except MemoryError:
+            pass
+        _consistent(c)
+        for u, m in enumerate(mine):
+            assert [pool[c._held[u][i // R]][i % R] for i in range(len(m))] == m, f"unit {u}"
+
+
 # ---- on the GPU ----
 
 def _append(c, k, v):
@@ -246,6 +363,36 @@ def test_a_search_over_pages(fmt):
             rows = counts
             for a, b in zip(_all_rows(c, rows), mine):
                 assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", [nkv.PAGES_FP4, nkv.PAGES_16BIT])
+def test_rejected_tokens_of_sequences_that_share_pages(fmt):
+    """Lengths go back below the shared rows, every sequence goes on with tokens of its own: the others' rows stay as they were, bit by bit."""
+    S, H, d = 3, 2, 64
+    g = torch.Generator(device=DEV).manual_seed(8)
+    c = _cache(S, H, 60, 400, DEV, d, fmt)
+
+    def append(n):
+        rows = [r + n for r in c.lens.tolist()]
+        c.reserve(rows)
+        c.lens.add_(n)
+        nkv.pages_append(*(torch.randn(S, n, H, d, device=DEV, generator=g).to(torch.bfloat16) for _ in range(2)), c.pages)
+        return _all_rows(c, rows)
+
+    append(192)
+    c.fork([0, 0, 0], [192] * (S * H))
+    mine = _all_rows(c, [192] * (S * H))
+    for parents, back in (([0, 1, 2], (50, 100, 0)), ([1, 0, 2], (3, 3, 70)), ([0, 0, 2], (90, 0, 1)), ([0, 1, 2], (64, 1, 130))):
+        rows = [len(k) - back[u // H] for u, (k, _) in enumerate(mine)]
+        c.lens.copy_(torch.tensor(rows, dtype=torch.int32))
+        c.fork(parents, rows)
+        _consistent(c)
+        kept = [(mine[p * H + h][0][:rows[p * H + h]], mine[p * H + h][1][:rows[p * H + h]]) for p in parents for h in range(H)]
+        assert c.lens.tolist() == [len(k) for k, _ in kept]
+        mine = append(70)
+        for u, (got, want) in enumerate(zip(mine, kept)):
+            assert all(torch.equal(a[:len(b)], b) for a, b in zip(got, want)), f"unit {u}"
 
 
 @pytest.mark.gpu
