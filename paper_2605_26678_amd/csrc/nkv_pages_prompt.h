@@ -7,7 +7,7 @@
 namespace nkv {
 
 // A logit's cap: cap * log2(e) tanh(x), x = product * over_cap; none where cap_log2 is 0.  Products of up to `near` take near_by[0 .. 3] as the coefficients of
-// product^1, 3, 5 and 7, those of up to `mid` take mid_by for those up to 11.
+// product^1, 3, 5 and 7, those of up to `mid` (no less than near) take mid_by for those up to 11.
 struct Cap {
     float cap_log2, over_cap, near, near_by[4], mid, mid_by[6];
     bool small;                          // up to 64

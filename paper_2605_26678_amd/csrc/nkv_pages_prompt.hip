@@ -73,11 +73,12 @@ Cap cap_of(double cap, double scale)
     c.cap_log2 = pages_scale(cap), c.over_cap = (float)x;
     c.small = cap <= 64;
     // the coefficients' powers, and those of the products that they meet, stay well within fp32; otherwise no product is near
-    c.near = c.mid = -1.f;
+    c.near = -1.f;
     if (x >= 0x1p-14 && x <= 0x1p4 && cap >= 0x1p-8 && cap <= 0x1p16) {
         c.near = (float)(kNearBound / x);
         for (int i = 0; i < 4; ++i) c.near_by[i] = (float)(kNear[i] * cap * 1.4426950408889634 * pow(x, 2 * i + 1));
     }
+    c.mid = c.near;                                                        // without a longer polynomial a column's logits are near or beyond, whatever its neighbours' are
     if (x >= 0x1p-10 && x <= 0x1p4 && cap >= 0x1p-4 && cap <= 0x1p16) {
         c.mid = (float)(kMidBound / x);
         for (int i = 0; i < 6; ++i) c.mid_by[i] = (float)(kMid[i] * cap * 1.4426950408889634 * pow(x, 2 * i + 1));

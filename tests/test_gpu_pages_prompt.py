@@ -271,6 +271,26 @@ def test_rows_that_are_not_seen_leave_every_bit(dtype, fmt, width, cap):
             assert torch.equal(o[:, blind], o2[:, blind]) and torch.equal(l[:, blind], l2[:, blind]), f"{d}, {n}, {scale}"
 
 
+@pytest.mark.parametrize("d,scale,cap", [(128, 128 ** -0.5, 100.0), (128, 1 / 128, 30.0), (256, 1 / 16, 70.0), (64, 0.125, 2000.0), (192, 0.01, 64.0), (128, 0.1, 2e4)])
+@pytest.mark.parametrize("width", WIDTHS)
+@pytest.mark.parametrize("dtype,fmt", KINDS)
+def test_rows_that_are_not_seen_leave_every_bit_under_wide_caps(dtype, fmt, width, d, scale, cap):
+    """Caps of a thousand scales and more, with one polynomial for small logits, and none: how a column's logits are capped does not go by its neighbours'."""
+    for n, G in ((2, 3), (3, 2), (90, 3), (90, 1)):
+        if width and n > 3:
+            continue
+        c = Cache(1, 1, d, dtype, fmt, [300], width=width, seed=d, rows=1.0)
+        q = queries(c, n, G, n)
+        rules = dict(cap=cap, window=60, prefix=np.array([7], np.int32))
+        o, l = (x.clone() for x in check(c, q, G, scale, f"{n} tokens", **rules))
+        for _ in range(2):                                                 # twice: beyond what any polynomial takes
+            _enlarge(c, 0, 300 - n // 2)
+        o2, l2 = attend(c, q, G, scale, **rules)
+        blind = 300 - n + np.arange(n) < 300 - n // 2
+        assert 0 < blind.sum() < n
+        assert torch.equal(o[:, blind], o2[:, blind]) and torch.equal(l[:, blind], l2[:, blind]), f"{n} tokens of {G} heads"
+
+
 @pytest.mark.parametrize("width", WIDTHS)
 @pytest.mark.parametrize("dtype,fmt", KINDS)
 @pytest.mark.parametrize("n", [1, 2, 40])
