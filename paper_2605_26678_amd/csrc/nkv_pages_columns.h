@@ -360,7 +360,7 @@ __device__ __forceinline__ void accumulate(State<D, F16, FP4, COLS> &st, const R
         top = fmaxf(top, p[i]);
     }
     top *= scale_log2;                                                     // (positive, see load_query)
-    bool far = false;
+    bool far = false, own = false;
     if (__any(top > st.m || fabsf(st.m) >= kFar)) {                        // seldom after a unit's first steps
         auto larger = [](float a, float b) { return fmaxf(a, b); };
         top = swap_reduce<32>(swap_reduce<16>(top, larger), larger);
@@ -373,14 +373,17 @@ __device__ __forceinline__ void accumulate(State<D, F16, FP4, COLS> &st, const R
         for (int t = 0; t < Q::C; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i) st.o[t][i] *= f0;
-        far = __any(fabsf(m) >= kFar && m > kNone);                        // (not where a column has seen no row yet)
+        own = fabsf(m) >= kFar && m > kNone;                               // (not where a column has seen no row yet)
+        far = __any(own);
         if (far) {
 #pragma clang fp contract(off)
 #pragma unroll
-            for (int i = 0; i < 4 * Q::kTiles; ++i) p[i] = p[i] * scale_log2 - m;
+            for (int i = 0; i < 4 * Q::kTiles; ++i) p[i] = WHOLE || own ? p[i] * scale_log2 - m : p[i];
         }
     }
-    const float base = Q::kShift - (far ? 0.f : st.m), factor = far ? 1.f : scale_log2;
+    // By rules each column by itself: what others see leaves its weights as they are.
+    const bool rounded = WHOLE ? far : own;
+    const float base = Q::kShift - (rounded ? 0.f : st.m), factor = rounded ? 1.f : scale_log2;
 #pragma unroll
     for (int i = 0; i < 4 * Q::kTiles; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(p[i], factor, base));
     // dims 2 k and 2 k + 1 of row 16 t + 4 g + i, next to each other

@@ -291,6 +291,28 @@ def test_rows_that_are_not_seen_leave_every_bit_under_wide_caps(dtype, fmt, widt
         assert torch.equal(o[:, blind], o2[:, blind]) and torch.equal(l[:, blind], l2[:, blind]), f"{n} tokens of {G} heads"
 
 
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("width", WIDTHS)
+@pytest.mark.parametrize("dtype,fmt", KINDS)
+def test_far_logits_of_other_columns_leave_every_bit(dtype, fmt, width, d):
+    """The last token's logits are beyond 2^24 by its own row, which no other sees."""
+    for n, G in ((2, 8), (3, 5), (90, 3)):
+        if width and n > 3:
+            continue
+        for rules in (dict(), dict(window=200), dict(slopes=slopes_of(G))):
+            c = Cache(1, 1, d, dtype, fmt, [300], width=width, seed=d, rows=1.0)
+            q = queries(c, n, G, n)
+            q[:, -1] *= 8192
+            q[:, -1, 1] = -q[:, -1, 0]                                     # (the row's logit is positive of one of the two)
+            o, l = (x.clone() for x in attend(c, q, G, 0.3, **rules))
+            assert float(l[:, -1].abs().max()) < 2.0 ** 20
+            for _ in range(2):
+                _enlarge(c, 0, 299)
+            o2, l2 = attend(c, q, G, 0.3, **rules)
+            assert float(l2[:, -1].abs().max()) > 2.0 ** 24
+            assert torch.equal(o[:, :-1], o2[:, :-1]) and torch.equal(l[:, :-1], l2[:, :-1]), f"{n} tokens of {G} heads, {list(rules)}"
+
+
 @pytest.mark.parametrize("width", WIDTHS)
 @pytest.mark.parametrize("dtype,fmt", KINDS)
 @pytest.mark.parametrize("n", [1, 2, 40])
