@@ -467,7 +467,8 @@ int nkv_pages_compact(const int32_t *kept_idx, const int64_t *head_off, int64_t 
  * themselves.  Which tokens of a beam are in goes by their logits, those too that lie so near to each other that their values are equal in 64 bits.
  * A token whose logit is -inf is no candidate, and a beam has none whose score is infinite or NaN (a beam that is not there yet: -inf) or whose log sum is (one of
  * its logits is NaN or +inf, or all are -inf).  Where there are fewer than n_out the rest is score -inf, beam -1, token -1.
- * NKV_ESHAPE: n_beams over NKV_MAX_BEAMS, n_beams * vocab of 2^32 and more, vocab over 2^30, or 2^24 and more stretches of 2048 logits (8192 where there are 512 and more of these).
+ * NKV_ESHAPE: n_beams over NKV_MAX_BEAMS, n_beams * vocab of 2^32 and more, vocab over 2^30, 2^22 and more prompts, or 2^24 and more stretches of 2048 logits (8192 where there are 512 and more
+ * of these).
  * Deterministic; out_scores may be scores where n_out is n_beams.  Scratch: nkv_beam_workspace_bytes, n_out * 8 + 8 bytes a stretch.
  */
 #define NKV_MAX_BEAMS 1024

@@ -518,7 +518,12 @@ size_t up(size_t x) { return (x + 255) / 256 * 256; }
 
 }  // namespace
 
-bool beam_one_launch(const nkv_beams &s) { return (int64_t)s.n_prompts * s.n_beams < (1 << 24) && (int64_t)s.n_prompts * s.n_beams * stretches_of(s) < (1 << 24); }
+bool beam_one_launch(const nkv_beams &s)
+{
+    // fewer than 2^32 threads: 1024 a prompt where its lists are joined, 256 a stretch
+    const int64_t rows = (int64_t)s.n_prompts * s.n_beams;
+    return s.n_prompts < (1 << 22) && rows < (1 << 24) && rows * stretches_of(s) < (1 << 24);
+}
 
 size_t beam_ws_bytes(const nkv_beams &s)
 {

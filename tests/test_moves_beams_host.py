@@ -50,6 +50,16 @@ def test_beams_refuse(kw, status):
     assert L.nkv_beam_select(C.byref(_beams(**kw)), FAKE, FAKE, FAKE, FAKE, 1 << 40, 0) == status
 
 
+def test_beams_of_more_prompts_than_one_launch_joins():
+    """A workgroup of 1024 threads a prompt, and fewer than 2^32 threads."""
+    L, n = nkv.lib(), C.c_size_t(0)
+    for prompts, status in (((1 << 22) - 1, nkv.NKV_OK), (1 << 22, nkv.NKV_ESHAPE), ((1 << 24) - 1, nkv.NKV_ESHAPE)):
+        b = _beams(n_prompts=prompts, n_beams=1, vocab=5, n_out=4)
+        assert L.nkv_beam_workspace_bytes(C.byref(b), C.byref(n)) == status
+        if status:
+            assert L.nkv_beam_select(C.byref(b), FAKE, FAKE, FAKE, FAKE, 1 << 40, 0) == status
+
+
 def test_beams_refuse_outputs_and_scratch():
     L, n, b = nkv.lib(), C.c_size_t(0), _beams()
     assert L.nkv_beam_workspace_bytes(C.byref(b), None) == nkv.NKV_EINVAL and L.nkv_beam_workspace_bytes(None, C.byref(n)) == nkv.NKV_EINVAL
