@@ -424,7 +424,10 @@ int nkv_pages_attention(const void *q, const nkv_pages *pages, int32_t n_q_heads
  * rows, fp16's 11 for fp16 rows (two pieces of bf16 on 4-bit pages), so an output is off by that much of its largest terms at most, as its own rounding is.
  * scale as for nkv_pages_attention; NKV_EINVAL for a negative or NaN cap, and one that, or whose quotient with the scale, is not within 1e-30 and fp32's range;
  * slopes are finite.
- * Scratch: nkv_pages_prompt_workspace_bytes, 0 where the columns fill the chip or the tables are short (ws may be NULL then), some 35 MiB at most for heads of 128 dims where the rows are shared out.
+ * Scratch: nkv_pages_prompt_workspace_bytes.  0 where the columns fill the chip or the tables are short (ws may be NULL then); where the rows are shared out among
+ * tiles of columns 33 MiB at most, whatever the sizes.  Of few columns C = n_new * G of a unit (up to 16 on tables of more than 20 pages, on 4-bit pages up to 16 on any and to 32 on
+ * more than 32 pages) as for nkv_pages_attention, (stretches + units) * C * (d + 4) * 4 bytes and 16 a unit, which grows with the units: 8 KV heads of 128 dims, 32 columns, 50 MiB for a
+ * sequence, 83 for 256 of them and 182 for 1024.
  * NKV_ESHAPE from 2^30 columns (n_new * G) of a unit, and 2^23 pieces of 128 columns of all units, on.  Deterministic.
  */
 typedef struct nkv_logit_rules {

@@ -58,6 +58,29 @@ def test_scratch_is_bounded():
                     assert n.value < 80 << 20
 
 
+@pytest.mark.parametrize("fmt", [nkv.PAGES_16BIT, nkv.PAGES_FP4])
+def test_scratch_is_what_the_header_says(fmt):
+    """Few columns: (stretches + units) * columns * (d + 4) * 4 bytes and 16 a unit, or none; more of them: 33 MiB at most."""
+    n, needed = C.c_size_t(0), set()
+    for d, stretches in ((64, 4096), (96, 3072), (128, 3072), (192, 2048), (256, 2048)):
+        for S in (1, 2, 31, 256, 1024):
+            for H in (1, 8):
+                for width in (1, 4, 5, 20, 21, 32, 33, 100, 1000):
+                    for cols in (1, 5, 16, 17, 32, 33, 64, 257, 1000, 20000):
+                        assert nkv.lib().nkv_pages_prompt_workspace_bytes(C.byref(_pages(n_seqs=S, H=H, d=d, format=fmt, max_pages=width)), H * cols, 1, C.byref(n)) == 0
+                        units, few = S * H, cols <= 16 and width > 20 if fmt == nkv.PAGES_16BIT else cols <= (32 if width > 32 else 16)
+                        parts = min(stretches, 4 * ((units * width + 3) // 4)) + units
+                        bound = parts * cols * (d + 4) * 4 + (16 * units + 255) // 256 * 256
+                        what = f"{units} units of {width} pages, {cols} columns of {d} dims"
+                        assert n.value in (0, bound) if few else n.value <= 33 << 20, what
+                        needed.add((few, n.value > 0))
+    assert len(needed) == 4
+    if fmt == nkv.PAGES_FP4:                                                # (the header's figures)
+        for S, mib in ((1, 50), (256, 83), (1024, 182)):
+            assert nkv.lib().nkv_pages_prompt_workspace_bytes(C.byref(_pages(n_seqs=S, H=8, d=128, format=fmt, max_pages=1000)), 256, 1, C.byref(n)) == 0
+            assert round(n.value / 2 ** 20) == mib
+
+
 def test_binding_refuses():
     z = lambda *s, dt=torch.bfloat16: torch.zeros(*s, dtype=dt)  # noqa: E731
     table, lens = z(2, 3, dt=torch.int32), z(2, dt=torch.int32)
