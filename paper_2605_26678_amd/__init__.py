@@ -538,8 +538,8 @@ class LogitRules:
         for t, what, dtype in ((slopes, "slopes", torch.float32), (prefix, "prefix", torch.int32)):
             if t is not None and (t.dtype is not dtype or t.dim() != 1 or not t.is_contiguous()):
                 raise ValueError(f"{what} is contiguous {dtype} of one dim")
-        if not cap >= 0.0 or window < 0:
-            raise ValueError("cap and window are not negative")
+        if not cap >= 0.0 or window < 0 or int(window) >= 1 << 31:           # (ctypes cuts a longer number off)
+            raise ValueError("cap and window are not negative, and a window is of 31 bits")
         self.cap, self.window, self.slopes, self.prefix = float(cap), int(window), slopes, prefix
         self.c = nkv_logit_rules(C.sizeof(nkv_logit_rules), self.window, self.cap, _ptr(slopes), _ptr(prefix))
         self.ref = C.byref(self.c)

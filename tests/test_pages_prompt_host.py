@@ -58,6 +58,14 @@ def test_scratch_is_bounded():
                     assert n.value < 80 << 20
 
 
+def test_windows_beyond_32_bits():
+    """A window is an int32 in the header: what is more is refused, not cut off."""
+    assert nkv.LogitRules(window=(1 << 31) - 1).c.window == (1 << 31) - 1
+    for window in (1 << 31, (1 << 32) + 5, 1 << 62):
+        with pytest.raises(ValueError):
+            nkv.LogitRules(window=window)
+
+
 @pytest.mark.parametrize("fmt", [nkv.PAGES_16BIT, nkv.PAGES_FP4])
 def test_scratch_is_what_the_header_says(fmt):
     """Few columns: (stretches + units) * columns * (d + 4) * 4 bytes and 16 a unit, or none; more of them: 33 MiB at most."""
