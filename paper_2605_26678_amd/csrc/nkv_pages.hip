@@ -182,8 +182,11 @@ __device__ __forceinline__ Span span_of(const int64_t *head_off, const int32_t *
 
 // Packed rows to and from the pages.  A workgroup takes one page of one unit: 16 rows at a time, D / 8 threads a row.  The pages that a unit's
 // rows touch are numbered from off[u] / 64 + 2 u on, which leaves room for all of them (n rows touch at most n / 64 + 2 pages), so no kernel plans in front.
-// grid: as many numbers as there are.  (Pages of 16-bit rows are read past the caches as well as written past them: 36 x 8 units of some 3700 rows of 128 dims 264 -> 205 us,
-// 5.3 TB/s.)
+// grid: as many numbers as there are.
+// Pages of 16-bit rows are read past the caches, whatever their number: what a read finds in the last-level cache it takes faster through the caches, but where other writes came in
+// between that costs more than it gains, and the host does not know which it is.  us of a read of 128 dims, through the caches and past them:
+//   after other writes             8 MiB of rows 10.5 and 8.9;  32 MiB 23.4 and 17.4;  128 MiB 82 and 54;  520 MiB 261 and 194 (5.6 TB/s)
+//   after the load of these rows   8 MiB 7.3 and 7.2;  32 MiB 14.1 and 17.0;  128 MiB 43 and 62;  288 MiB 162 and 129;  520 MiB 264 and 212
 template <int D, bool F16, bool FP4, bool LOAD>
 __global__ __launch_bounds__(2 * D) void rows_kernel(uint16_t *__restrict__ pk, uint16_t *__restrict__ pv, const int64_t *__restrict__ head_off,
                                                     int64_t rows, int n_units, uint8_t *__restrict__ pool, const int32_t *__restrict__ table,

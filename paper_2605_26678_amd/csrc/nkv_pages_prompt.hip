@@ -7,7 +7,8 @@
 namespace nkv {
 namespace {
 
-// Tables of up to that many pages: all rows in one launch.  (8 KV heads of 400 rows: 14 us so, shared out 12; of 64 rows 7.5, single tokens' kernels 11.5)
+// Tables of up to that many pages: all rows in one launch, and no scratch.  That costs where the tiles are few: 256 rows, us so and shared out in two, 128 columns of a unit of 256 dims
+// 26.9 and 21.2, 256 of 128 dims 17.8 and 15.3; 8 units of 256 columns of 128 dims are not shared out by the rule below either (18.1 and 18.1).
 constexpr int kShort = 4;
 
 struct Grid {
@@ -29,17 +30,18 @@ Grid grid_of(const nkv_pages &p, int n_q_heads, int n_new)
     return {(int)tiles, splits > 1 && walk / splits + splits * part + 2 < walk ? splits : 1};
 }
 
-// Whether a call goes with the single tokens' kernels.  They share out all units' pages evenly and take up to 16 columns at a time, in some 10 us and what memory takes; the
-// tiles take a page a microsecond in each workgroup whatever the columns, in one launch or two.  us, theirs / tiles, 8 KV heads of 128 dims:
-//   4 bits    16 columns: 1024 rows of 1, 32 sequences 10.6 / 11.6, 22 / 29; 16384 rows 15 / 24, 110 / 364
-//             32 columns: 1024 rows 11.1 / 11.8, 40 / 29; 4096 rows 12 / 16, 73 / 95; 16384 rows 24 / 25, 214 / 365
-//             64 columns: 4096 rows 15 / 19, 140 / 97;  one column, 3 rows of 33 sequences with 32 heads 15 / 29
-//   16 bits   8 columns: 600 rows 11.8 / 10.1, 25 / 19; 1024 rows 12.5 / 10.9, 39 / 28; 4096 rows 12.5 / 13.6, 92 / 96; 16384 rows 21 / 23, 284 / 354
-//             32 columns: 4096 rows 19 / 16, 208 / 98
+// Whether a call goes with the single tokens' kernels, where no workgroup has a unit to itself (below).  They share out all units' pages evenly and take up to 16 columns at a time, in some
+// 10 us and what memory takes; the tiles take a page a microsecond in each workgroup whatever the columns, in one launch or two.  us, theirs / tiles, 8 KV heads of 128 dims:
+//   4 bits    16 columns: 16384 rows of 1, 32 sequences 15 / 22, 112 / 363
+//             32 columns: 1024 rows 10.6 / 10.8, 37 / 27; 4096 rows 11 / 16, 79 / 90; 16384 rows 23 / 23, 216 / 363
+//             64 columns: 4096 rows 13 / 17, 150 / 93;  one column, 3 rows of 33 sequences with 32 heads 14 / 26
+//   16 bits   8 columns: 600, 1024 rows of 1 sequence 12.8 / 10.6, 11.9 / 10.3; 1 sequence of up to 1400, 4096, 16384 rows (a quarter to all of them, as units have) 12.7 / 11.3, 13.4 / 12.7, 16.5 / 20.8;
+//             4 of 1400, 4096, 16384 13.8 / 11.9, 20.8 / 18.9, 50 / 48; 32 of 16384 246 / 346, and all of the same length 366 / 365
+//             32 columns: 4096 rows of 1, 32 sequences 14.5 / 15.7, 246 / 98
+// (16 bits, some thousand rows of a few sequences: up to 2 us more than the tiles take.)
 bool few_columns(const nkv_pages &p, int n_q_heads, int n_new)
 {
     const int64_t cols = (int64_t)(n_q_heads / p.H) * n_new;
-    if (p.max_pages <= kShort && p.n_seqs * p.H <= 512) return false;
     return p.format == NKV_PAGES_FP4 ? cols <= (p.max_pages > 32 ? 32 : 16) : cols <= 16 && p.max_pages > 20;
 }
 
